@@ -62,7 +62,7 @@ typedef enum {
 
 enum { GTA_F32 = 0, GTA_BF16 = 1 };            /* gta_config.dtype */
 enum { GTA_GATE_SIGMOID = 0, GTA_GATE_OFF = 1, GTA_GATE_SILU = 2, GTA_GATE_RELU2 = 3 }; /* gta_config.gate  */
-enum { GTA_MODE_PREFILL = 0, GTA_MODE_DECODE = 1, GTA_MODE_PREFILL_CHUNK = 2 };
+enum { GTA_MODE_PREFILL = 0, GTA_MODE_DECODE = 1, GTA_MODE_PREFILL_CHUNK = 2, GTA_MODE_MX_DECODE = 3 };
 
 /* Hyper-parameters of one GTA layer (Sec. 3.2).  Host memory. */
 typedef struct {
@@ -123,12 +123,39 @@ typedef struct {
   int32_t  num_pages;
 } gta_cache;
 
+/* The same caches with rows of 8 bits: keys and latent values as e4m3 codes in blocks of GTA_MX_BLOCK
+ * elements of one head (key rows) or latent group, and one scale byte e + 127 per block: an element is
+ * code * 2^e.  e is the least exponent with which the block's largest finite magnitude is at most
+ * 448 * 2^e, kept within -117 .. 119: every stored value is zero or a normal bf16 number, and a code is
+ * the element rounded once, to 3 bits behind the leading one (2^-4 relative at most for magnitudes from
+ * 2^-6 * 2^e on, half of 2^-9 * 2^e absolute below).  NaN and infinities are stored as NaN and do not enter e.
+ * head_dim and latent_dim must be multiples of GTA_MX_BLOCK.  Struct host, arrays device, all
+ * 16-byte aligned (lengths, status and table 4).  Layouts and block table as in gta_cache: row p of a
+ * slot has the same index in all four arrays. */
+#define GTA_MX_BLOCK 32
+typedef struct {
+  void    *k;         /* codes, width n_k*d_h bytes */
+  void    *c;         /* codes, width n_c*d_l bytes */
+  uint8_t *k_scale;   /* scale bytes, width n_k*d_h / 32 */
+  uint8_t *c_scale;   /* scale bytes, width n_c*d_l / 32 */
+  int32_t *seq_lens;  /* [max_batch] */
+  int32_t *status;    /* [max_batch]; as in gta_cache */
+  int32_t  max_batch;
+  int32_t  max_seq;
+  const int32_t *block_table; /* [max_batch, pages_per_slot] device, or NULL */
+  int32_t  page_size;
+  int32_t  pages_per_slot;
+  int32_t  num_pages;
+} gta_mx_cache;
+
 /* Bytes of device workspace the call described by the arguments needs.
  *   mode PREFILL: batch sequences, total_tokens packed tokens, longest sequence <= max_len.
  *   mode DECODE : batch sequences, max_len = cache->max_seq, num_splits as passed to gta_decode
  *                 (0 = library's choice; a call with a smaller workspace that still holds context
  *                 slices of at least 256 rows runs with those).
  *   mode PREFILL_CHUNK: as PREFILL, for gta_prefill_chunk (max_len = max_chunk).
+ *   mode MX_DECODE: for gta_mx_decode_attention (max_len = cache->max_seq, num_splits as passed there;
+ *                 with 0, a smaller workspace that holds one split is used with the splits it holds).
  * Returns 0 if cfg is NULL or invalid. */
 GTA_API size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64_t total_tokens,
                            int32_t max_len, int32_t num_splits);
@@ -206,6 +233,57 @@ GTA_API int gta_decode_static(const gta_config *cfg, const gta_weights *weights,
 GTA_API int gta_cache_append(const gta_config *cfg, const gta_cache *cache, const int32_t *slots,
                      const void *k_new, const void *c_new, const int32_t *cu_new, int32_t batch,
                      int32_t max_new, void *hip_stream);
+
+/* RMS norm of every query and key head, then its rotation, in one pass:
+ *   y_j = x_j / sqrt(mean_i x_i^2 + eps) * gain_j  (i, j within one head), then, with cfg->rope, the
+ *   pair (j, j + d_h/2) turned by position * rope_base^(-2j/d_h).  Computed in fp32 (angles in fp64) and
+ *   rounded once.  For models that norm their queries and keys: project with rope = 0
+ *   (gta_prefill_projection, for a decode step with one token per sequence), then call this.
+ *   q, k        device, rows of n_q*d_h and n_k*d_h elements, q_stride and k_stride elements apart (at
+ *               least the width): columns of one wide projection's output will do.  Aligned to an
+ *               element; rows of 16-byte aligned chunks run faster
+ *   q_gain, k_gain  device [d_h], element type = cfg->dtype, or NULL for ones
+ *   positions   device [total_tokens], or NULL: 0 .. total_tokens - 1.  Not read with rope = 0.  For a
+ *               decode step over slots 0 .. batch-1 it is cache->seq_lens as it is before the append
+ *   q_out [total_tokens, n_q*d_h], k_out [total_tokens, n_k*d_h]  device, dense.  An output may be its
+ *               own input where that is dense; otherwise outputs and inputs must not overlap
+ * eps must be finite and not negative. */
+GTA_API int gta_qk_norm_rope(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                             const void *q_gain, const void *k_gain, float eps, const int32_t *positions,
+                             int64_t total_tokens, void *q_out, void *k_out, void *hip_stream);
+
+/* gta_cache_append for 8-bit caches: rows [cu_new[b], cu_new[b+1]) of k_new / c_new (element type =
+ * cfg->dtype) are quantised (see gta_mx_cache) into slot slots[b] behind its seq_lens[slot] rows, then
+ * seq_lens[slot] += their count.  A sequence that does not fit stores nothing and is flagged
+ * GTA_ERR_CACHE_FULL; one of more than max_new rows stores nothing and is flagged GTA_ERR_SHAPE.
+ *   k_new   rows of n_k*d_h elements, k_stride elements apart;  c_new  rows of n_c*d_l, c_stride apart;
+ *           aligned to an element, strides at least the widths
+ *   cu_new  device [batch+1];  slots device [batch] distinct slots or NULL
+ *   max_new host upper bound of rows per sequence (sizes the launch) */
+GTA_API int gta_mx_cache_append(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const void *k_new,
+                                int64_t k_stride, const void *c_new, int64_t c_stride, const int32_t *cu_new,
+                                int32_t batch, int32_t max_new, void *hip_stream);
+
+/* Reads cached rows back: rows first[b] .. first[b] + n_b - 1 of slot slots[b], n_b = cu_rows[b+1] - cu_rows[b],
+ * become rows [cu_rows[b], cu_rows[b+1]) of k_out [total, n_k*d_h] and c_out [total, n_c*d_l] (element
+ * type = cfg->dtype; nothing is rounded).  Rows outside 0 .. seq_lens[slot] - 1, rows without a page and
+ * slots out of range read as zeros.  A sequence of more than max_rows rows is skipped and its slot's
+ * status set to GTA_ERR_SHAPE.
+ *   first   device [batch], or NULL for zeros;  cu_rows device [batch+1];  slots device [batch] or NULL
+ * With gta_cache_append the rows go on into a gta_cache, e.g. for gta_prefill_chunk. */
+GTA_API int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const int32_t *first,
+                              const int32_t *cu_rows, int32_t batch, int32_t max_rows, void *k_out, void *c_out,
+                              void *hip_stream);
+
+/* Attention of one new token per sequence over the seq_lens[slot] rows in an 8-bit cache (its own row
+ * appended before): l_out[b, g*d_l : (g+1)*d_l] = sum_t Softmax_t(q_g . k_{k(g)}[t] * scale) c_{c(g)}[t].
+ *   q [batch, n_q*d_h] rotated queries, l_out [batch, n_q*d_l]; device, element type = cfg->dtype
+ *   num_splits  context splits per sequence; 0 = library's choice;  workspace: mode MX_DECODE
+ * Sums and softmax statistics are fp32.  A sequence without rows, or with a slot out of range, gets zeros.
+ * l_out goes on into gta_prefill_decoder.  head_dim up to 1024 and latent_dim up to 4096. */
+GTA_API int gta_mx_decode_attention(const gta_config *cfg, const void *q, const gta_mx_cache *cache, const int32_t *slots,
+                                    int32_t batch, int32_t num_splits, void *l_out, void *workspace,
+                                    size_t workspace_bytes, void *hip_stream);
 
 /* ---- stage entry points: one stage of the pass on already projected inputs, in the launch
  * configuration gta_prefill / gta_decode use (for stage-wise tests and per-kernel timing). ---- */

@@ -17,15 +17,17 @@ GTA_F32, GTA_BF16 = 0, 1
 GTA_GATE_SIGMOID, GTA_GATE_OFF, GTA_GATE_SILU, GTA_GATE_RELU2 = 0, 1, 2, 3
 GATE_CODES = {True: GTA_GATE_SIGMOID, "sigmoid": GTA_GATE_SIGMOID, False: GTA_GATE_OFF, "off": GTA_GATE_OFF,
               "silu": GTA_GATE_SILU, "relu2": GTA_GATE_RELU2}
-GTA_MODE_PREFILL, GTA_MODE_DECODE, GTA_MODE_PREFILL_CHUNK = 0, 1, 2
+GTA_MODE_PREFILL, GTA_MODE_DECODE, GTA_MODE_PREFILL_CHUNK, GTA_MODE_MX_DECODE = 0, 1, 2, 3
 GTA_OK = 0
 GTA_ERR_NULL, GTA_ERR_SHAPE, GTA_ERR_ALIGN, GTA_ERR_DTYPE = -1, -2, -3, -4
 GTA_ERR_UNSUPPORTED, GTA_ERR_WORKSPACE, GTA_ERR_HIP, GTA_ERR_CACHE_FULL = -5, -6, -7, -8
 
 GTA_STATIC_SCRATCH_BYTES = 32 << 20
+GTA_MX_BLOCK = 32
 EXPORTS = ["gta_workspace_bytes", "gta_prefill", "gta_prefill_chunk", "gta_decode", "gta_decode_static", "gta_cache_append", "gta_strerror",
            "gta_uses_tuned_kernels", "gta_prefill_projection", "gta_prefill_decoder", "gta_output_projection", "gta_prefill_attention", "gta_decode_attention", "gta_decode_combine", "gta_calibration_copy",
-           "gta_calibration_read", "gta_calibration_mfma"]
+           "gta_calibration_read", "gta_calibration_mfma", "gta_qk_norm_rope", "gta_mx_cache_append", "gta_mx_cache_read",
+           "gta_mx_decode_attention"]
 
 
 class gta_config(ctypes.Structure):
@@ -43,6 +45,13 @@ class gta_cache(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("c", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
                 ("status", ctypes.c_void_p), ("max_batch", ctypes.c_int32), ("max_seq", ctypes.c_int32),
                 ("block_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
+                ("pages_per_slot", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class gta_mx_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("c", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("c_scale", ctypes.c_void_p),
+                ("seq_lens", ctypes.c_void_p), ("status", ctypes.c_void_p), ("max_batch", ctypes.c_int32),
+                ("max_seq", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
                 ("pages_per_slot", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
 
 
@@ -100,6 +109,15 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.gta_calibration_read.argtypes = [vp, i64, ctypes.c_int32, vp, vp]
     lib.gta_calibration_mfma.restype = ctypes.c_int
     lib.gta_calibration_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, vp, vp]
+    mp, f32 = ctypes.POINTER(gta_mx_cache), ctypes.c_float
+    lib.gta_qk_norm_rope.restype = ctypes.c_int
+    lib.gta_qk_norm_rope.argtypes = [cfgp, vp, i64, vp, i64, vp, vp, f32, vp, i64, vp, vp, vp]
+    lib.gta_mx_cache_append.restype = ctypes.c_int
+    lib.gta_mx_cache_append.argtypes = [cfgp, mp, vp, vp, i64, vp, i64, vp, i32, i32, vp]
+    lib.gta_mx_cache_read.restype = ctypes.c_int
+    lib.gta_mx_cache_read.argtypes = [cfgp, mp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.gta_mx_decode_attention.restype = ctypes.c_int
+    lib.gta_mx_decode_attention.argtypes = [cfgp, vp, mp, vp, i32, i32, vp, vp, sz, vp]
     lib.gta_strerror.restype = ctypes.c_char_p
     lib.gta_strerror.argtypes = [ctypes.c_int]
     lib.gta_uses_tuned_kernels.restype = ctypes.c_int
@@ -156,6 +174,19 @@ def make_paged_cache(k_pool, c_pool, seq_lens, status, block_table) -> gta_cache
     slots, pps = block_table.shape
     return gta_cache(_ptr(k_pool), _ptr(c_pool), _ptr(seq_lens), _ptr(status), slots, pps * k_pool.shape[1],
                      _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0])
+
+
+def make_mx_cache(k, c, k_scale, c_scale, seq_lens, status) -> gta_mx_cache:
+    """k [slots, max_seq, n_k*d_h] and c [slots, max_seq, n_c*d_l] of 8 bits (float8_e4m3fn or uint8), k_scale and c_scale
+    uint8 with one byte per 32 elements of a row, seq_lens/status int32 [slots] (device)."""
+    return gta_mx_cache(_ptr(k), _ptr(c), _ptr(k_scale), _ptr(c_scale), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1])
+
+
+def make_paged_mx_cache(k_pool, c_pool, k_scale, c_scale, seq_lens, status, block_table) -> gta_mx_cache:
+    """The same in pools [num_pages, page_size, width], with a block_table as make_paged_cache takes it."""
+    slots, pps = block_table.shape
+    return gta_mx_cache(_ptr(k_pool), _ptr(c_pool), _ptr(k_scale), _ptr(c_scale), _ptr(seq_lens), _ptr(status), slots,
+                        pps * k_pool.shape[1], _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0])
 
 
 def _check(rc: int, where: str) -> None:
@@ -284,6 +315,45 @@ def gta_decode_combine(cfg: gta_config, cache: gta_cache, slots, batch: int, num
                                    _stream(stream))
     if check:
         _check(rc, "gta_decode_combine")
+    return rc
+
+
+def gta_qk_norm_rope(cfg: gta_config, q, q_stride: int, k, k_stride: int, q_gain, k_gain, eps: float, positions,
+                     total_tokens: int, q_out, k_out, stream=None, check: bool = True) -> int:
+    rc = load().gta_qk_norm_rope(ctypes.byref(cfg), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_gain), _ptr(k_gain), eps,
+                                 _ptr(positions), total_tokens, _ptr(q_out), _ptr(k_out), _stream(stream))
+    if check:
+        _check(rc, "gta_qk_norm_rope")
+    return rc
+
+
+def gta_mx_cache_append(cfg: gta_config, cache: gta_mx_cache, slots, k_new, k_stride: int, c_new, c_stride: int, cu_new,
+                        batch: int, max_new: int, stream=None, check: bool = True) -> int:
+    rc = load().gta_mx_cache_append(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _ptr(slots),
+                                    _ptr(k_new), k_stride, _ptr(c_new), c_stride, _ptr(cu_new), batch, max_new,
+                                    _stream(stream))
+    if check:
+        _check(rc, "gta_mx_cache_append")
+    return rc
+
+
+def gta_mx_cache_read(cfg: gta_config, cache: gta_mx_cache, slots, first, cu_rows, batch: int, max_rows: int, k_out, c_out,
+                      stream=None, check: bool = True) -> int:
+    rc = load().gta_mx_cache_read(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _ptr(slots),
+                                  _ptr(first), _ptr(cu_rows), batch, max_rows, _ptr(k_out), _ptr(c_out), _stream(stream))
+    if check:
+        _check(rc, "gta_mx_cache_read")
+    return rc
+
+
+def gta_mx_decode_attention(cfg: gta_config, q, cache: gta_mx_cache, slots, batch: int, num_splits: int, l_out, workspace,
+                            stream=None, check: bool = True) -> int:
+    rc = load().gta_mx_decode_attention(ctypes.byref(cfg), _ptr(q), ctypes.byref(cache) if cache is not None else None,
+                                        _ptr(slots), batch, num_splits, _ptr(l_out), _ptr(workspace),
+                                        0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                        _stream(stream))
+    if check:
+        _check(rc, "gta_mx_decode_attention")
     return rc
 
 

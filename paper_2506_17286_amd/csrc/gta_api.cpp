@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include "gta_internal.h"
+#include "gta_mx.h"
 #include "gta_tuned.h"
 
 namespace gta {
@@ -191,6 +192,17 @@ static int check_cache(const gta_cache *c) {
   return GTA_OK;
 }
 
+static int check_mx_cache(const gta_mx_cache *c) {
+  if (!c->k_scale || !c->c_scale) return GTA_ERR_NULL;
+  if (misaligned(c->k_scale) || misaligned(c->c_scale)) return GTA_ERR_ALIGN;
+  const gta_cache same{c->k, c->c, c->seq_lens, c->status, c->max_batch, c->max_seq,
+                       c->block_table, c->page_size, c->pages_per_slot, c->num_pages};
+  return check_cache(&same);
+}
+
+// A row stride in elements: at least the width, and no product with a row number that leaves 64 bits.
+static bool bad_stride(int64_t stride, int width) { return stride < width || stride > ((int64_t)1 << 28); }
+
 static const int kMaxBatch = 65535;  // grid.y / grid.z limit
 
 // ---- fixed scratch of gta_decode_static ---------------------------------------------------------
@@ -219,6 +231,10 @@ static int static_scratch(void **out) {
   }
   *out = scratch_of_device[dev];
   return GTA_OK;
+}
+
+static int mx_splits(const Dims &d, int batch, int max_seq, int requested) {
+  return requested > 0 ? std::min(requested, 1024) : mx_decode_splits(d, batch, max_seq);
 }
 
 static bool decode_is_tuned(const Dims &d, const gta_cache &c) {
@@ -280,6 +296,10 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
     if (total_tokens < 0) return 0;
     // sized for a call with W_O (a superset of the call without)
     return carve_prefill(d, tuned_prefill_supported(d), true, batch, total_tokens, max_len, nullptr).bytes + 256;
+  }
+  if (mode == GTA_MODE_MX_DECODE) {
+    if (!mx_decode_dims_ok(d) || num_splits < 0) return 0;
+    return mx_split_bytes(d, batch) * (size_t)mx_splits(d, batch, max_len, num_splits) + 256;
   }
   if (mode == GTA_MODE_DECODE) {
     int splits = choose_splits(d, batch, max_len, num_splits);
@@ -461,6 +481,79 @@ int gta_output_projection(const gta_config *cfg, const gta_weights *weights, con
   if (total_tokens == 0) return GTA_OK;
   launch_plain_gemm(heads, d.wg_w, (int)total_tokens, d.H, d.wg_w, weights->wo, out, (hipStream_t)hip_stream);
   return check_launch();
+}
+
+int gta_qk_norm_rope(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const void *q_gain, const void *k_gain, float eps, const int32_t *positions, int64_t total_tokens,
+                     void *q_out, void *k_out, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!q || !k || !q_out || !k_out) return GTA_ERR_NULL;
+  if (total_tokens < 0 || total_tokens > INT32_MAX || !(eps >= 0.f) || !(eps <= 3e38f)) return GTA_ERR_SHAPE;
+  if (bad_stride(q_stride, d.wq_w) || bad_stride(k_stride, d.wk_w)) return GTA_ERR_SHAPE;
+  const uintptr_t el = (uintptr_t)d.esize() - 1;
+  if (misaligned(q_out) || misaligned(k_out) || (((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_gain | (uintptr_t)k_gain) & el) ||
+      ((uintptr_t)positions & 3u))
+    return GTA_ERR_ALIGN;
+  if (total_tokens * (int64_t)(d.nq + d.nk) > ((int64_t)1 << 32)) return GTA_ERR_UNSUPPORTED;   // launch size
+  if (total_tokens == 0) return GTA_OK;
+  return launch_qk_norm_rope(d, q, q_stride, k, k_stride, q_gain, k_gain, eps, positions, total_tokens, q_out, k_out,
+                             (hipStream_t)hip_stream);
+}
+
+int gta_mx_cache_append(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const void *k_new,
+                        int64_t k_stride, const void *c_new, int64_t c_stride, const int32_t *cu_new, int32_t batch,
+                        int32_t max_new, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!cache || !k_new || !c_new || !cu_new) return GTA_ERR_NULL;
+  if ((rc = check_mx_cache(cache)) != GTA_OK) return rc;
+  if (!mx_widths_ok(d)) return GTA_ERR_UNSUPPORTED;
+  if (batch <= 0 || batch > kMaxBatch || max_new < 0 || max_new > (1 << 30) || (!slots && batch > cache->max_batch))
+    return GTA_ERR_SHAPE;
+  if (bad_stride(k_stride, d.wk_w) || bad_stride(c_stride, d.wc_w)) return GTA_ERR_SHAPE;
+  const uintptr_t el = (uintptr_t)d.esize() - 1;
+  if ((((uintptr_t)k_new | (uintptr_t)c_new) & el) || ((uintptr_t)cu_new & 3u) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
+  return launch_mx_append(d, mx_view_of(*cache, slots), k_new, k_stride, c_new, c_stride, cu_new, batch, max_new,
+                          (hipStream_t)hip_stream);
+}
+
+int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const int32_t *first,
+                      const int32_t *cu_rows, int32_t batch, int32_t max_rows, void *k_out, void *c_out, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!cache || !cu_rows || !k_out || !c_out) return GTA_ERR_NULL;
+  if ((rc = check_mx_cache(cache)) != GTA_OK) return rc;
+  if (!mx_widths_ok(d)) return GTA_ERR_UNSUPPORTED;
+  if (batch <= 0 || batch > kMaxBatch || max_rows < 0 || max_rows > (1 << 30) || (!slots && batch > cache->max_batch))
+    return GTA_ERR_SHAPE;
+  if (misaligned(k_out) || misaligned(c_out) || ((uintptr_t)cu_rows & 3u) || ((uintptr_t)slots & 3u) || ((uintptr_t)first & 3u))
+    return GTA_ERR_ALIGN;
+  return launch_mx_read(d, mx_view_of(*cache, slots), first, cu_rows, batch, max_rows, k_out, c_out, (hipStream_t)hip_stream);
+}
+
+int gta_mx_decode_attention(const gta_config *cfg, const void *q, const gta_mx_cache *cache, const int32_t *slots,
+                            int32_t batch, int32_t num_splits, void *l_out, void *workspace, size_t workspace_bytes,
+                            void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!q || !cache || !l_out) return GTA_ERR_NULL;
+  if ((rc = check_mx_cache(cache)) != GTA_OK) return rc;
+  if (!mx_decode_dims_ok(d)) return GTA_ERR_UNSUPPORTED;
+  if (batch <= 0 || batch > kMaxBatch || num_splits < 0 || (!slots && batch > cache->max_batch)) return GTA_ERR_SHAPE;
+  if (misaligned(q) || misaligned(l_out) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
+  if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
+  int splits = mx_splits(d, batch, cache->max_seq, num_splits);
+  const size_t fit = workspace_bytes / mx_split_bytes(d, batch);
+  if (fit < (size_t)splits) {
+    if (num_splits > 0 || fit == 0) return GTA_ERR_WORKSPACE;
+    splits = (int)fit;
+  }
+  return launch_mx_decode(d, q, mx_view_of(*cache, slots), batch, splits, (float *)workspace, l_out, (hipStream_t)hip_stream);
 }
 
 static int decode_stage_args(const gta_config *cfg, const gta_cache *cache, const int32_t *slots, int32_t batch,
