@@ -37,6 +37,7 @@ int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const 
 
 // Attention of one token per sequence: partial sums [batch, splits, n_q, d_l], then (maximum, sum) [batch, splits, n_q, 2].
 bool mx_decode_dims_ok(const Dims &d);
+bool mx_decode_tuned(const Dims &d);   // taken by the matrix-instruction kernel, with pages of a power of two of at least 16 rows
 int mx_decode_splits(const Dims &d, int batch, int max_seq);
 inline size_t mx_split_bytes(const Dims &d, int batch) { return (size_t)batch * d.nq * ((size_t)d.dl + 2) * 4; }
 int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int splits, float *part, void *l_out, hipStream_t st);
