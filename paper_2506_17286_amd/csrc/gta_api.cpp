@@ -233,10 +233,6 @@ static int static_scratch(void **out) {
   return GTA_OK;
 }
 
-static int mx_splits(const Dims &d, int batch, int max_seq, int requested) {
-  return requested > 0 ? std::min(requested, 1024) : mx_decode_splits(d, batch, max_seq);
-}
-
 static bool decode_is_tuned(const Dims &d, const gta_cache &c) {
   return tuned_decode_supported(d) && tuned_decode_layout_ok(c);
 }
@@ -299,7 +295,7 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
   }
   if (mode == GTA_MODE_MX_DECODE) {
     if (!mx_decode_dims_ok(d) || num_splits < 0) return 0;
-    return mx_split_bytes(d, batch) * (size_t)mx_splits(d, batch, max_len, num_splits) + 256;
+    return mx_decode_bytes(d, batch, max_len, num_splits) + 256;
   }
   if (mode == GTA_MODE_DECODE) {
     int splits = choose_splits(d, batch, max_len, num_splits);
@@ -547,13 +543,8 @@ int gta_mx_decode_attention(const gta_config *cfg, const void *q, const gta_mx_c
   if (batch <= 0 || batch > kMaxBatch || num_splits < 0 || (!slots && batch > cache->max_batch)) return GTA_ERR_SHAPE;
   if (misaligned(q) || misaligned(l_out) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
   if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
-  int splits = mx_splits(d, batch, cache->max_seq, num_splits);
-  const size_t fit = workspace_bytes / mx_split_bytes(d, batch);
-  if (fit < (size_t)splits) {
-    if (num_splits > 0 || fit == 0) return GTA_ERR_WORKSPACE;
-    splits = (int)fit;
-  }
-  return launch_mx_decode(d, q, mx_view_of(*cache, slots), batch, splits, (float *)workspace, l_out, (hipStream_t)hip_stream);
+  return launch_mx_decode(d, q, mx_view_of(*cache, slots), batch, num_splits, workspace, workspace_bytes, l_out,
+                          (hipStream_t)hip_stream);
 }
 
 static int decode_stage_args(const gta_config *cfg, const gta_cache *cache, const int32_t *slots, int32_t batch,

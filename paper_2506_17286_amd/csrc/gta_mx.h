@@ -35,12 +35,13 @@ int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t
 int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const int32_t *cu_rows, int batch, int max_rows,
                    void *k_out, void *c_out, hipStream_t st);
 
-// Attention of one token per sequence: partial sums [batch, splits, n_q, d_l], then (maximum, sum) [batch, splits, n_q, 2].
+// Attention of one token per sequence.
 bool mx_decode_dims_ok(const Dims &d);
 bool mx_decode_tuned(const Dims &d);   // taken by the matrix-instruction kernel, with pages of a power of two of at least 16 rows
-int mx_decode_splits(const Dims &d, int batch, int max_seq);
-inline size_t mx_split_bytes(const Dims &d, int batch) { return (size_t)batch * d.nq * ((size_t)d.dl + 2) * 4; }
-int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int splits, float *part, void *l_out, hipStream_t st);
+size_t mx_decode_bytes(const Dims &d, int batch, int max_seq, int requested);
+// GTA_ERR_WORKSPACE, with nothing launched, where the workspace is too small
+int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int requested, void *ws, size_t ws_bytes, void *l_out,
+                     hipStream_t st);
 
 int launch_qk_norm_rope(const Dims &d, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_gain,
                         const void *k_gain, float eps, const int32_t *positions, int64_t total, void *q_out, void *k_out,

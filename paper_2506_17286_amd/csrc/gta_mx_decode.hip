@@ -21,10 +21,11 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 struct MxAttnArgs {
   const void *q;
   MxView cv;
-  int nq, qpk, qpc, dh, dl, kw, cw, splits, ps_shift;
+  int nq, qpk, qpc, dh, dl, kw, cw, batch, splits, ps_shift;
   float scale_log2e;
-  float *pacc, *pml;   // [batch, splits, n_q, d_l], [batch, splits, n_q, 2]
-  void *l_out;         // the result itself where there is one split, or NULL
+  float *pacc, *pml;   // [pieces, n_q, d_l], [pieces, n_q, 2]
+  int32_t *prefix;     // [batch + 1] row tiles in front of each sequence, where the tiles of a batch are shared out evenly
+  void *l_out;
 };
 
 // rows of the slot that take part
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
       }
     __syncthreads();
   }
-  const int64_t at = ((int64_t)b * a.splits + s) * a.nq + g;
+  const int64_t at = ((int64_t)b * a.splits + s) * a.nq + g;   // every split writes, those without rows too
   float *out = a.pacc + at * a.dl;
   if (groups == 1) {
     for (int v = 0; v * 256 + my < quads; ++v)
@@ -177,183 +178,312 @@ template <> struct Word<16> { typedef u32x4 type; };
 constexpr float kLowest = -3e38f;   // stands for "no score yet" where a difference is taken
 constexpr float kMostAbove = 40.f;
 
-template <typename T, int KB, int CS, int TT, int OCC>
+// Sequences that the batch's tiles are shared out over; a larger batch has a workgroup per sequence.
+constexpr int kShareBatch = 1024;
+constexpr int kTile = 32;
+
+// Tiles of rows in front of each sequence (LDS, batch + 1 entries); returns their number.
+__device__ __forceinline__ int scan_tiles(const MxView &cv, int batch, int tt, int *prefix, int *wsum) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  int before = 0;
+#pragma unroll 1
+  for (int b0 = 0; b0 < batch; b0 += 256) {
+    const int b = b0 + tid;
+    int slot;
+    const int mine = b < batch ? (mx_rows(cv, b, slot) + tt - 1) / tt : 0;
+    int run = mine;
+#pragma unroll
+    for (int i = 1; i < 64; i <<= 1) {
+      const int v = __shfl_up(run, i);
+      if (lane >= i) run += v;
+    }
+    if (b0) __syncthreads();
+    if (lane == 63) wsum[tid >> 6] = run;
+    __syncthreads();
+    const int w0 = wsum[0], w1 = wsum[1], w2 = wsum[2];
+    run += before + (tid >= 64 ? w0 : 0) + (tid >= 128 ? w1 : 0) + (tid >= 192 ? w2 : 0);
+    if (b < batch) prefix[b + 1] = run;
+    before += w0 + w1 + w2 + wsum[3];
+  }
+  if (tid == 0) prefix[0] = 0;
+  __syncthreads();
+  return before;
+}
+
+// Workgroup w of `share` has tiles [share_begin(w), share_begin(w + 1)) of `tiles`, one more each for the first of them;
+// share_of is the workgroup that has tile u.  tiles >= share.
+__device__ __forceinline__ int share_begin(int tiles, int w, int share) { return w * (tiles / share) + min(w, tiles % share); }
+__device__ __forceinline__ int share_of(int tiles, int u, int share) {
+  const int q = tiles / share, r = tiles % share, more = r * (q + 1);
+  return u < more ? u / (q + 1) : r + (u - more) / q;
+}
+// Workgroups that get tiles: at least kLeastTiles each.
+constexpr int kLeastTiles = 4;
+__device__ __forceinline__ int share_count(int tiles, int share) { return max(1, min(share, tiles / kLeastTiles)); }
+
+// KB bytes of a key row, CS latent columns of a workgroup.  WPT waves take a tile of 32 rows together where the sums of all columns
+// would not fit one wave's registers: each has the scores of its half of the rows, hands them to the other through LDS, and the
+// sums of its half of the columns.
+template <typename T, int KB, int CS, int WPT, int OCC, bool SHARED>
 __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int NQP = Parts<T>::Q, NPP = Parts<T>::P;
-  constexpr int HF = TT / 16, KP = KB / 64;                          // half tiles, key pieces
-  constexpr int LC = CS >= 256 ? 16 : CS / 16, NCH = CS / (16 * LC);   // bytes per lane and load, chunks
-  constexpr int KW = KB >= 128 ? KB / 128 : 1;                       // scale words of a key row: four bytes (two for one piece)
-  constexpr bool QREG = KB * NQP <= 256;
+  constexpr int HF = 2, KH = HF / WPT, KP = KB / 64;                     // half tiles, those this wave scores, key pieces
+  constexpr int CW = CS / WPT, LC = CW >= 256 ? 16 : CW / 16, NCH = CW / (16 * LC);   // this wave's columns, bytes per lane and load, chunks
+  constexpr int KW = KB >= 128 ? KB / 128 : 1;                           // scale words of a key row: four bytes (two for one piece)
+  constexpr int NS = 4 / WPT;                                            // tiles worked on at a time
+  constexpr bool QREG = KB * NQP <= 192;
   typedef typename Word<LC>::type CWord;
+  __shared__ int prefix[SHARED ? kShareBatch + 1 : 1], wsum[4];
+  __shared__ float sm[NS][16], sl[NS][16];
+  __shared__ f32x4 handed[WPT > 1 ? 2 : 1][NS][2][WPT > 1 ? 64 : 1];
   extern __shared__ char lds[];
   const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, h = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int s = blockIdx.x, z = blockIdx.y, b = blockIdx.z;
-  int slot, j0, j1;
-  const int n = mx_rows(a.cv, b, slot);
-  mx_slice(n, s, a.splits, TT, j0, j1);
-  const int64_t part = ((int64_t)b * a.splits + s) * a.nq;
-  if (j0 >= j1) {
-    if (a.l_out) {
-      for (int i = tid; i < a.nq * CS; i += 256) {
-        const int g = i / CS, col = z * CS + i % CS;
-        if (col / a.dl == g / a.qpc) ((T *)a.l_out)[((int64_t)b * a.nq + g) * a.dl + col % a.dl] = (T)0.f;
-      }
-    } else if (z == 0 && tid < a.nq) {
-      a.pml[(part + tid) * 2] = -INFINITY;
-      a.pml[(part + tid) * 2 + 1] = 0.f;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), stream = wave / WPT, role = wave % WPT;
+  const int z = blockIdx.y;
+
+  // ---- this workgroup's tiles [u0, u1), b the sequence of the first
+  int u0 = 0, u1 = 0, b = blockIdx.x;
+  const int wg = blockIdx.x;
+  if constexpr (SHARED) {
+    const int tiles = __builtin_amdgcn_readfirstlane(scan_tiles(a.cv, a.batch, kTile, prefix, wsum));
+    if (wg == 0 && z == 0)
+      for (int i = tid; i <= a.batch; i += 256) a.prefix[i] = prefix[i];
+    const int share = share_count(tiles, gridDim.x);
+    if (wg >= share || tiles == 0) return;
+    u0 = share_begin(tiles, wg, share);
+    u1 = u0 + tiles / share + (wg < tiles % share);
+    int lo = 0, hi = a.batch;   // the last sequence that begins at or before u0 (empty ones in front of it are passed over)
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (prefix[mid] <= u0) lo = mid; else hi = mid;
     }
-    return;
+    b = __builtin_amdgcn_readfirstlane(lo);
   }
-  const int nt = (j1 - j0 + TT - 1) / TT;
+  bool first_piece = true;
 
-  // pool row of the first row of half tile hf of tile t, and the last row of that half that exists; a half behind the slice's
-  // end takes the rows of the last one that is not
-  auto half_at = [&](int t, int hf, int &lim) -> int64_t {
-    int jb = j0 + t * TT + hf * 16;
-    jb = min(jb, (j1 - 1) & ~15);
-    lim = min(15, j1 - 1 - jb);
-    if (!a.cv.pm.table) return (int64_t)slot * a.cv.max_seq + jb;
-    // (constant memory: a scalar load that waits for no other load)
-    typedef const __attribute__((address_space(4))) int32_t *Table;
-    int pg = ((Table)a.cv.pm.table)[(int64_t)slot * a.cv.pm.pages_per_slot + (jb >> a.ps_shift)];
-    pg = (unsigned)pg >= (unsigned)a.cv.pm.num_pages ? 0 : pg;
-    return ((int64_t)pg << a.ps_shift) + (jb & ((1 << a.ps_shift) - 1));
-  };
+  while (true) {   // a sequence's share at a time
+  int slot, j0, j1, next_u = 0;
+  bool whole = true;
+  const int n = mx_rows(a.cv, b, slot);
+  if constexpr (SHARED) {
+    const int begin = __builtin_amdgcn_readfirstlane(prefix[b]), end = __builtin_amdgcn_readfirstlane(prefix[b + 1]);
+    next_u = min(u1, end);
+    j0 = (u0 - begin) * kTile;
+    j1 = min(n, (next_u - begin) * kTile);
+    whole = u0 == begin && next_u == end;
+  } else {
+    j0 = 0;
+    j1 = n;
+    if (n == 0) {
+      for (int i = tid; i < a.nq * CS; i += 256) {
+        const int g = i / CS, col = z * CS + i % CS - g / a.qpc * a.dl;
+        if (col >= 0 && col < a.dl) ((T *)a.l_out)[((int64_t)b * a.nq + g) * a.dl + col] = (T)0.f;
+      }
+      return;
+    }
+  }
+  const int64_t part = (int64_t)(2 * wg + (first_piece ? 0 : 1)) * a.nq;   // where a share that is not the whole sequence goes
+  const int nt = (j1 - j0 + kTile - 1) / kTile;
 
-  u32x4 kb[HF][KP];
-  unsigned ks[HF][KW];
-  CWord cb[HF][4][NCH];
-  unsigned cs[HF][4][NCH];
-  struct At { int64_t row[HF]; int lim[HF]; };
-  auto at_tile = [&](int t) { At r; 
+  // Where the rows of tile t are: the pool row of the first row of each half, and how many rows the half has.  Page numbers are
+  // asked for (constant memory, a scalar load that waits for no other) some time before they are used.
+  typedef const __attribute__((address_space(4))) int32_t *Table;
+  const bool paged = a.cv.pm.table != nullptr;   // contiguous slots: one page, of number 0, at the slot's first row
+  const Table pages = paged ? (Table)a.cv.pm.table + (int64_t)slot * a.cv.pm.pages_per_slot : (Table)a.cv.seq_lens;
+  const int64_t slot_row = paged ? 0 : (int64_t)slot * a.cv.max_seq;
+  const int in_page = paged ? (1 << a.ps_shift) - 1 : INT32_MAX, any_page = paged ? -1 : 0, num_pages = paged ? a.cv.pm.num_pages : 0;
+  struct Pages { int page[HF]; };
+  struct At { int64_t row[HF]; int rows[HF]; };
+  auto ask = [&](int t) {
+    Pages r;
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf) r.row[hf] = half_at(t, hf, r.lim[hf]);
-    return r; };
-  auto load_key_scales = [&](const At &at) {
+    for (int hf = 0; hf < HF; ++hf) r.page[hf] = pages[(min(j0 + t * kTile + hf * 16, j1 - 1) >> a.ps_shift) & any_page];
+    return r;
+  };
+  auto settle = [&](int t, const Pages &r) {
+    At at;
 #pragma unroll
     for (int hf = 0; hf < HF; ++hf) {
-      const uint8_t *base = a.cv.ks + at.row[hf] * (KB / 32);
+      const int jb = j0 + t * kTile + hf * 16, pg = (unsigned)r.page[hf] < (unsigned)num_pages ? r.page[hf] : 0;
+      // (the compiler does not see that these are the same in all lanes)
+      at.rows[hf] = __builtin_amdgcn_readfirstlane(min(max(j1 - jb, 0), 16));
+      const int64_t row = slot_row + ((int64_t)pg << a.ps_shift) + (jb & in_page);
+      at.row[hf] = (int64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)row) | (int64_t)__builtin_amdgcn_readfirstlane((int)(row >> 32)) << 32;
+    }
+    return at;
+  };
+
+  // Loads through buffers that end with the half's rows: what lies behind reads as zeros and costs nothing, in the last tile of
+  // a share and in the tiles that a wave asks for behind it.
+  u32x4 kb[KH][KP];
+  unsigned ks[KH][KW];
+  CWord cb[HF][4][NCH];
+  unsigned cs[HF][4][NCH];
+  const int col0 = z * CS + role * CW;
+  const unsigned koff = x * KB + h * 16, ksoff = x * (KB / 32);
+  unsigned coff[4], csoff[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    coff[j] = (4 * h + j) * a.cw + x * LC;
+    csoff[j] = (4 * h + j) * (a.cw / 32) + x * LC / 32;
+  }
+  auto buffer = [&](const uint8_t *pool, const At &at, int hf, int width, int skip) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)(pool + at.row[hf] * width + skip), 0, max(at.rows[hf] * width - skip, 0), 0x00020000);
+  };
+  constexpr int kNt = 2;   // streamed: not kept in the caches
+  auto my_half = [&](const At &at, int kh) {   // of the rows that this wave scores
+    if constexpr (WPT == 1) return at;
+    At r;
+    r.row[kh] = role ? at.row[1] : at.row[0];
+    r.rows[kh] = role ? at.rows[1] : at.rows[0];
+    return r;
+  };
+  auto load_key_scales = [&](const At &at) {
+#pragma unroll
+    for (int hf = 0; hf < KH; ++hf) {
+      const auto r = buffer(a.cv.ks, my_half(at, hf), hf, KB / 32, 0);
 #pragma unroll
       for (int i = 0; i < KW; ++i) {
-        const uint8_t *p = base + (unsigned)(min(x, at.lim[hf]) * (KB / 32) + i * 4);
-        if constexpr (KB >= 128) ks[hf][i] = __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(p));
-        else ks[hf][i] = __builtin_nontemporal_load(reinterpret_cast<const unsigned short *>(p));
+        if constexpr (KB >= 128) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(r, ksoff + i * 4, 0, kNt);
+        else ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b16(r, ksoff, 0, kNt);
       }
     }
   };
   auto load_keys = [&](const At &at, int p) {
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf) {
-      const uint8_t *base = a.cv.k + at.row[hf] * KB;
-      kb[hf][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(base + (unsigned)(min(x, at.lim[hf]) * KB + h * 16 + p * 64)));
-    }
+    for (int hf = 0; hf < KH; ++hf)
+      kb[hf][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer(a.cv.k, my_half(at, hf), hf, KB, 0), koff + p * 64, 0, kNt));
   };
   auto load_latents = [&](const At &at, int c) {
 #pragma unroll
     for (int hf = 0; hf < HF; ++hf) {
-      const uint8_t *base = a.cv.c + at.row[hf] * a.cw + z * CS;
-      const uint8_t *sb = a.cv.cs + at.row[hf] * (a.cw / 32) + z * (CS / 32);
+      const auto r = buffer(a.cv.c, at, hf, a.cw, col0), rs = buffer(a.cv.cs, at, hf, a.cw / 32, col0 / 32);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int r = min(4 * h + j, at.lim[hf]);
-        cb[hf][j][c] = __builtin_nontemporal_load(reinterpret_cast<const CWord *>(base + (unsigned)(r * a.cw + x * LC + c * 16 * LC)));
-        cs[hf][j][c] = __builtin_nontemporal_load(sb + (unsigned)(r * (a.cw / 32) + x * LC / 32 + c * 16 * LC / 32));
+        if constexpr (LC == 16) cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b128(r, coff[j] + c * 256, 0, kNt));
+        else cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b64(r, coff[j] + c * 128, 0, kNt));
+        cs[hf][j][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, csoff[j] + c * LC / 2, 0, kNt);
       }
     }
   };
 
-  // the first tile's rows are on their way while the queries are laid out
+  // the queries are asked for first, then the first tile's rows: these are on their way while the queries are laid out
+  const int ppk = a.dh / 64;   // pieces of a key head
+  const int kg = x < a.nq ? x / a.qpk : -1;
+  typedef __attribute__((ext_vector_type(8))) T Eight;
+  constexpr int QF = QREG ? KP * 2 : KP / 2;   // fragments this wave lays out: all of them, or every fourth
+  Eight qv[QF];
+#pragma unroll
+  for (int i = 0; i < QF; ++i) {   // second operand for half a piece: dimensions h * 16 + (f & 1) * 8 .. of the piece
+    const int f = QREG ? i : wave + 4 * i, p = f >> 1;
+    qv[i] = *reinterpret_cast<const Eight *>((const T *)a.q + ((int64_t)b * a.nq + (kg == p / ppk ? x : 0)) * a.dh + (p % ppk) * 64 + h * 16 + (f & 1) * 8);
+  }
   At nxt{};
   auto start = [&]() {
-    const At first = at_tile(wave);
+    const Pages now = ask(stream), later = ask(stream + NS);
+    const At first = settle(stream, now);
     load_key_scales(first);
 #pragma unroll
     for (int p = 0; p < KP; ++p) load_keys(first, p);
 #pragma unroll
     for (int c = 0; c < NCH; ++c) load_latents(first, c);
-    nxt = at_tile(min(wave + 4, nt - 1));
+    nxt = settle(stream + NS, later);
   };
-  if (wave < nt) start();
-  const int ppk = a.dh / 64;   // pieces of a key head
-  const int kg = x < a.nq ? x / a.qpk : -1;
-  auto query_fragment = [&](int f, bf16x8 (&out)[NQP]) {   // second operand for half a piece: dimensions h * 16 + (f & 1) * 8 ..
-    const int p = f >> 1;
-    const bool mine = kg == p / ppk;
-    typedef __attribute__((ext_vector_type(8))) T Eight;
-    const Eight src = *reinterpret_cast<const Eight *>((const T *)a.q + ((int64_t)b * a.nq + (mine ? x : 0)) * a.dh + (p % ppk) * 64 + h * 16 + (f & 1) * 8);
+  __builtin_amdgcn_sched_barrier(0);
+  start();
+  __builtin_amdgcn_sched_barrier(0);
+  bf16x8 qr[QREG ? KP * 2 : 1][NQP];
+  bf16x8 *qs = reinterpret_cast<bf16x8 *>(lds);   // [KP * 2][NQP][64]
+#pragma unroll
+  for (int i = 0; i < QF; ++i) {
+    const int f = QREG ? i : wave + 4 * i;
+    bf16x8 out[NQP];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 v[NQP];
-      split_parts<NQP>(mine ? to_f(src[e]) : 0.f, v);
+      split_parts<NQP>(kg == (f >> 1) / ppk ? to_f(qv[i][e]) : 0.f, v);
 #pragma unroll
-      for (int i = 0; i < NQP; ++i) out[i][e] = v[i];
+      for (int j = 0; j < NQP; ++j) out[j][e] = v[j];
     }
-  };
-  bf16x8 qr[QREG ? KP * 2 : 1][NQP];
-  bf16x8 *qs = reinterpret_cast<bf16x8 *>(lds);   // [KP * 2][NQP][64]
-  if constexpr (QREG) {
 #pragma unroll
-    for (int f = 0; f < KP * 2; ++f) query_fragment(f, qr[f]);
-  } else {
-    for (int f = wave; f < KP * 2; f += 4) {
-      bf16x8 v[NQP];
-      query_fragment(f, v);
-#pragma unroll
-      for (int i = 0; i < NQP; ++i) qs[(f * NQP + i) * 64 + lane] = v[i];
+    for (int j = 0; j < NQP; ++j) {
+      if constexpr (QREG) qr[i][j] = out[j];
+      else qs[(f * NQP + j) * 64 + lane] = out[j];
     }
-    __syncthreads();
   }
+  if constexpr (!QREG) __syncthreads();
 
   f32x4 acc[NCH][LC];
   float m = -INFINITY, l = 0.f, seen = -INFINITY;   // what weights refer to, their sum, the largest score of this lane's rows
 
-  auto tile = [&](int t, auto more) {
-    constexpr bool MORE = decltype(more)::value;
-    // ---- scores
-    f32x4 sc[HF];
+  auto tile = [&](int t, int turn) {
+    // ---- scores; a piece's query fragments are asked for a piece ahead, its sums are taken a piece later
+    f32x4 sc[HF], before[KH];
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf) sc[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
-    unsigned kscale[HF][KW];
+    for (int hf = 0; hf < KH; ++hf) sc[hf] = before[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+    unsigned kscale[KH][KW];
 #pragma unroll
-    for (int hf = 0; hf < HF; ++hf)
+    for (int hf = 0; hf < KH; ++hf)
 #pragma unroll
       for (int i = 0; i < KW; ++i) kscale[hf][i] = ks[hf][i] >> (8 * (h >> 1));
-    if constexpr (MORE) load_key_scales(nxt);
+    load_key_scales(nxt);
+    auto fragments = [&](int p, bf16x8 (&out)[2][NQP]) {
 #pragma unroll
-    for (int p = 0; p < KP; ++p) {
-      f32x4 d[HF];
-#pragma unroll
-      for (int hf = 0; hf < HF; ++hf) d[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        bf16x8 qf[NQP];
+      for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int i = 0; i < NQP; ++i) {
-          if constexpr (QREG) qf[i] = qr[p * 2 + half][i];
-          else qf[i] = qs[((p * 2 + half) * NQP + i) * 64 + lane];
+          if constexpr (QREG) out[half][i] = qr[p * 2 + half][i];
+          else out[half][i] = qs[((p * 2 + half) * NQP + i) * 64 + lane];
         }
-#pragma unroll
-        for (int hf = 0; hf < HF; ++hf) {
-          const unsigned w = kscale[hf][p / 2];
-          const float sl = __uint_as_float((p & 1 ? w << 7 : w << 23) & 0x7f800000u);
-          const u32x4 k4 = {cvt_lo(kb[hf][p][2 * half], sl), cvt_hi(kb[hf][p][2 * half], sl), cvt_lo(kb[hf][p][2 * half + 1], sl),
-                            cvt_hi(kb[hf][p][2 * half + 1], sl)};
-#pragma unroll
-          for (int i = 0; i < NQP; ++i)
-            d[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k4), qf[i], d[hf], 0, 0, 0);
-        }
-      }
-      if constexpr (MORE) load_keys(nxt, p);
+    };
+    auto take = [&](int p) {
       const bool mine = kg == p / ppk;
 #pragma unroll
-      for (int hf = 0; hf < HF; ++hf)
+      for (int hf = 0; hf < KH; ++hf)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[hf][i] += mine ? d[hf][i] : 0.f;
+        for (int i = 0; i < 4; ++i) sc[hf][i] += mine ? before[hf][i] : 0.f;
+    };
+    bf16x8 qf[2][NQP], qn[2][NQP];
+    fragments(0, qf);
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      if (p + 1 < KP) fragments(p + 1, qn);
+      f32x4 d[KH];
+#pragma unroll
+      for (int hf = 0; hf < KH; ++hf) d[hf] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int hf = 0; hf < KH; ++hf) {
+          const unsigned w = kscale[hf][p / 2];
+          const float s = __uint_as_float((p & 1 ? w << 7 : w << 23) & 0x7f800000u);
+          const u32x4 k4 = {cvt_lo(kb[hf][p][2 * half], s), cvt_hi(kb[hf][p][2 * half], s), cvt_lo(kb[hf][p][2 * half + 1], s),
+                            cvt_hi(kb[hf][p][2 * half + 1], s)};
+#pragma unroll
+          for (int i = 0; i < NQP; ++i)
+            d[hf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k4), qf[half][i], d[hf], 0, 0, 0);
+        }
+      load_keys(nxt, p);
+      if (p) take(p - 1);
+#pragma unroll
+      for (int hf = 0; hf < KH; ++hf) before[hf] = d[hf];
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int i = 0; i < NQP; ++i) qf[half][i] = qn[half][i];
       __builtin_amdgcn_sched_barrier(0);   // one piece at a time: conversions taken up early would need registers
     }
+    take(KP - 1);
+    if constexpr (WPT > 1) {
+      handed[turn][stream][role][lane] = sc[0];
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_barrier();   // (two sets of places: the one written here is read no later than in front of the next)
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      sc[0] = handed[turn][stream][0][lane];
+      sc[1] = handed[turn][stream][1][lane];
+    }
     // ---- weights
-    const int left = j1 - (j0 + t * TT);   // rows of this tile
+    const int left = j1 - (j0 + t * kTile);   // rows of this tile
     float mx = -INFINITY;
 #pragma unroll
     for (int hf = 0; hf < HF; ++hf)
@@ -363,7 +493,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
         mx = fmaxf(mx, sc[hf][i]);
       }
     seen = fmaxf(seen, mx);
-    if (t == wave && m == -INFINITY) {
+    if (t == stream && m == -INFINITY) {
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       m = fmaxf(mx, __shfl_xor(mx, 32));
     }
@@ -384,6 +514,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
         }
       }
     // ---- sums
+    const Pages then = ask(t + 2 * NS);   // (no LDS is read from here on, whose waits would be waits for these loads)
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
 #pragma unroll
@@ -406,18 +537,15 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 #pragma unroll
           for (int i = 0; i < NPP; ++i) {
             f32x4 &d = acc[c][w * 4 + e];
-            if constexpr (HF == 2)
-              d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{op[e][0], op[e][1], op[e][2], op[e][3]}),
-                                                          __builtin_bit_cast(bf16x8, u32x4{pp[i][0], pp[i][1], pp[i][2], pp[i][3]}), d, 0, 0, 0);
-            else
-              d = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4, u32x2{op[e][0], op[e][1]}),
-                                                            __builtin_bit_cast(s16x4, u32x2{pp[i][0], pp[i][1]}), d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{op[e][0], op[e][1], op[e][2], op[e][3]}),
+                                                        __builtin_bit_cast(bf16x8, u32x4{pp[i][0], pp[i][1], pp[i][2], pp[i][3]}), d, 0, 0, 0);
           }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (MORE) load_latents(nxt, c);
+      load_latents(nxt, c);
       __builtin_amdgcn_sched_barrier(0);
     }
+    nxt = settle(t + 2 * NS, then);
   };
 
   while (true) {
@@ -426,105 +554,169 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 #pragma unroll
       for (int j = 0; j < LC; ++j) acc[c][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     l = 0.f;
-    int t = wave;
-    for (; t + 4 < nt; t += 4) {
-      const At after = at_tile(min(t + 8, nt - 1));
-      tile(t, std::true_type{});
-      nxt = after;
+    if constexpr (WPT == 1) {
+      for (int t = stream; t < nt; t += NS) tile(t, 0);
+    } else {   // all waves go through as many tiles: they meet in each
+      for (int t = stream; t - stream < nt; t += NS) tile(t, ((t - stream) / NS) & 1);
     }
-    if (t < nt) tile(t, std::false_type{});
     seen = fmaxf(seen, __shfl_xor(seen, 16));
     seen = fmaxf(seen, __shfl_xor(seen, 32));
-    if (!__any(seen > m + kMostAbove)) break;   // (always the second time)
+    bool again = __any(seen > m + kMostAbove);   // (never the second time)
+    if constexpr (WPT > 1) again = __syncthreads_or(again);
+    if (!again) break;
     m = fmaxf(m, seen);
     start();
   }
 
-  // ---- the four waves' sums, chunk by chunk through LDS
+  // ---- the four waves' sums, through LDS
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  __syncthreads();   // queries are not read any more
-  float *sm = reinterpret_cast<float *>(lds), *sl = sm + 64, *buf = sm + 128;   // [4][16], [4][16], [4][n_q][16 * LC]
-  if (lane < 16) { sm[wave * 16 + x] = m; sl[wave * 16 + x] = l; }
-  __syncthreads();
-  float top = fmaxf(fmaxf(sm[x], sm[16 + x]), fmaxf(sm[32 + x], sm[48 + x]));
-  const float f = __builtin_amdgcn_exp2f(fmaxf(m, kLowest) - fmaxf(top, kLowest));
-  auto joined = [&](int g, float &mg) {   // sum of the weights of map g
-    mg = fmaxf(fmaxf(sm[g], sm[16 + g]), fmaxf(sm[32 + g], sm[48 + g]));
-    float v = 0.f;
+  if (lane < 16 && role == 0) { sm[stream][x] = m; sl[stream][x] = l; }
+  __syncthreads();   // (queries are not read any more, either)
+  float *buf = reinterpret_cast<float *>(lds);   // [NS][n_q][CS]
+  auto highest = [&](int g) {
+    float v = sm[0][g];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) v += sl[w * 16 + g] * __builtin_amdgcn_exp2f(fmaxf(sm[w * 16 + g], kLowest) - fmaxf(mg, kLowest));
+    for (int w = 1; w < NS; ++w) v = fmaxf(v, sm[w][g]);
     return v;
   };
-  if (!a.l_out && z == 0 && tid < a.nq) {
+  const float top = highest(x);
+  const float f = __builtin_amdgcn_exp2f(fmaxf(m, kLowest) - fmaxf(top, kLowest));
+  auto joined = [&](int g, float &mg) {   // sum of the weights of map g
+    mg = highest(g);
+    float v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NS; ++w) v += sl[w][g] * __builtin_amdgcn_exp2f(fmaxf(sm[w][g], kLowest) - fmaxf(mg, kLowest));
+    return v;
+  };
+  if (!whole && z == 0 && tid < a.nq) {
     float mg;
     const float lg = joined(tid, mg);
     a.pml[(part + tid) * 2] = mg;
     a.pml[(part + tid) * 2 + 1] = lg;
   }
-  constexpr int CW = 16 * LC;
+  auto park = [&](int c, float *dst) {   // this wave's sums of a chunk
 #pragma unroll
-  for (int c = 0; c < NCH; ++c) {
-    if (c) __syncthreads();
-    if (x < a.nq) {
-      float *dst = buf + (wave * a.nq + x) * CW;
+    for (int j = 0; j < LC; j += 4) {
 #pragma unroll
-      for (int j = 0; j < LC; j += 4) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<f32x4 *>(dst + (4 * h + i) * LC + j) =
-              f32x4{acc[c][j][i] * f, acc[c][j + 1][i] * f, acc[c][j + 2][i] * f, acc[c][j + 3][i] * f};
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4 *>(dst + (4 * h + i) * LC + j) =
+            f32x4{acc[c][j][i] * f, acc[c][j + 1][i] * f, acc[c][j + 2][i] * f, acc[c][j + 3][i] * f};
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
-    for (int i = tid; i < a.nq * (CW / 4); i += 256) {
-      const int g = i / (CW / 4), cc = i % (CW / 4) * 4, col = z * CS + c * CW + cc;
-      if (col / a.dl != g / a.qpc) continue;
-      f32x4 v = *reinterpret_cast<const f32x4 *>(buf + g * CW + cc);
+  };
+  if (x < a.nq) {
 #pragma unroll
-      for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * a.nq + g) * CW + cc);
-      if (a.l_out) {
-        float mg;
-        const float inv = 1.f / joined(g, mg);
-        T *o = (T *)a.l_out + ((int64_t)b * a.nq + g) * a.dl + col % a.dl;
+    for (int c = 0; c < NCH; ++c) park(c, buf + (stream * a.nq + x) * CS + role * CW + c * 16 * LC);
+  }
+  __syncthreads();
+  for (int i = tid; i < a.nq * (CS / 4); i += 256) {
+    const int g = i / (CS / 4), cc = i % (CS / 4) * 4, col = z * CS + cc - g / a.qpc * a.dl;   // latent of the map's group
+    if (col < 0 || col >= a.dl) continue;
+    f32x4 v = *reinterpret_cast<const f32x4 *>(buf + g * CS + cc);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = (T)(v[e] * inv);
-      } else {
-        *reinterpret_cast<f32x4 *>(a.pacc + (part + g) * a.dl + col % a.dl) = v;
-      }
+    for (int w = 1; w < NS; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * a.nq + g) * CS + cc);
+    if (whole) {
+      float mg;
+      const float lg = joined(g, mg);
+      T *o = (T *)a.l_out + ((int64_t)b * a.nq + g) * a.dl + col;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = (T)(v[e] / lg);
+    } else {
+      *reinterpret_cast<f32x4 *>(a.pacc + (part + g) * a.dl + col) = v;
     }
+  }
+  if constexpr (!SHARED) return;
+  u0 = next_u;
+  if (u0 >= u1) return;
+  do ++b; while (__builtin_amdgcn_readfirstlane(prefix[b + 1]) <= u0);
+  first_piece = false;
+  __syncthreads();   // the next share's queries and sums take the same LDS
   }
 }
 
-// Joins the splits: a thread per latent of a map.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_join_kernel(MxView cv, const float *pacc, const float *pml, int splits, int nq, int dl, T *l_out) {
-  const int b = blockIdx.y, i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= nq * dl) return;
-  int slot;
-  const int n = mx_rows(cv, b, slot);
-  const int g = i / dl;
-  const int64_t base = (int64_t)b * splits * nq;
-  float m = -INFINITY, l = 0.f, acc = 0.f;
-  for (int s = 0; s < splits; ++s) m = fmaxf(m, pml[(base + s * nq + g) * 2]);
-  for (int s = 0; s < splits; ++s) {
-    const int64_t at = base + s * nq + g;
-    const float ls = pml[at * 2 + 1];
-    if (ls == 0.f) continue;                        // a split without rows
-    const float ms = pml[at * 2];
-    const float w = ms == m ? 1.f : exp2f(ms - m);   // (-inf) - (-inf): scores of nothing but NaN
-    l = fmaf(ls, w, l);
-    acc = fmaf(pacc[at * dl + i % dl], w, acc);
+// Joins the pieces of a map: a workgroup per (map, sequence, 256 latents), four latents per thread and the pieces dealt to as
+// many groups of threads as there are.  SHARED: the pieces that mx_attn_kernel left (it has written sequences of one piece itself); otherwise
+// a.splits of them for every sequence.
+constexpr int kMaxPieces = 2048;
+
+template <typename T, bool SHARED>
+__global__ __launch_bounds__(256) void mx_join_kernel(MxAttnArgs a, int share) {
+  __shared__ float wt[kMaxPieces];
+  __shared__ float red[4], red2[4];
+  __shared__ f32x4 sums[256];
+  const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  T *out = (T *)a.l_out + ((int64_t)b * a.nq + g) * a.dl;
+  int64_t first, base;
+  int pieces, step;
+  bool none;
+  if constexpr (SHARED) {
+    const int p0 = a.prefix[b], p1 = a.prefix[b + 1], tiles = a.prefix[a.batch];
+    none = p0 == p1;
+    if (!none) {
+      share = share_count(tiles, share);
+      const int w0 = share_of(tiles, p0, share), w1 = share_of(tiles, p1 - 1, share);
+      if (w0 == w1) return;
+      pieces = w1 - w0 + 1;
+      base = 2 * w0;
+      first = base + (share_begin(tiles, w0, share) == p0 ? 0 : 1);
+      step = 2;
+    }
+  } else {
+    int slot;
+    none = mx_rows(a.cv, b, slot) == 0;
+    pieces = a.splits;
+    first = base = (int64_t)b * a.splits;
+    step = 1;
   }
-  l_out[(int64_t)b * nq * dl + i] = (T)(n == 0 ? 0.f : acc / l);   // scores of nothing but -inf: 0 / 0
+  if (none) {
+    const int i = blockIdx.z * 256 + tid;
+    if (i < a.dl) out[i] = (T)0.f;
+    return;
+  }
+  auto at = [&](int i) { return ((i == 0 ? first : base + (int64_t)i * step)) * a.nq + g; };
+  float m = -INFINITY;
+  for (int i = tid; i < pieces; i += 256) {
+    const float v = a.pml[at(i) * 2];
+    wt[i] = v;
+    m = fmaxf(m, v);
+  }
+#pragma unroll
+  for (int i = 32; i; i >>= 1) m = fmaxf(m, __shfl_xor(m, i));
+  if ((tid & 63) == 0) red[tid >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), kLowest);
+  float l = 0.f;
+  for (int i = tid; i < pieces; i += 256) {
+    const float w = __builtin_amdgcn_exp2f(fmaxf(wt[i], kLowest) - m);
+    wt[i] = w;
+    l = fmaf(a.pml[at(i) * 2 + 1], w, l);
+  }
+#pragma unroll
+  for (int i = 32; i; i >>= 1) l += __shfl_xor(l, i);
+  if ((tid & 63) == 0) red2[tid >> 6] = l;
+  __syncthreads();
+  l = (red2[0] + red2[1]) + (red2[2] + red2[3]);
+  // 64 threads for 256 latents (fewer where there are fewer), the pieces dealt to the others
+  const int c0 = blockIdx.z * 256, lanes = min(a.dl - c0, 256) / 4, groups = 256 / lanes, my = tid % lanes, grp = tid / lanes;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+  if (grp < groups) {
+#pragma unroll 8
+    for (int i = grp; i < pieces; i += groups) v += *reinterpret_cast<const f32x4 *>(a.pacc + at(i) * a.dl + c0 + my * 4) * wt[i];
+  }
+  sums[tid] = v;
+  __syncthreads();
+  if (grp) return;
+  for (int r = 1; r < groups; ++r) v += sums[r * lanes + my];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[c0 + my * 4 + e] = (T)(v[e] / l);   // scores of nothing but -inf: 0 / 0
 }
 
 }  // namespace
 
 bool mx_decode_dims_ok(const Dims &d) { return mx_widths_ok(d) && d.dh <= kAnyMaxHead && d.dl <= kAnyMaxLatent && d.nq <= 65535; }
 
-// Widths of a latent slice: one workgroup's columns of a latent row.
+// Latent columns of a workgroup: the whole row where it has an instantiation, else slices of it.
 static int mx_slice_width(const Dims &d) {
   for (int cs = 1024; cs >= 128; cs /= 2)
     if (d.wc_w % cs == 0 && (d.wc_w == cs || cs >= 512)) return cs;
@@ -542,62 +734,98 @@ static bool mx_layout_tuned(const MxView &cv) {
   return !cv.pm.table || (cv.pm.page_size >= 16 && (cv.pm.page_size & (cv.pm.page_size - 1)) == 0);
 }
 
-int mx_decode_splits(const Dims &d, int batch, int max_seq) {
-  if (mx_decode_tuned(d)) {
-    const int z = d.wc_w / mx_slice_width(d);
-    const int target = d.wk_w + mx_slice_width(d) >= 1024 ? 256 : d.wk_w + mx_slice_width(d) >= 512 ? 512 : 1024;
-    const int want = target / (batch * z), cap = max_seq / 128;
-    return std::max(1, std::min(std::min(want, cap), 256));
-  }
+// Workgroups per CU, by the registers that a slice's sums, a tile's codes and the rest take.
+static int mx_occupancy(int cs) { return cs >= 512 ? 1 : cs >= 256 ? 2 : 3; }
+
+// Pieces that sums are kept of.  Matrix-instruction kernel: two per workgroup, and one round of workgroups (requested: that many
+// per sequence).  General kernel: one per sequence and split.
+static int mx_shares(const Dims &d, int batch, int requested) {
+  if (requested > 0) return (int)std::min<int64_t>((int64_t)batch * requested, kMaxPieces);
+  const int cs = mx_slice_width(d);
+  return std::max(1, 256 * mx_occupancy(cs) / (d.wc_w / cs));
+}
+
+static int mx_equal_splits(const Dims &d, int batch, int max_seq, int requested) {
+  if (requested > 0) return std::min(requested, 1024);
   const int want = (1024 + batch * d.nq - 1) / (batch * d.nq), cap = max_seq / 256;
   return std::max(1, std::min(std::min(want, cap), 256));
 }
 
+static size_t piece_bytes(const Dims &d) { return (size_t)d.nq * ((size_t)d.dl + 2) * 4; }
+static size_t prefix_bytes(int batch) { return batch <= kShareBatch ? align_up(((size_t)batch + 1) * 4) : 0; }
+
+size_t mx_decode_bytes(const Dims &d, int batch, int max_seq, int requested) {
+  // the call picks the kernel by the page size too: enough for either
+  size_t n = piece_bytes(d) * batch * mx_equal_splits(d, batch, max_seq, requested);
+  if (mx_decode_tuned(d) && batch <= kShareBatch) n = std::max(n, prefix_bytes(batch) + 2 * piece_bytes(d) * mx_shares(d, batch, requested));
+  return n;
+}
+
 template <typename T, int KB, int CS>
-static void launch_tuned(const MxAttnArgs &a, int z, int batch, hipStream_t st) {
-  constexpr int TT = KB + CS > 512 ? 16 : 32;
-  constexpr int OCC = CS >= 1024 ? 1 : KB + CS >= 512 ? 2 : KB + CS > 192 ? 3 : 4;
-  constexpr int LC = CS >= 256 ? 16 : CS / 16;
-  const int lds = std::max(KB * Parts<T>::Q * 32, 512 + 4 * a.nq * 16 * LC * 4);
-  if (lds > 65536) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, TT, OCC>, lds);
-  mx_attn_kernel<T, KB, CS, TT, OCC><<<dim3(a.splits, z, batch), 256, lds, st>>>(a);
+static void launch_tuned(const MxAttnArgs &a, int share, int z, hipStream_t st) {
+  constexpr int WPT = CS > 512 ? 2 : 1;
+  constexpr int OCC = CS >= 512 ? 1 : CS >= 256 ? 2 : 3;
+  const int lds = std::max(KB * Parts<T>::Q * 32, 4 / WPT * a.nq * CS * 4);   // the queries, then the waves' sums
+  if (share) {
+    if (lds > 56 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true>, lds);
+    mx_attn_kernel<T, KB, CS, WPT, OCC, true><<<dim3(share, z), 256, lds, st>>>(a);
+    mx_join_kernel<T, true><<<dim3(a.nq, a.batch, (a.dl + 255) / 256), 256, 0, st>>>(a, share);
+  } else {
+    if (lds > 56 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, false>, lds);
+    mx_attn_kernel<T, KB, CS, WPT, OCC, false><<<dim3(a.batch, z), 256, lds, st>>>(a);
+  }
 }
 
 template <typename T>
-static void launch_decode(const Dims &d, MxAttnArgs a, int batch, hipStream_t st) {
-  const int splits = a.splits;
-  T *out = (T *)a.l_out;
-  if (mx_decode_tuned(d) && mx_layout_tuned(a.cv)) {
-    const int cs = mx_slice_width(d), z = d.wc_w / cs;
-    if (splits > 1) a.l_out = nullptr;
-    switch (d.wk_w * 4096 + cs) {
-      case 64 * 4096 + 128: launch_tuned<T, 64, 128>(a, z, batch, st); break;
-      case 64 * 4096 + 256: launch_tuned<T, 64, 256>(a, z, batch, st); break;
-      case 64 * 4096 + 512: launch_tuned<T, 64, 512>(a, z, batch, st); break;
-      case 128 * 4096 + 128: launch_tuned<T, 128, 128>(a, z, batch, st); break;
-      case 128 * 4096 + 256: launch_tuned<T, 128, 256>(a, z, batch, st); break;
-      case 128 * 4096 + 512: launch_tuned<T, 128, 512>(a, z, batch, st); break;
-      case 256 * 4096 + 256: launch_tuned<T, 256, 256>(a, z, batch, st); break;
-      case 256 * 4096 + 512: launch_tuned<T, 256, 512>(a, z, batch, st); break;
-      case 256 * 4096 + 1024: launch_tuned<T, 256, 1024>(a, z, batch, st); break;
-      case 512 * 4096 + 512: launch_tuned<T, 512, 512>(a, z, batch, st); break;
-      case 512 * 4096 + 1024: launch_tuned<T, 512, 1024>(a, z, batch, st); break;
-      case 1024 * 4096 + 1024: launch_tuned<T, 1024, 1024>(a, z, batch, st); break;
-    }
-    if (splits == 1) return;
-  } else {
-    mx_attn_any_kernel<T><<<dim3(splits, d.nq, batch), 256, 0, st>>>(a);
+static void launch_decode(const Dims &d, const MxAttnArgs &a, int share, hipStream_t st) {
+  if (a.splits) {
+    mx_attn_any_kernel<T><<<dim3(a.splits, d.nq, a.batch), 256, 0, st>>>(a);
+    mx_join_kernel<T, false><<<dim3(d.nq, a.batch, (d.dl + 255) / 256), 256, 0, st>>>(a, 0);
+    return;
   }
-  mx_join_kernel<T><<<dim3((d.nq * d.dl + 255) / 256, batch), 256, 0, st>>>(a.cv, a.pacc, a.pml, splits, d.nq, d.dl, out);
+  const int cs = mx_slice_width(d), z = d.wc_w / cs;
+  switch (d.wk_w * 4096 + cs) {
+    case 64 * 4096 + 128: return launch_tuned<T, 64, 128>(a, share, z, st);
+    case 64 * 4096 + 256: return launch_tuned<T, 64, 256>(a, share, z, st);
+    case 64 * 4096 + 512: return launch_tuned<T, 64, 512>(a, share, z, st);
+    case 128 * 4096 + 128: return launch_tuned<T, 128, 128>(a, share, z, st);
+    case 128 * 4096 + 256: return launch_tuned<T, 128, 256>(a, share, z, st);
+    case 128 * 4096 + 512: return launch_tuned<T, 128, 512>(a, share, z, st);
+    case 256 * 4096 + 256: return launch_tuned<T, 256, 256>(a, share, z, st);
+    case 256 * 4096 + 512: return launch_tuned<T, 256, 512>(a, share, z, st);
+    case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024>(a, share, z, st);
+    case 512 * 4096 + 512: return launch_tuned<T, 512, 512>(a, share, z, st);
+    case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024>(a, share, z, st);
+    case 1024 * 4096 + 1024: return launch_tuned<T, 1024, 1024>(a, share, z, st);
+  }
 }
 
-int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int splits, float *part, void *l_out, hipStream_t st) {
-  int shift = 0;
+int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int requested, void *ws, size_t ws_bytes, void *l_out,
+                     hipStream_t st) {
+  int shift = 0, share = 0, splits = 0;
+  int64_t pieces;
+  size_t head = 0;
+  if (mx_decode_tuned(d) && mx_layout_tuned(cv)) {
+    head = prefix_bytes(batch);
+    pieces = batch <= kShareBatch ? 2 * (int64_t)mx_shares(d, batch, requested) : 0;
+  } else {
+    splits = mx_equal_splits(d, batch, cv.max_seq, requested);
+    pieces = (int64_t)batch * splits;
+  }
+  if (pieces) {   // a smaller workspace: as many pieces as it holds
+    const int64_t least = splits ? batch : 2, fit = ws_bytes > head ? (int64_t)((ws_bytes - head) / piece_bytes(d)) : 0;
+    if (fit < pieces && (requested > 0 || fit < least)) return GTA_ERR_WORKSPACE;
+    pieces = std::min(pieces, fit);
+    if (splits) splits = (int)(pieces / batch);
+    else share = (int)(pieces / 2);
+    pieces = splits ? (int64_t)splits * batch : 2 * (int64_t)share;
+  }
   if (cv.pm.table) while ((1 << shift) < cv.pm.page_size && shift < 30) ++shift;
-  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, splits, shift, d.scale * 1.4426950408889634f,
-                     part, part + (int64_t)batch * splits * d.nq * d.dl, l_out};
-  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, batch, st);
-  else launch_decode<float>(d, a, batch, st);
+  float *acc = (float *)((char *)ws + head);
+  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, batch, splits, shift, d.scale * 1.4426950408889634f,
+                     acc, acc + pieces * d.nq * d.dl, (int32_t *)ws, l_out};
+  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, share, st);
+  else launch_decode<float>(d, a, share, st);
   return check_launch();
 }
 
