@@ -21,10 +21,10 @@ typedef __attribute__((ext_vector_type(4))) short s16x4;
 struct MxAttnArgs {
   const void *q;
   MxView cv;
-  int nq, qpk, qpc, dh, dl, kw, cw, batch, splits, ps_shift;
+  int nq, qpk, qpc, dh, dl, kw, cw, batch, splits, share, ps_shift;
   float scale_log2e;
   float *pacc, *pml;   // [pieces, n_q, d_l], [pieces, n_q, 2]
-  int32_t *prefix;     // [batch + 1] row tiles in front of each sequence, where the tiles of a batch are shared out evenly
+  int32_t *prefix;     // [batch + 1] pieces in front of each sequence (matrix-instruction kernel)
   void *l_out;
 };
 
@@ -178,48 +178,130 @@ template <> struct Word<16> { typedef u32x4 type; };
 constexpr float kLowest = -3e38f;   // stands for "no score yet" where a difference is taken
 constexpr float kMostAbove = 40.f;
 
-// Sequences that the batch's tiles are shared out over; a larger batch has a workgroup per sequence.
-constexpr int kShareBatch = 1024;
-constexpr int kTile = 32;
+constexpr int kTile = 32;           // rows of a tile
+constexpr int kShareBatch = 1024;   // a larger batch has a workgroup per sequence
 
-// Tiles of rows in front of each sequence (LDS, batch + 1 entries); returns their number.
-__device__ __forceinline__ int scan_tiles(const MxView &cv, int batch, int tt, int *prefix, int *wsum) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  int before = 0;
-#pragma unroll 1
-  for (int b0 = 0; b0 < batch; b0 += 256) {
-    const int b = b0 + tid;
-    int slot;
-    const int mine = b < batch ? (mx_rows(cv, b, slot) + tt - 1) / tt : 0;
-    int run = mine;
+// inclusive sums over the lanes of a wave
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
+
+// How a batch is cut into pieces, one per workgroup.  A round is what a workgroup's waves take at a time; a sequence of r rounds
+// becomes ceil(r / T) pieces of about as many rounds.  T is the least of eight values, between the rounds that each of `share`
+// workgroups has if nothing is lost and those with which every batch fits, with which there are no more pieces than workgroups:
+// all run at once, and the longest ends no later than it must.  Batches of many sequences are cut finer than the chip needs at
+// once, and the pieces dealt out as workgroups end.  (Workgroups that go on into the next sequence instead have to set out twice,
+// 5 to 10 us: 64 x 8192 rows of 1024 bytes 104 us against 93.)
+constexpr int kCutTries = 8;
+struct Cut {
+  int prefix[kShareBatch + 1], rows[kShareBatch];   // pieces in front of each sequence, its rows
+  int sums[4][kCutTries], found;
+};
+
+__device__ __forceinline__ int rounds_of(int n, int per_round) { return (n + per_round - 1) / per_round; }
+
+// Returns the number of pieces.  splits > 0: that many of each sequence that has the rounds.
+__device__ __forceinline__ int cut_batch(const MxView &cv, int batch, int per_round, int splits, int share, Cut &cut) {
+  constexpr int PER = kShareBatch / 256, NT = kCutTries;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int r[PER], total = 0, some = 0;
 #pragma unroll
-    for (int i = 1; i < 64; i <<= 1) {
-      const int v = __shfl_up(run, i);
-      if (lane >= i) run += v;
+  for (int i = 0; i < PER; ++i) {
+    r[i] = 0;
+    const int b = tid + 256 * i;
+    if (256 * i < batch && b < batch) {
+      int slot;
+      const int n = mx_rows(cv, b, slot);
+      cut.rows[b] = n;
+      r[i] = rounds_of(n, per_round);
+      total += r[i];
+      some += n > 0;
     }
-    if (b0) __syncthreads();
-    if (lane == 63) wsum[tid >> 6] = run;
-    __syncthreads();
-    const int w0 = wsum[0], w1 = wsum[1], w2 = wsum[2];
-    run += before + (tid >= 64 ? w0 : 0) + (tid >= 128 ? w1 : 0) + (tid >= 192 ? w2 : 0);
-    if (b < batch) prefix[b + 1] = run;
-    before += w0 + w1 + w2 + wsum[3];
   }
-  if (tid == 0) prefix[0] = 0;
+  int t = 1;
+  if (!splits) {
+    total = wave_scan(total);
+    some = wave_scan(some);
+    if (lane == 63) { cut.sums[wave][0] = total; cut.sums[wave][1] = some; }
+    __syncthreads();
+    total = cut.sums[0][0] + cut.sums[1][0] + cut.sums[2][0] + cut.sums[3][0];
+    some = cut.sums[0][1] + cut.sums[1][1] + cut.sums[2][1] + cut.sums[3][1];
+    total = __builtin_amdgcn_readfirstlane(total);
+    some = __builtin_amdgcn_readfirstlane(some);
+    __syncthreads();
+    if (2 * some > share) {
+      t = max(1, (total + 2 * share - 1) / (2 * share));
+    } else {
+      const int lo = max(1, (total + share - 1) / share), hi = max(lo, (total + share - some - 1) / (share - some));
+      auto candidate = [&](int i) { return lo + (int)((int64_t)(hi - lo) * i / (NT - 1)); };
+#pragma unroll
+      for (int c = 0; c < NT; ++c) {
+        const int tc = candidate(c);
+        int k = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+          if (256 * i < batch) k += rounds_of(r[i], tc);
+        k = wave_scan(k);
+        if (lane == 63) cut.sums[wave][c] = k;
+      }
+      __syncthreads();
+      t = hi;
+#pragma unroll
+      for (int c = NT - 2; c >= 0; --c)
+        if (cut.sums[0][c] + cut.sums[1][c] + cut.sums[2][c] + cut.sums[3][c] <= share) t = candidate(c);
+      t = __builtin_amdgcn_readfirstlane(t);
+      __syncthreads();
+    }
+  }
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (256 * i >= batch) break;
+    const int b = tid + 256 * i, k = splits ? min(splits, r[i]) : rounds_of(r[i], t);
+    int run = wave_scan(k);
+    if (lane == 63) cut.sums[wave][i] = run;   // (a column of its own each time)
+    __syncthreads();
+    const int w0 = cut.sums[0][i], w1 = cut.sums[1][i], w2 = cut.sums[2][i];
+    run += before + (wave > 0 ? w0 : 0) + (wave > 1 ? w1 : 0) + (wave > 2 ? w2 : 0);
+    if (b < batch) cut.prefix[b + 1] = run;
+    before += w0 + w1 + w2 + cut.sums[3][i];
+  }
+  if (tid == 0) cut.prefix[0] = 0;
   __syncthreads();
-  return before;
+  return __builtin_amdgcn_readfirstlane(before);
 }
 
-// Workgroup w of `share` has tiles [share_begin(w), share_begin(w + 1)) of `tiles`, one more each for the first of them;
-// share_of is the workgroup that has tile u.  tiles >= share.
-__device__ __forceinline__ int share_begin(int tiles, int w, int share) { return w * (tiles / share) + min(w, tiles % share); }
-__device__ __forceinline__ int share_of(int tiles, int u, int share) {
-  const int q = tiles / share, r = tiles % share, more = r * (q + 1);
-  return u < more ? u / (q + 1) : r + (u - more) / q;
+// The same for up to 64 sequences, a lane each, by every wave for itself: no LDS and no barrier (2 us less at the start of a launch).
+// Lane b: pieces in front of and of sequence b, its rows.  Returns the number of pieces.
+__device__ __forceinline__ int cut_lanes(const MxView &cv, int batch, int per_round, int splits, int share, int &before, int &mine, int &rows) {
+  const int b = threadIdx.x & 63;
+  int slot;
+  rows = b < batch ? mx_rows(cv, b, slot) : 0;
+  const int r = rounds_of(rows, per_round);
+  int t = 1;
+  if (!splits) {
+    const int total = __builtin_amdgcn_readlane(wave_scan(r), 63), some = __popcll(__ballot(rows > 0));
+    if (2 * some > share) {
+      t = max(1, (total + 2 * share - 1) / (2 * share));
+    } else {
+      const int lo = max(1, (total + share - 1) / share), hi = max(lo, (total + share - some - 1) / (share - some));
+      t = lo;
+#pragma unroll 1
+      for (int c = 1; c < kCutTries && __builtin_amdgcn_readlane(wave_scan(rounds_of(r, t)), 63) > share; ++c)
+        t = lo + (int)((int64_t)(hi - lo) * c / (kCutTries - 1));
+    }
+  }
+  mine = splits ? min(splits, r) : rounds_of(r, t);
+  const int run = wave_scan(mine);
+  before = run - mine;
+  return __builtin_amdgcn_readlane(run, 63);
 }
-// Workgroups that get tiles: at least kLeastTiles each.
-constexpr int kLeastTiles = 4;
-__device__ __forceinline__ int share_count(int tiles, int share) { return max(1, min(share, tiles / kLeastTiles)); }
 
 // KB bytes of a key row, CS latent columns of a workgroup.  WPT waves take a tile of 32 rows together where the sums of all columns
 // would not fit one wave's registers: each has the scores of its half of the rows, hands them to the other through LDS, and the
@@ -233,7 +315,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int NS = 4 / WPT;                                            // tiles worked on at a time
   constexpr bool QREG = KB * NQP <= 192;
   typedef typename Word<LC>::type CWord;
-  __shared__ int prefix[SHARED ? kShareBatch + 1 : 1], wsum[4];
+  __shared__ std::conditional_t<SHARED, Cut, int> cut;
   __shared__ float sm[NS][16], sl[NS][16];
   __shared__ f32x4 handed[WPT > 1 ? 2 : 1][NS][2][WPT > 1 ? 64 : 1];
   extern __shared__ char lds[];
@@ -241,38 +323,44 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), stream = wave / WPT, role = wave % WPT;
   const int z = blockIdx.y;
 
-  // ---- this workgroup's tiles [u0, u1), b the sequence of the first
-  int u0 = 0, u1 = 0, b = blockIdx.x;
-  const int wg = blockIdx.x;
-  if constexpr (SHARED) {
-    const int tiles = __builtin_amdgcn_readfirstlane(scan_tiles(a.cv, a.batch, kTile, prefix, wsum));
-    if (wg == 0 && z == 0)
-      for (int i = tid; i <= a.batch; i += 256) a.prefix[i] = prefix[i];
-    const int share = share_count(tiles, gridDim.x);
-    if (wg >= share || tiles == 0) return;
-    u0 = share_begin(tiles, wg, share);
-    u1 = u0 + tiles / share + (wg < tiles % share);
-    int lo = 0, hi = a.batch;   // the last sequence that begins at or before u0 (empty ones in front of it are passed over)
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (prefix[mid] <= u0) lo = mid; else hi = mid;
-    }
-    b = __builtin_amdgcn_readfirstlane(lo);
-  }
-  bool first_piece = true;
-
-  while (true) {   // a sequence's share at a time
-  int slot, j0, j1, next_u = 0;
+  // ---- this workgroup's piece: rows [j0, j1) of sequence b
+  int b = blockIdx.x, slot, j0 = 0, j1, n;
   bool whole = true;
-  const int n = mx_rows(a.cv, b, slot);
   if constexpr (SHARED) {
-    const int begin = __builtin_amdgcn_readfirstlane(prefix[b]), end = __builtin_amdgcn_readfirstlane(prefix[b + 1]);
-    next_u = min(u1, end);
-    j0 = (u0 - begin) * kTile;
-    j1 = min(n, (next_u - begin) * kTile);
-    whole = u0 == begin && next_u == end;
+    const int wg = blockIdx.x;
+    int first, k;
+    if (a.batch <= 64) {
+      int before, mine, rows;
+      const int pieces = cut_lanes(a.cv, a.batch, kTile * NS, a.splits, a.share, before, mine, rows);
+      if (wg == 0 && z == 0 && wave == 0) {
+        if (lane < a.batch) a.prefix[lane + 1] = before + mine;
+        if (lane == 0) a.prefix[0] = 0;
+      }
+      if (wg >= pieces) return;
+      b = __builtin_amdgcn_readfirstlane(__ffsll(__ballot(before + mine > wg)) - 1);
+      first = __builtin_amdgcn_readlane(before, b);
+      k = __builtin_amdgcn_readlane(mine, b);
+      n = __builtin_amdgcn_readlane(rows, b);
+    } else {
+      const int pieces = cut_batch(a.cv, a.batch, kTile * NS, a.splits, a.share, cut);
+      if (wg == 0 && z == 0)
+        for (int i = tid; i <= a.batch; i += 256) a.prefix[i] = cut.prefix[i];
+      if (wg >= pieces) return;
+      for (int i = tid; i < a.batch; i += 256)
+        if (cut.prefix[i] <= wg && wg < cut.prefix[i + 1]) cut.found = i;
+      __syncthreads();
+      b = __builtin_amdgcn_readfirstlane(cut.found);
+      n = __builtin_amdgcn_readfirstlane(cut.rows[b]);
+      first = __builtin_amdgcn_readfirstlane(cut.prefix[b]);
+      k = __builtin_amdgcn_readfirstlane(cut.prefix[b + 1]) - first;
+    }
+    slot = a.cv.slots ? a.cv.slots[b] : b;
+    const int r = rounds_of(n, kTile * NS), q = r / k, more = r % k, i = wg - first;   // one round more for the first of them
+    j0 = (i * q + min(i, more)) * (kTile * NS);
+    j1 = min(n, j0 + (q + (i < more)) * (kTile * NS));
+    whole = k == 1;
   } else {
-    j0 = 0;
+    n = mx_rows(a.cv, b, slot);
     j1 = n;
     if (n == 0) {
       for (int i = tid; i < a.nq * CS; i += 256) {
@@ -282,7 +370,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       return;
     }
   }
-  const int64_t part = (int64_t)(2 * wg + (first_piece ? 0 : 1)) * a.nq;   // where a share that is not the whole sequence goes
+  const int64_t part = (int64_t)blockIdx.x * a.nq;   // where a piece that is not the whole sequence goes
   const int nt = (j1 - j0 + kTile - 1) / kTile;
 
   // Where the rows of tile t are: the pool row of the first row of each half, and how many rows the half has.  Page numbers are
@@ -573,7 +661,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   l += __shfl_xor(l, 32);
   if (lane < 16 && role == 0) { sm[stream][x] = m; sl[stream][x] = l; }
   __syncthreads();   // (queries are not read any more, either)
-  float *buf = reinterpret_cast<float *>(lds);   // [NS][n_q][CS]
+  float *buf = reinterpret_cast<float *>(lds);   // [NS][n_q][ROW]
   auto highest = [&](int g) {
     float v = sm[0][g];
 #pragma unroll
@@ -595,27 +683,30 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     a.pml[(part + tid) * 2] = mg;
     a.pml[(part + tid) * 2 + 1] = lg;
   }
-  auto park = [&](int c, float *dst) {   // this wave's sums of a chunk
-#pragma unroll
-    for (int j = 0; j < LC; j += 4) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4 *>(dst + (4 * h + i) * LC + j) =
-            f32x4{acc[c][j][i] * f, acc[c][j + 1][i] * f, acc[c][j + 2][i] * f, acc[c][j + 3][i] * f};
-      __builtin_amdgcn_sched_barrier(0);
-    }
-  };
+  // Rows of n_q maps, CS columns in words of 16 bytes; a word's place is turned by the lane group that wrote it and rows are
+  // padded, so that the lanes of a store meet different banks.
+  constexpr int ROW = CS + 16;
+  auto place = [](int col) { return col ^ (((col / (4 * LC)) & 3) * 4); };
   if (x < a.nq) {
+    float *dst = buf + (stream * a.nq + x) * ROW;
 #pragma unroll
-    for (int c = 0; c < NCH; ++c) park(c, buf + (stream * a.nq + x) * CS + role * CW + c * 16 * LC);
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int j = 0; j < LC; j += 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<f32x4 *>(dst + place(role * CW + c * 16 * LC + (4 * h + i) * LC + j)) =
+              f32x4{acc[c][j][i] * f, acc[c][j + 1][i] * f, acc[c][j + 2][i] * f, acc[c][j + 3][i] * f};
+        __builtin_amdgcn_sched_barrier(0);   // not all of them out of the accumulation registers at once
+      }
   }
   __syncthreads();
   for (int i = tid; i < a.nq * (CS / 4); i += 256) {
     const int g = i / (CS / 4), cc = i % (CS / 4) * 4, col = z * CS + cc - g / a.qpc * a.dl;   // latent of the map's group
     if (col < 0 || col >= a.dl) continue;
-    f32x4 v = *reinterpret_cast<const f32x4 *>(buf + g * CS + cc);
+    f32x4 v = *reinterpret_cast<const f32x4 *>(buf + g * ROW + place(cc));
 #pragma unroll
-    for (int w = 1; w < NS; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * a.nq + g) * CS + cc);
+    for (int w = 1; w < NS; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * a.nq + g) * ROW + place(cc));
     if (whole) {
       float mg;
       const float lg = joined(g, mg);
@@ -626,55 +717,39 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       *reinterpret_cast<f32x4 *>(a.pacc + (part + g) * a.dl + col) = v;
     }
   }
-  if constexpr (!SHARED) return;
-  u0 = next_u;
-  if (u0 >= u1) return;
-  do ++b; while (__builtin_amdgcn_readfirstlane(prefix[b + 1]) <= u0);
-  first_piece = false;
-  __syncthreads();   // the next share's queries and sums take the same LDS
-  }
 }
 
 // Joins the pieces of a map: a workgroup per (map, sequence, 256 latents), four latents per thread and the pieces dealt to as
 // many groups of threads as there are.  SHARED: the pieces that mx_attn_kernel left (it has written sequences of one piece itself); otherwise
 // a.splits of them for every sequence.
-constexpr int kMaxPieces = 2048;
+constexpr int kMaxPieces = 2560;   // of a sequence: at most twice the workgroups that the chip holds, and one, or 1024 splits
 
 template <typename T, bool SHARED>
-__global__ __launch_bounds__(256) void mx_join_kernel(MxAttnArgs a, int share) {
+__global__ __launch_bounds__(256) void mx_join_kernel(MxAttnArgs a) {
   __shared__ float wt[kMaxPieces];
   __shared__ float red[4], red2[4];
   __shared__ f32x4 sums[256];
   const int g = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
   T *out = (T *)a.l_out + ((int64_t)b * a.nq + g) * a.dl;
-  int64_t first, base;
-  int pieces, step;
+  int first, pieces;
   bool none;
   if constexpr (SHARED) {
-    const int p0 = a.prefix[b], p1 = a.prefix[b + 1], tiles = a.prefix[a.batch];
-    none = p0 == p1;
-    if (!none) {
-      share = share_count(tiles, share);
-      const int w0 = share_of(tiles, p0, share), w1 = share_of(tiles, p1 - 1, share);
-      if (w0 == w1) return;
-      pieces = w1 - w0 + 1;
-      base = 2 * w0;
-      first = base + (share_begin(tiles, w0, share) == p0 ? 0 : 1);
-      step = 2;
-    }
+    first = a.prefix[b];
+    pieces = a.prefix[b + 1] - first;
+    none = pieces == 0;
+    if (pieces == 1) return;
   } else {
     int slot;
     none = mx_rows(a.cv, b, slot) == 0;
     pieces = a.splits;
-    first = base = (int64_t)b * a.splits;
-    step = 1;
+    first = b * a.splits;
   }
   if (none) {
     const int i = blockIdx.z * 256 + tid;
     if (i < a.dl) out[i] = (T)0.f;
     return;
   }
-  auto at = [&](int i) { return ((i == 0 ? first : base + (int64_t)i * step)) * a.nq + g; };
+  auto at = [&](int i) { return ((int64_t)first + i) * a.nq + g; };
   float m = -INFINITY;
   for (int i = tid; i < pieces; i += 256) {
     const float v = a.pml[at(i) * 2];
@@ -735,14 +810,17 @@ static bool mx_layout_tuned(const MxView &cv) {
 }
 
 // Workgroups per CU, by the registers that a slice's sums, a tile's codes and the rest take.
-static int mx_occupancy(int cs) { return cs >= 512 ? 1 : cs >= 256 ? 2 : 3; }
+constexpr int mx_occupancy(int cs) { return cs >= 512 ? 1 : cs >= 256 ? 2 : 3; }
 
-// Pieces that sums are kept of.  Matrix-instruction kernel: two per workgroup, and one round of workgroups (requested: that many
-// per sequence).  General kernel: one per sequence and split.
-static int mx_shares(const Dims &d, int batch, int requested) {
-  if (requested > 0) return (int)std::min<int64_t>((int64_t)batch * requested, kMaxPieces);
+// Workgroups that the chip holds at once.
+static int mx_share(const Dims &d) {
   const int cs = mx_slice_width(d);
-  return std::max(1, 256 * mx_occupancy(cs) / (d.wc_w / cs));
+  return std::max(2, 256 * mx_occupancy(cs) / (d.wc_w / cs));
+}
+
+// Most pieces of a batch (Cut).
+static int64_t mx_most_pieces(int batch, int share, int requested) {
+  return requested > 0 ? (int64_t)batch * std::min(requested, 1024) : 2 * batch > share ? 2 * (int64_t)share + batch : share;
 }
 
 static int mx_equal_splits(const Dims &d, int batch, int max_seq, int requested) {
@@ -757,75 +835,82 @@ static size_t prefix_bytes(int batch) { return batch <= kShareBatch ? align_up((
 size_t mx_decode_bytes(const Dims &d, int batch, int max_seq, int requested) {
   // the call picks the kernel by the page size too: enough for either
   size_t n = piece_bytes(d) * batch * mx_equal_splits(d, batch, max_seq, requested);
-  if (mx_decode_tuned(d) && batch <= kShareBatch) n = std::max(n, prefix_bytes(batch) + 2 * piece_bytes(d) * mx_shares(d, batch, requested));
+  if (mx_decode_tuned(d) && batch <= kShareBatch) n = std::max(n, prefix_bytes(batch) + piece_bytes(d) * mx_most_pieces(batch, mx_share(d), requested));
   return n;
 }
 
 template <typename T, int KB, int CS>
-static void launch_tuned(const MxAttnArgs &a, int share, int z, hipStream_t st) {
+static void launch_tuned(const MxAttnArgs &a, int pieces, int z, hipStream_t st) {
   constexpr int WPT = CS > 512 ? 2 : 1;
-  constexpr int OCC = CS >= 512 ? 1 : CS >= 256 ? 2 : 3;
-  const int lds = std::max(KB * Parts<T>::Q * 32, 4 / WPT * a.nq * CS * 4);   // the queries, then the waves' sums
-  if (share) {
-    if (lds > 56 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true>, lds);
-    mx_attn_kernel<T, KB, CS, WPT, OCC, true><<<dim3(share, z), 256, lds, st>>>(a);
-    mx_join_kernel<T, true><<<dim3(a.nq, a.batch, (a.dl + 255) / 256), 256, 0, st>>>(a, share);
+  constexpr int OCC = mx_occupancy(CS);
+  const int lds = std::max(KB * Parts<T>::Q * 32, 4 / WPT * a.nq * (CS + 16) * 4);   // the queries, then the waves' sums
+  if (pieces) {
+    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true>, lds);
+    mx_attn_kernel<T, KB, CS, WPT, OCC, true><<<dim3(pieces, z), 256, lds, st>>>(a);
+    mx_join_kernel<T, true><<<dim3(a.nq, a.batch, (a.dl + 255) / 256), 256, 0, st>>>(a);
   } else {
-    if (lds > 56 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, false>, lds);
+    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, false>, lds);
     mx_attn_kernel<T, KB, CS, WPT, OCC, false><<<dim3(a.batch, z), 256, lds, st>>>(a);
   }
 }
 
 template <typename T>
-static void launch_decode(const Dims &d, const MxAttnArgs &a, int share, hipStream_t st) {
-  if (a.splits) {
+static void launch_decode(const Dims &d, const MxAttnArgs &a, bool tuned, int pieces, hipStream_t st) {
+  if (!tuned) {
     mx_attn_any_kernel<T><<<dim3(a.splits, d.nq, a.batch), 256, 0, st>>>(a);
-    mx_join_kernel<T, false><<<dim3(d.nq, a.batch, (d.dl + 255) / 256), 256, 0, st>>>(a, 0);
+    mx_join_kernel<T, false><<<dim3(d.nq, a.batch, (d.dl + 255) / 256), 256, 0, st>>>(a);
     return;
   }
   const int cs = mx_slice_width(d), z = d.wc_w / cs;
   switch (d.wk_w * 4096 + cs) {
-    case 64 * 4096 + 128: return launch_tuned<T, 64, 128>(a, share, z, st);
-    case 64 * 4096 + 256: return launch_tuned<T, 64, 256>(a, share, z, st);
-    case 64 * 4096 + 512: return launch_tuned<T, 64, 512>(a, share, z, st);
-    case 128 * 4096 + 128: return launch_tuned<T, 128, 128>(a, share, z, st);
-    case 128 * 4096 + 256: return launch_tuned<T, 128, 256>(a, share, z, st);
-    case 128 * 4096 + 512: return launch_tuned<T, 128, 512>(a, share, z, st);
-    case 256 * 4096 + 256: return launch_tuned<T, 256, 256>(a, share, z, st);
-    case 256 * 4096 + 512: return launch_tuned<T, 256, 512>(a, share, z, st);
-    case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024>(a, share, z, st);
-    case 512 * 4096 + 512: return launch_tuned<T, 512, 512>(a, share, z, st);
-    case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024>(a, share, z, st);
-    case 1024 * 4096 + 1024: return launch_tuned<T, 1024, 1024>(a, share, z, st);
+    case 64 * 4096 + 128: return launch_tuned<T, 64, 128>(a, pieces, z, st);
+    case 64 * 4096 + 256: return launch_tuned<T, 64, 256>(a, pieces, z, st);
+    case 64 * 4096 + 512: return launch_tuned<T, 64, 512>(a, pieces, z, st);
+    case 128 * 4096 + 128: return launch_tuned<T, 128, 128>(a, pieces, z, st);
+    case 128 * 4096 + 256: return launch_tuned<T, 128, 256>(a, pieces, z, st);
+    case 128 * 4096 + 512: return launch_tuned<T, 128, 512>(a, pieces, z, st);
+    case 256 * 4096 + 256: return launch_tuned<T, 256, 256>(a, pieces, z, st);
+    case 256 * 4096 + 512: return launch_tuned<T, 256, 512>(a, pieces, z, st);
+    case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024>(a, pieces, z, st);
+    case 512 * 4096 + 512: return launch_tuned<T, 512, 512>(a, pieces, z, st);
+    case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024>(a, pieces, z, st);
+    case 1024 * 4096 + 1024: return launch_tuned<T, 1024, 1024>(a, pieces, z, st);
   }
 }
 
 int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int requested, void *ws, size_t ws_bytes, void *l_out,
                      hipStream_t st) {
-  int shift = 0, share = 0, splits = 0;
-  int64_t pieces;
-  size_t head = 0;
-  if (mx_decode_tuned(d) && mx_layout_tuned(cv)) {
-    head = prefix_bytes(batch);
-    pieces = batch <= kShareBatch ? 2 * (int64_t)mx_shares(d, batch, requested) : 0;
-  } else {
+  const bool tuned = mx_decode_tuned(d) && mx_layout_tuned(cv);
+  const size_t head = tuned ? prefix_bytes(batch) : 0;
+  const int64_t fit = ws_bytes > head ? (int64_t)((ws_bytes - head) / piece_bytes(d)) : 0;
+  int share = 0, splits = 0;
+  int64_t pieces = 0;
+  if (ws_bytes < head) return GTA_ERR_WORKSPACE;
+  if (tuned && batch <= kShareBatch) {
+    share = mx_share(d);
+    splits = std::min(requested, 1024);
+    pieces = mx_most_pieces(batch, share, requested);
+    if (fit < pieces) {   // a smaller workspace: as many pieces as it holds, or whole sequences
+      if (requested > 0) return GTA_ERR_WORKSPACE;
+      share = (int)fit;
+      splits = share < 2 * batch ? 1 : 0;
+      pieces = splits ? batch : share;
+    }
+  } else if (!tuned) {
     splits = mx_equal_splits(d, batch, cv.max_seq, requested);
+    if (fit < (int64_t)batch * splits) {
+      if (requested > 0 || fit < batch) return GTA_ERR_WORKSPACE;
+      splits = (int)(fit / batch);
+    }
     pieces = (int64_t)batch * splits;
   }
-  if (pieces) {   // a smaller workspace: as many pieces as it holds
-    const int64_t least = splits ? batch : 2, fit = ws_bytes > head ? (int64_t)((ws_bytes - head) / piece_bytes(d)) : 0;
-    if (fit < pieces && (requested > 0 || fit < least)) return GTA_ERR_WORKSPACE;
-    pieces = std::min(pieces, fit);
-    if (splits) splits = (int)(pieces / batch);
-    else share = (int)(pieces / 2);
-    pieces = splits ? (int64_t)splits * batch : 2 * (int64_t)share;
-  }
+  int shift = 0;
   if (cv.pm.table) while ((1 << shift) < cv.pm.page_size && shift < 30) ++shift;
   float *acc = (float *)((char *)ws + head);
-  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, batch, splits, shift, d.scale * 1.4426950408889634f,
-                     acc, acc + pieces * d.nq * d.dl, (int32_t *)ws, l_out};
-  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, share, st);
-  else launch_decode<float>(d, a, share, st);
+  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, batch, splits, share, shift, d.scale * 1.4426950408889634f,
+                     acc, acc + std::min(pieces, fit) * d.nq * d.dl, (int32_t *)ws, l_out};
+  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, tuned, (int)pieces, st);
+  else launch_decode<float>(d, a, tuned, (int)pieces, st);
   return check_launch();
 }
 
