@@ -129,7 +129,8 @@ typedef struct {
  * 448 * 2^e, kept within -117 .. 119: every stored value is zero or a normal bf16 number, and a code is
  * the element rounded once, to 3 bits behind the leading one (2^-4 relative at most for magnitudes from
  * 2^-6 * 2^e on, half of 2^-9 * 2^e absolute below).  NaN and infinities are stored as NaN and do not enter e.
- * head_dim and latent_dim must be multiples of GTA_MX_BLOCK.  Struct host, arrays device, all
+ * head_dim and latent_dim must be multiples of GTA_MX_BLOCK, a key and a latent row together at most 2^18
+ * elements (GTA_ERR_UNSUPPORTED otherwise).  Struct host, arrays device, all
  * 16-byte aligned (lengths, status and table 4).  Layouts and block table as in gta_cache: row p of a
  * slot has the same index in all four arrays. */
 #define GTA_MX_BLOCK 32

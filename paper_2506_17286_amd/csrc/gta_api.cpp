@@ -492,7 +492,7 @@ int gta_qk_norm_rope(const gta_config *cfg, const void *q, int64_t q_stride, con
   if (misaligned(q_out) || misaligned(k_out) || (((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_gain | (uintptr_t)k_gain) & el) ||
       ((uintptr_t)positions & 3u))
     return GTA_ERR_ALIGN;
-  if (total_tokens * (int64_t)(d.nq + d.nk) > ((int64_t)1 << 32)) return GTA_ERR_UNSUPPORTED;   // launch size
+  if (total_tokens * (int64_t)(d.nq + d.nk) > ((int64_t)1 << 31)) return GTA_ERR_UNSUPPORTED;   // launch size
   if (total_tokens == 0) return GTA_OK;
   return launch_qk_norm_rope(d, q, q_stride, k, k_stride, q_gain, k_gain, eps, positions, total_tokens, q_out, k_out,
                              (hipStream_t)hip_stream);

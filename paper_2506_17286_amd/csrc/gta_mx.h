@@ -27,8 +27,8 @@ inline MxView mx_view_of(const gta_mx_cache &c, const int32_t *slots) {
 // 2^e of a scale byte
 __device__ __forceinline__ float mx_scale(unsigned byte) { return __uint_as_float(byte << 23); }
 
-// Do heads and latents consist of whole blocks?
-inline bool mx_widths_ok(const Dims &d) { return d.dh % kMxBlock == 0 && d.dl % kMxBlock == 0; }
+// Do heads and latents consist of whole blocks, and rows of no more elements than the kernels' divisions take?
+inline bool mx_widths_ok(const Dims &d) { return d.dh % kMxBlock == 0 && d.dl % kMxBlock == 0 && d.wk_w + d.wc_w <= (1 << 18); }
 
 int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t k_stride, const void *c_new, int64_t c_stride,
                      const int32_t *cu_new, int batch, int max_new, hipStream_t st);

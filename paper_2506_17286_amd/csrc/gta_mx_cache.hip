@@ -3,6 +3,8 @@
 //           kept in [-117, 119]; code = x * 2^-e rounded to e4m3 (to nearest, ties to even).  The scaling is by a power of
 //           two and exact, so a code is the one rounding there is.  NaN and infinities become the NaN code.
 //   read:   code * 2^e, exact in bf16 and fp32.
+#include <type_traits>
+
 #include "gta_mx.h"
 
 namespace gta {
@@ -14,8 +16,51 @@ typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
-__device__ __forceinline__ f32x8 load8(const float *p) { f32x8 v; for (int i = 0; i < 8; ++i) v[i] = p[i]; return v; }
-__device__ __forceinline__ f32x8 load8(const __bf16 *p) { f32x8 v; for (int i = 0; i < 8; ++i) v[i] = (float)p[i]; return v; }
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// eight consecutive elements; VEC: on 16 bytes
+template <bool VEC>
+__device__ __forceinline__ f32x8 load8(const float *p) {
+  if constexpr (VEC) return __builtin_shufflevector(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+  f32x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = p[i];
+  return v;
+}
+template <bool VEC>
+__device__ __forceinline__ f32x8 load8(const __bf16 *p) {
+  if constexpr (VEC) return __builtin_convertvector(*reinterpret_cast<const bf16x8 *>(p), f32x8);
+  f32x8 v;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
+  return v;
+}
+__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
+  *reinterpret_cast<f32x4 *>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+}
+__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(v, bf16x8); }
+
+// A workgroup's rows as words of eight elements, keys first: `per_row` of them a row, an inverse of it for divisions of numbers
+// below 2^16.
+struct Words {
+  int kw, cw, per_row;
+  unsigned inverse;
+};
+__device__ __forceinline__ int row_of(const Words &w, int i) { return (int)__umulhi((unsigned)i, w.inverse); }
+constexpr int kMostWords = 4096, kAtOnce = 4;   // words of a workgroup, words that a thread has on their way at once
+
+// Where word i of the workgroup lies: its row there, its column, whether it is a key's.
+struct Place { int row, at, width; bool key; };
+__device__ __forceinline__ Place place_of(const Words &w, int i) {
+  Place p;
+  p.row = row_of(w, i);
+  const int col = (i - p.row * w.per_row) * 8;
+  p.key = col < w.kw;
+  p.at = p.key ? col : col - w.kw;
+  p.width = p.key ? w.kw : w.cw;
+  return p;
+}
 
 // Exponent of a block by its largest finite magnitude: 448 = 1.75 * 2^8.
 __device__ __forceinline__ int mx_exponent(float amax) {
@@ -65,25 +110,37 @@ __device__ __forceinline__ AppendPlan append_plan(const MxView &cv, const int32_
   return a;
 }
 
-// Lanes of a row: one per 8 elements, keys first.  rows_per_wg rows of sequence blockIdx.y from blockIdx.x * rows_per_wg on.
+// rows_per_wg rows of sequence blockIdx.y from blockIdx.x * rows_per_wg on, a thread to eight elements and four threads to a block.
 // COMMIT: the workgroup has the whole sequence and sets its length as well.
-template <typename T, bool COMMIT>
+template <typename T, bool COMMIT, bool VEC>
 __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_new, int64_t k_stride, const T *c_new, int64_t c_stride,
-                                                        const int32_t *cu_new, int kw, int cw, int max_new, int rows_per_wg) {
+                                                        const int32_t *cu_new, Words w, int max_new, int rows_per_wg) {
   const int b = blockIdx.y;
   const AppendPlan a = append_plan(cv, cu_new, b, max_new);
   if (a.slot < 0) return;
   if (a.n <= max_new && !a.full) {
-    const int per_row = (kw + cw) / 8, j0 = blockIdx.x * rows_per_wg, j1 = min(a.n, j0 + rows_per_wg);
-    for (int i = threadIdx.x; i < (j1 - j0) * per_row; i += 256) {
-      const int j = j0 + i / per_row, col = i % per_row * 8;
-      const int64_t src = (int64_t)cu_new[b] + j, dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j);
-      const bool key = col < kw;
-      const int at = key ? col : col - kw, width = key ? kw : cw;
-      int e;
-      const u32x2 codes = quantise8(key ? load8(k_new + src * k_stride + at) : load8(c_new + src * c_stride + at), e);
-      *reinterpret_cast<u32x2 *>((key ? cv.k : cv.c) + dst * width + at) = codes;
-      if ((at & 31) == 0) (key ? cv.ks : cv.cs)[dst * (width / kMxBlock) + at / kMxBlock] = (uint8_t)(e + 127);
+    const int j0 = blockIdx.x * rows_per_wg, words = min(a.n - j0, rows_per_wg) * w.per_row;
+    const int64_t src0 = (int64_t)cu_new[b] + j0;
+    for (int i0 = threadIdx.x; i0 < words; i0 += 256 * kAtOnce) {
+      f32x8 x[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + 256 * u;
+        if (i >= words) break;
+        const Place p = place_of(w, i);
+        x[u] = load8<VEC>(p.key ? k_new + (src0 + p.row) * k_stride + p.at : c_new + (src0 + p.row) * c_stride + p.at);
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + 256 * u;
+        if (i >= words) break;
+        const Place p = place_of(w, i);
+        const int64_t dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j0 + p.row);
+        int e;
+        const u32x2 codes = quantise8(x[u], e);
+        *reinterpret_cast<u32x2 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at) = codes;
+        if ((p.at & 31) == 0) (p.key ? cv.ks : cv.cs)[dst * (p.width / kMxBlock) + p.at / kMxBlock] = (uint8_t)(e + 127);
+      }
     }
   }
   if (COMMIT) {
@@ -107,12 +164,9 @@ __global__ __launch_bounds__(256) void mx_append_commit_kernel(MxView cv, const 
   else cv.seq_lens[a.slot] = a.p + a.n;
 }
 
-__device__ __forceinline__ void store8(float *p, const f32x8 &v) { for (int i = 0; i < 8; ++i) p[i] = v[i]; }
-__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { for (int i = 0; i < 8; ++i) p[i] = (__bf16)v[i]; }
-
 template <typename T>
-__global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *first, const int32_t *cu_rows, int kw, int cw,
-                                                      int max_rows, int rows_per_wg, T *k_out, T *c_out) {
+__global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *first, const int32_t *cu_rows, Words w, int max_rows,
+                                                      int rows_per_wg, T *k_out, T *c_out) {
   const int b = blockIdx.y, n = cu_rows[b + 1] - cu_rows[b];
   const int slot = cv.slots ? cv.slots[b] : b;
   const bool slot_ok = slot >= 0 && slot < cv.max_batch;
@@ -120,44 +174,72 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
     if (slot_ok && blockIdx.x == 0 && threadIdx.x == 0) cv.status[slot] = GTA_ERR_SHAPE;
     return;
   }
-  const int per_row = (kw + cw) / 8, j0 = blockIdx.x * rows_per_wg, j1 = min(n, j0 + rows_per_wg);
-  const int have = slot_ok ? min(cv.seq_lens[slot], cv.max_seq) : 0, f = first ? first[b] : 0;
-  for (int i = threadIdx.x; i < (j1 - j0) * per_row; i += 256) {
-    const int j = j0 + i / per_row, col = i % per_row * 8;
-    const bool key = col < kw;
-    const int at = key ? col : col - kw, width = key ? kw : cw;
-    const int64_t row = (int64_t)f + j;
-    const int64_t src = row >= 0 && row < have ? cache_row(cv.pm, cv.max_seq, slot, (int)row) : -1;
-    f32x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
-    if (src >= 0) {
-      const u32x2 w = *reinterpret_cast<const u32x2 *>((key ? cv.k : cv.c) + src * width + at);
-      const float s = mx_scale((key ? cv.ks : cv.cs)[src * (width / kMxBlock) + at / kMxBlock]);
+  const int j0 = blockIdx.x * rows_per_wg, words = min(n - j0, rows_per_wg) * w.per_row;
+  const int have = slot_ok ? min(cv.seq_lens[slot], cv.max_seq) : 0;
+  const int64_t row0 = (int64_t)(first ? first[b] : 0) + j0, dst0 = (int64_t)cu_rows[b] + j0;
+  for (int i0 = threadIdx.x; i0 < words; i0 += 256 * kAtOnce) {
+    u32x2 codes[kAtOnce];
+    float scale[kAtOnce];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[h], true);
-        v[4 * h] = lo[0] * s; v[4 * h + 1] = lo[1] * s; v[4 * h + 2] = hi[0] * s; v[4 * h + 3] = hi[1] * s;
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + 256 * u;
+      if (i >= words) break;
+      const Place p = place_of(w, i);
+      const int64_t row = row0 + p.row, src = row >= 0 && row < have ? cache_row(cv.pm, cv.max_seq, slot, (int)row) : -1;
+      codes[u] = u32x2{0u, 0u};   // rows that are not there read as zeros
+      scale[u] = 0.f;
+      if (src >= 0) {
+        codes[u] = *reinterpret_cast<const u32x2 *>((p.key ? cv.k : cv.c) + src * p.width + p.at);
+        scale[u] = mx_scale((p.key ? cv.ks : cv.cs)[src * (p.width / kMxBlock) + p.at / kMxBlock]);
       }
     }
-    const int64_t dst = (int64_t)cu_rows[b] + j;
-    store8((key ? k_out : c_out) + dst * width + at, v);
+#pragma unroll
+    for (int u = 0; u < kAtOnce; ++u) {
+      const int i = i0 + 256 * u;
+      if (i >= words) break;
+      const Place p = place_of(w, i);
+      f32x8 v;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], true);
+        v[4 * h] = lo[0] * scale[u]; v[4 * h + 1] = lo[1] * scale[u]; v[4 * h + 2] = hi[0] * scale[u]; v[4 * h + 3] = hi[1] * scale[u];
+      }
+      store8((p.key ? k_out : c_out) + (dst0 + p.row) * p.width + p.at, v);
+    }
   }
 }
 
 }  // namespace
 
+// Rows of a workgroup: about `words` words of them, so that every thread has several loads on their way, and no more than the
+// division takes.
+static int rows_per_workgroup(const Words &w, int words) { return std::max(1, std::min(words, kMostWords) / w.per_row); }
+
+static Words words_of(const Dims &d) {
+  const int per_row = (d.wk_w + d.wc_w) / 8;
+  return Words{d.wk_w, d.wc_w, per_row, (unsigned)(((uint64_t)1 << 32) / per_row + 1)};
+}
+
 int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t k_stride, const void *c_new, int64_t c_stride,
                      const int32_t *cu_new, int batch, int max_new, hipStream_t st) {
-  const int rows = 16;
-  const dim3 grid((unsigned)((max_new + rows - 1) / rows), batch);
+  const Words w = words_of(d);
+  const int most = std::min(max_new, cv.max_seq);   // a sequence of more rows than a slot has stores none
+  // few rows: a workgroup per sequence, which sets the length as well; otherwise the lengths need a launch behind this one
+  const bool one = (int64_t)most * w.per_row <= kMostWords;
+  const int rows = one ? std::max(most, 1) : rows_per_workgroup(w, 1024);
+  const dim3 grid(one ? 1u : (unsigned)(((int64_t)most + rows - 1) / rows), batch);
+  if (grid.x >= (1u << 24)) return GTA_ERR_UNSUPPORTED;   // launch size
   auto run = [&](auto t) {
     using T = decltype(t);
     const T *k = (const T *)k_new, *c = (const T *)c_new;
-    if (grid.x <= 1) {
-      mx_append_kernel<T, true><<<dim3(1, batch), 256, 0, st>>>(cv, k, k_stride, c, c_stride, cu_new, d.wk_w, d.wc_w, max_new, rows);
-      return;
-    }
-    mx_append_kernel<T, false><<<grid, 256, 0, st>>>(cv, k, k_stride, c, c_stride, cu_new, d.wk_w, d.wc_w, max_new, rows);
-    mx_append_commit_kernel<<<(batch + 3) / 4, 256, 0, st>>>(cv, cu_new, batch, max_new);
+    const int64_t per = 16 / (int)sizeof(T);
+    const bool vec = k_stride % per == 0 && c_stride % per == 0 && (((uintptr_t)k | (uintptr_t)c) & 15u) == 0;
+    auto go = [&](auto commit, auto v) {
+      mx_append_kernel<T, decltype(commit)::value, decltype(v)::value><<<grid, 256, 0, st>>>(cv, k, k_stride, c, c_stride, cu_new, w, max_new, rows);
+    };
+    if (one) { if (vec) go(std::true_type{}, std::true_type{}); else go(std::true_type{}, std::false_type{}); }
+    else { if (vec) go(std::false_type{}, std::true_type{}); else go(std::false_type{}, std::false_type{}); }
+    if (!one) mx_append_commit_kernel<<<(batch + 3) / 4, 256, 0, st>>>(cv, cu_new, batch, max_new);
   };
   if (d.dtype == GTA_BF16) run(__bf16{}); else run(float{});
   return check_launch();
@@ -165,13 +247,15 @@ int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t
 
 int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const int32_t *cu_rows, int batch, int max_rows,
                    void *k_out, void *c_out, hipStream_t st) {
-  const int rows = 16;
-  const dim3 grid((unsigned)((max_rows + rows - 1) / rows), batch);
+  const Words w = words_of(d);
+  const int rows = rows_per_workgroup(w, 1024);
+  const dim3 grid((unsigned)(((int64_t)max_rows + rows - 1) / rows), batch);
   if (grid.x == 0) return GTA_OK;
+  if (grid.x >= (1u << 24)) return GTA_ERR_UNSUPPORTED;   // launch size
   if (d.dtype == GTA_BF16)
-    mx_read_kernel<__bf16><<<grid, 256, 0, st>>>(cv, first, cu_rows, d.wk_w, d.wc_w, max_rows, rows, (__bf16 *)k_out, (__bf16 *)c_out);
+    mx_read_kernel<__bf16><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (__bf16 *)k_out, (__bf16 *)c_out);
   else
-    mx_read_kernel<float><<<grid, 256, 0, st>>>(cv, first, cu_rows, d.wk_w, d.wc_w, max_rows, rows, (float *)k_out, (float *)c_out);
+    mx_read_kernel<float><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (float *)k_out, (float *)c_out);
   return check_launch();
 }
 

@@ -1,6 +1,10 @@
 // RMS norm of every query and key head with its rotation (App. B.1.1) in the same pass:
 //   y_j = x_j / sqrt(mean_i x_i^2 + eps) * gain_j,   then (y_j, y_{j + d/2}) turned by position * base^(-2j/d).
 // Sums, the norm and the rotation are fp32 (angles fp64); the only rounding to 16 bits is that of the result.
+#include <math.h>
+
+#include <type_traits>
+
 #include "gta_mx.h"
 #include "gta_rope.h"
 
@@ -56,13 +60,117 @@ __global__ __launch_bounds__(256) void norm_rope_any_kernel(NormRopeArgs a) {
   }
 }
 
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+__device__ __forceinline__ f32x8 load8(const __bf16 *p) { return __builtin_convertvector(*reinterpret_cast<const bf16x8 *>(p), f32x8); }
+__device__ __forceinline__ f32x8 load8(const float *p) {
+  return __builtin_shufflevector(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(v, bf16x8); }
+__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
+  *reinterpret_cast<f32x4 *>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+}
+
+struct RopeFreqs { double f[128]; };   // base^(-2j/d_h), j < d_h/2, from the host
+
+// Heads of 16 * LANES elements, rows and rows' starts in whole 16 bytes.  A lane has eight elements j.. and their partners
+// j + d_h/2 of HEADS heads of one token: their sines are the same and worked out once, a head's sum of squares is taken over
+// LANES neighbours, and loads and stores are 16 bytes.  Bound by memory where there are many tokens and by the launch where there
+// are few.
+template <typename T, int LANES, int HEADS>
+__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, RopeFreqs rf) {
+  constexpr int DH = 16 * LANES, HALF = DH / 2;
+  const int heads = a.nq + a.nk, groups = (heads + HEADS - 1) / HEADS;
+  const unsigned item = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, row = item / groups;   // token and group of heads
+  const int j = threadIdx.x % LANES * 8;
+  const int64_t t = row;
+  if (t >= a.total) return;
+  const int h0 = (int)(item - row * groups) * HEADS;
+  const int p = a.rope ? (a.positions ? a.positions[t] : (int)t) : 0;
+  const T *qg = (const T *)a.q_gain, *kg = (const T *)a.k_gain;
+  f32x8 lo[HEADS], hi[HEADS];
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = min(h0 + i, heads - 1);   // (a last group may be short: it repeats a head and stores nothing for it)
+    const T *x = h < a.nq ? (const T *)a.q + t * a.q_stride + h * DH : (const T *)a.k + t * a.k_stride + (h - a.nq) * DH;
+    lo[i] = load8(x + j);
+    hi[i] = load8(x + j + HALF);
+  }
+  f32x8 cs, sn;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float2 c = make_float2(1.f, 0.f);
+    if (a.rope) c = sizeof(T) == 2 ? rope_cos_sin_short(p, rf.f[j + e]) : rope_cos_sin(p, rf.f[j + e]);
+    cs[e] = c.x;
+    sn[e] = c.y;
+  }
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = h0 + i;
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss = fmaf(lo[i][e], lo[i][e], fmaf(hi[i][e], hi[i][e], ss));
+#pragma unroll
+    for (int m = 1; m < LANES; m <<= 1) ss += __shfl_xor(ss, m);
+    const float r = rsqrtf(ss * (1.f / DH) + a.eps);
+    const T *gain = h < a.nq ? qg : kg;
+    lo[i] *= r;
+    hi[i] *= r;
+    if (gain) {
+      lo[i] *= load8(gain + j);
+      hi[i] *= load8(gain + j + HALF);
+    }
+    if (h < heads) {
+      T *y = h < a.nq ? (T *)a.q_out + (t * a.nq + h) * DH : (T *)a.k_out + (t * a.nk + h - a.nq) * DH;
+      store8(y + j, lo[i] * cs - hi[i] * sn);
+      store8(y + j + HALF, hi[i] * cs + lo[i] * sn);
+    }
+  }
+}
+
 }  // namespace
+
+template <typename T, int LANES>
+static void launch_vector(const NormRopeArgs &a, hipStream_t st) {
+  RopeFreqs rf{};
+  if (a.rope)
+    for (int j = 0; j < a.dh / 2; ++j) rf.f[j] = pow(a.base, -2.0 * j / a.dh);
+  const int heads = a.nq + a.nk;
+  auto run = [&](auto n) {
+    constexpr int HEADS = decltype(n)::value;
+    const int64_t threads = a.total * ((heads + HEADS - 1) / HEADS) * LANES;
+    norm_rope_kernel<T, LANES, HEADS><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(a, rf);
+  };
+  // few tokens: a head to every group of lanes, so that its load is the only one waited for
+  if (a.total * heads * LANES < (1 << 17)) run(std::integral_constant<int, 1>{});
+  else run(std::integral_constant<int, 4>{});
+}
+
+// Heads of 32, 64, 128 or 256, 16-byte rows and frequencies that the short reduction takes.
+template <typename T>
+static bool try_vector(const NormRopeArgs &a, hipStream_t st) {
+  const int64_t per = 16 / (int)sizeof(T);
+  if (a.q_stride % per || a.k_stride % per || (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.q_gain | (uintptr_t)a.k_gain) & 15u) ||
+      !rope_angles_small(a.rope, a.base))
+    return false;
+  switch (a.dh) {
+    case 32: launch_vector<T, 2>(a, st); return true;
+    case 64: launch_vector<T, 4>(a, st); return true;
+    case 128: launch_vector<T, 8>(a, st); return true;
+    case 256: launch_vector<T, 16>(a, st); return true;
+    default: return false;
+  }
+}
 
 int launch_qk_norm_rope(const Dims &d, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *q_gain,
                         const void *k_gain, float eps, const int32_t *positions, int64_t total, void *q_out, void *k_out,
                         hipStream_t st) {
   const NormRopeArgs a{q, k, q_gain, k_gain, q_stride, k_stride, positions, q_out, k_out, total, d.nq, d.nk, d.dh, d.rope, eps,
                        d.rope_base};
+  if (d.dtype == GTA_BF16 ? try_vector<__bf16>(a, st) : try_vector<float>(a, st)) return check_launch();
   const int64_t items = total * (d.nq + d.nk);
   const dim3 grid((unsigned)((items + 3) / 4));
   if (d.dtype == GTA_BF16) norm_rope_any_kernel<__bf16><<<grid, 256, 0, st>>>(a);
