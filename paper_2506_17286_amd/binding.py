@@ -159,6 +159,20 @@ def _stream(stream) -> Optional[int]:
     return h or None
 
 
+def _device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
+def _on(device: int, t) -> Optional[int]:
+    """Address of a tensor that has to be on the current device (its stream and kernels are that device's)."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"tensor on {t.device}, current device is cuda:{device}")
+    return t.data_ptr()
+
+
 def make_weights(w: Dict[str, "object"]) -> gta_weights:
     return gta_weights(_ptr(w["wq"]), _ptr(w["wk"]), _ptr(w["wc"]), _ptr(w["wg"]), _ptr(w["wp"]), _ptr(w.get("wo")))
 
@@ -320,8 +334,9 @@ def gta_decode_combine(cfg: gta_config, cache: gta_cache, slots, batch: int, num
 
 def gta_qk_norm_rope(cfg: gta_config, q, q_stride: int, k, k_stride: int, q_gain, k_gain, eps: float, positions,
                      total_tokens: int, q_out, k_out, stream=None, check: bool = True) -> int:
-    rc = load().gta_qk_norm_rope(ctypes.byref(cfg), _ptr(q), q_stride, _ptr(k), k_stride, _ptr(q_gain), _ptr(k_gain), eps,
-                                 _ptr(positions), total_tokens, _ptr(q_out), _ptr(k_out), _stream(stream))
+    d = _device()
+    rc = load().gta_qk_norm_rope(ctypes.byref(cfg), _on(d, q), q_stride, _on(d, k), k_stride, _on(d, q_gain), _on(d, k_gain),
+                                 eps, _on(d, positions), total_tokens, _on(d, q_out), _on(d, k_out), _stream(stream))
     if check:
         _check(rc, "gta_qk_norm_rope")
     return rc
@@ -329,8 +344,9 @@ def gta_qk_norm_rope(cfg: gta_config, q, q_stride: int, k, k_stride: int, q_gain
 
 def gta_mx_cache_append(cfg: gta_config, cache: gta_mx_cache, slots, k_new, k_stride: int, c_new, c_stride: int, cu_new,
                         batch: int, max_new: int, stream=None, check: bool = True) -> int:
-    rc = load().gta_mx_cache_append(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _ptr(slots),
-                                    _ptr(k_new), k_stride, _ptr(c_new), c_stride, _ptr(cu_new), batch, max_new,
+    d = _device()
+    rc = load().gta_mx_cache_append(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _on(d, slots),
+                                    _on(d, k_new), k_stride, _on(d, c_new), c_stride, _on(d, cu_new), batch, max_new,
                                     _stream(stream))
     if check:
         _check(rc, "gta_mx_cache_append")
@@ -339,8 +355,10 @@ def gta_mx_cache_append(cfg: gta_config, cache: gta_mx_cache, slots, k_new, k_st
 
 def gta_mx_cache_read(cfg: gta_config, cache: gta_mx_cache, slots, first, cu_rows, batch: int, max_rows: int, k_out, c_out,
                       stream=None, check: bool = True) -> int:
-    rc = load().gta_mx_cache_read(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _ptr(slots),
-                                  _ptr(first), _ptr(cu_rows), batch, max_rows, _ptr(k_out), _ptr(c_out), _stream(stream))
+    d = _device()
+    rc = load().gta_mx_cache_read(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _on(d, slots),
+                                  _on(d, first), _on(d, cu_rows), batch, max_rows, _on(d, k_out), _on(d, c_out),
+                                  _stream(stream))
     if check:
         _check(rc, "gta_mx_cache_read")
     return rc
@@ -348,8 +366,9 @@ def gta_mx_cache_read(cfg: gta_config, cache: gta_mx_cache, slots, first, cu_row
 
 def gta_mx_decode_attention(cfg: gta_config, q, cache: gta_mx_cache, slots, batch: int, num_splits: int, l_out, workspace,
                             stream=None, check: bool = True) -> int:
-    rc = load().gta_mx_decode_attention(ctypes.byref(cfg), _ptr(q), ctypes.byref(cache) if cache is not None else None,
-                                        _ptr(slots), batch, num_splits, _ptr(l_out), _ptr(workspace),
+    d = _device()
+    rc = load().gta_mx_decode_attention(ctypes.byref(cfg), _on(d, q), ctypes.byref(cache) if cache is not None else None,
+                                        _on(d, slots), batch, num_splits, _on(d, l_out), _on(d, workspace),
                                         0 if workspace is None else workspace.numel() * workspace.element_size(),
                                         _stream(stream))
     if check:

@@ -35,11 +35,6 @@ __device__ __forceinline__ f32x8 load8(const __bf16 *p) {
   for (int i = 0; i < 8; ++i) v[i] = (float)p[i];
   return v;
 }
-__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
-  *reinterpret_cast<f32x4 *>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-  *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-}
-__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(v, bf16x8); }
 
 // A workgroup's rows as words of eight elements, keys first: `per_row` of them a row, an inverse of it for divisions of numbers
 // below 2^16.
@@ -48,7 +43,7 @@ struct Words {
   unsigned inverse;
 };
 __device__ __forceinline__ int row_of(const Words &w, int i) { return (int)__umulhi((unsigned)i, w.inverse); }
-constexpr int kMostWords = 4096, kAtOnce = 4;   // words of a workgroup, words that a thread has on their way at once
+constexpr int kMostWords = 4096, kAtOnce = 2;   // words of a workgroup, words that a thread has on their way at once
 
 // Where word i of the workgroup lies: its row there, its column, whether it is a key's.
 struct Place { int row, at, width; bool key; };
@@ -138,7 +133,7 @@ __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_ne
         const int64_t dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j0 + p.row);
         int e;
         const u32x2 codes = quantise8(x[u], e);
-        *reinterpret_cast<u32x2 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at) = codes;
+        store16<!COMMIT>(reinterpret_cast<u32x2 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at), codes);   // (prompts: past the caches)
         if ((p.at & 31) == 0) (p.key ? cv.ks : cv.cs)[dst * (p.width / kMxBlock) + p.at / kMxBlock] = (uint8_t)(e + 127);
       }
     }
@@ -164,7 +159,7 @@ __global__ __launch_bounds__(256) void mx_append_commit_kernel(MxView cv, const 
   else cv.seq_lens[a.slot] = a.p + a.n;
 }
 
-template <typename T>
+template <typename T, bool NT>
 __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *first, const int32_t *cu_rows, Words w, int max_rows,
                                                       int rows_per_wg, T *k_out, T *c_out) {
   const int b = blockIdx.y, n = cu_rows[b + 1] - cu_rows[b];
@@ -204,7 +199,7 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
         const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], true);
         v[4 * h] = lo[0] * scale[u]; v[4 * h + 1] = lo[1] * scale[u]; v[4 * h + 2] = hi[0] * scale[u]; v[4 * h + 3] = hi[1] * scale[u];
       }
-      store8((p.key ? k_out : c_out) + (dst0 + p.row) * p.width + p.at, v);
+      store8<NT>((p.key ? k_out : c_out) + (dst0 + p.row) * p.width + p.at, v);
     }
   }
 }
@@ -252,10 +247,15 @@ int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const 
   const dim3 grid((unsigned)(((int64_t)max_rows + rows - 1) / rows), batch);
   if (grid.x == 0) return GTA_OK;
   if (grid.x >= (1u << 24)) return GTA_ERR_UNSUPPORTED;   // launch size
-  if (d.dtype == GTA_BF16)
-    mx_read_kernel<__bf16><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (__bf16 *)k_out, (__bf16 *)c_out);
-  else
-    mx_read_kernel<float><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (float *)k_out, (float *)c_out);
+  auto run = [&](auto t, auto nt) {
+    using T = decltype(t);
+    mx_read_kernel<T, decltype(nt)::value><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (T *)k_out, (T *)c_out);
+  };
+  if (stream_past_caches((int64_t)batch * max_rows * (d.wk_w + d.wc_w) * d.esize())) {
+    if (d.dtype == GTA_BF16) run(__bf16{}, std::true_type{}); else run(float{}, std::true_type{});
+  } else {
+    if (d.dtype == GTA_BF16) run(__bf16{}, std::false_type{}); else run(float{}, std::false_type{});
+  }
   return check_launch();
 }
 

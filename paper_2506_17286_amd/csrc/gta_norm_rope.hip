@@ -68,20 +68,15 @@ __device__ __forceinline__ f32x8 load8(const __bf16 *p) { return __builtin_conve
 __device__ __forceinline__ f32x8 load8(const float *p) {
   return __builtin_shufflevector(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { *reinterpret_cast<bf16x8 *>(p) = __builtin_convertvector(v, bf16x8); }
-__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
-  *reinterpret_cast<f32x4 *>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
-  *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
-}
 
-struct RopeFreqs { double f[128]; };   // base^(-2j/d_h), j < d_h/2, from the host
+struct Turns { uint64_t t[128]; };   // what one position turns pair j < d_h/2 by from the host
 
 // Heads of 16 * LANES elements, rows and rows' starts in whole 16 bytes.  A lane has eight elements j.. and their partners
 // j + d_h/2 of HEADS heads of one token: their sines are the same and worked out once, a head's sum of squares is taken over
 // LANES neighbours, and loads and stores are 16 bytes.  Bound by memory where there are many tokens and by the launch where there
 // are few.
-template <typename T, int LANES, int HEADS>
-__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, RopeFreqs rf) {
+template <typename T, int LANES, int HEADS, bool NT>
+__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, Turns turns) {
   constexpr int DH = 16 * LANES, HALF = DH / 2;
   const int heads = a.nq + a.nk, groups = (heads + HEADS - 1) / HEADS;
   const unsigned item = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, row = item / groups;   // token and group of heads
@@ -103,7 +98,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, RopeFreq
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     float2 c = make_float2(1.f, 0.f);
-    if (a.rope) c = sizeof(T) == 2 ? rope_cos_sin_short(p, rf.f[j + e]) : rope_cos_sin(p, rf.f[j + e]);
+    if (a.rope) c = rope_cos_sin_turn(p, turns.t[j + e]);
     cs[e] = c.x;
     sn[e] = c.y;
   }
@@ -125,8 +120,8 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, RopeFreq
     }
     if (h < heads) {
       T *y = h < a.nq ? (T *)a.q_out + (t * a.nq + h) * DH : (T *)a.k_out + (t * a.nk + h - a.nq) * DH;
-      store8(y + j, lo[i] * cs - hi[i] * sn);
-      store8(y + j + HALF, hi[i] * cs + lo[i] * sn);
+      store8<NT>(y + j, lo[i] * cs - hi[i] * sn);
+      store8<NT>(y + j + HALF, hi[i] * cs + lo[i] * sn);
     }
   }
 }
@@ -135,26 +130,25 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, RopeFreq
 
 template <typename T, int LANES>
 static void launch_vector(const NormRopeArgs &a, hipStream_t st) {
-  RopeFreqs rf{};
-  if (a.rope)
-    for (int j = 0; j < a.dh / 2; ++j) rf.f[j] = pow(a.base, -2.0 * j / a.dh);
+  Turns turns{};
+  if (a.rope) rope_turns(a.base, a.dh, a.dh / 2, turns.t);
   const int heads = a.nq + a.nk;
-  auto run = [&](auto n) {
+  auto run = [&](auto n, auto nt) {
     constexpr int HEADS = decltype(n)::value;
     const int64_t threads = a.total * ((heads + HEADS - 1) / HEADS) * LANES;
-    norm_rope_kernel<T, LANES, HEADS><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(a, rf);
+    norm_rope_kernel<T, LANES, HEADS, decltype(nt)::value><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(a, turns);
   };
   // few tokens: a head to every group of lanes, so that its load is the only one waited for
-  if (a.total * heads * LANES < (1 << 17)) run(std::integral_constant<int, 1>{});
-  else run(std::integral_constant<int, 4>{});
+  if (a.total * heads * LANES < (1 << 17)) run(std::integral_constant<int, 1>{}, std::false_type{});
+  else if (stream_past_caches(a.total * heads * a.dh * (int64_t)sizeof(T))) run(std::integral_constant<int, 4>{}, std::true_type{});
+  else run(std::integral_constant<int, 4>{}, std::false_type{});
 }
 
-// Heads of 32, 64, 128 or 256, 16-byte rows and frequencies that the short reduction takes.
+// Heads of 32, 64, 128 or 256 and 16-byte rows.
 template <typename T>
 static bool try_vector(const NormRopeArgs &a, hipStream_t st) {
   const int64_t per = 16 / (int)sizeof(T);
-  if (a.q_stride % per || a.k_stride % per || (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.q_gain | (uintptr_t)a.k_gain) & 15u) ||
-      !rope_angles_small(a.rope, a.base))
+  if (a.q_stride % per || a.k_stride % per || (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.q_gain | (uintptr_t)a.k_gain) & 15u))
     return false;
   switch (a.dh) {
     case 32: launch_vector<T, 2>(a, st); return true;
