@@ -135,8 +135,10 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
 }
 
 // ---- matrix-instruction kernel ------------------------------------------------------------------
-// A wave takes tiles of TT rows and keeps everything of a tile in registers, codes included: no barrier until the waves'
-// sums are joined, and the loads of the next tile go out piece by piece as the registers of this one come free.
+// A wave takes tiles of 32 rows and keeps everything of a tile in registers, codes included; the loads of the next tile go out
+// piece by piece as the registers of this one come free, so that about a tile per wave is on its way at any time (96 to 128 KiB
+// of a CU).  No barrier until the waves' sums are joined, but for the one a tile of waves that work in pairs.  What is left is
+// memory: in the loop 64 x 8192 rows of 1056 bytes come in at 6.6 TB/s, rows of 2112 at 6.0 (a bare read: 6.8 to 7.05).
 //
 //   scores  S[t][g] = K q: rows t are the 16 rows of the first operand (lane x = l % 16 has row x, 16 bytes of every 64-byte
 //           piece of it from h = l / 16 on), maps g the 16 columns of the second.  Codes become bf16 with their block's scale
@@ -303,9 +305,11 @@ __device__ __forceinline__ int cut_lanes(const MxView &cv, int batch, int per_ro
   return __builtin_amdgcn_readlane(run, 63);
 }
 
-// KB bytes of a key row, CS latent columns of a workgroup.  WPT waves take a tile of 32 rows together where the sums of all columns
-// would not fit one wave's registers: each has the scores of its half of the rows, hands them to the other through LDS, and the
-// sums of its half of the columns.
+// KB bytes of a key row, CS latent columns of a workgroup.  WPT: from 512 columns on two waves take a tile together; each has the
+// scores of its half of the rows, hands them to the other through LDS, and the sums of its half of the columns.  With 1024 the
+// sums alone would fill the accumulation registers (rows of 2112 bytes: 95 us against 67 for 8 x 8000..32768); with 512 one wave
+// can do it, but twice the waves for half the registers fill and drain sooner (one sequence of 8192 rows 17.3 -> 15.4 us, 64
+// of them the same).
 template <typename T, int KB, int CS, int WPT, int OCC, bool SHARED>
 __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int NQP = Parts<T>::Q, NPP = Parts<T>::P;
@@ -809,8 +813,8 @@ static bool mx_layout_tuned(const MxView &cv) {
   return !cv.pm.table || (cv.pm.page_size >= 16 && (cv.pm.page_size & (cv.pm.page_size - 1)) == 0);
 }
 
-// Workgroups per CU, by the registers that a slice's sums, a tile's codes and the rest take.
-constexpr int mx_occupancy(int cs) { return cs >= 512 ? 1 : cs >= 256 ? 2 : 3; }
+// Workgroups per CU, by the registers that a wave's sums, its codes and the rest take.
+constexpr int mx_occupancy(int cs) { return cs >= 1024 ? 1 : cs >= 256 ? 2 : 3; }
 
 // Workgroups that the chip holds at once.
 static int mx_share(const Dims &d) {
@@ -841,7 +845,7 @@ size_t mx_decode_bytes(const Dims &d, int batch, int max_seq, int requested) {
 
 template <typename T, int KB, int CS>
 static void launch_tuned(const MxAttnArgs &a, int pieces, int z, hipStream_t st) {
-  constexpr int WPT = CS > 512 ? 2 : 1;
+  constexpr int WPT = CS >= 512 ? 2 : 1;
   constexpr int OCC = mx_occupancy(CS);
   const int lds = std::max(KB * Parts<T>::Q * 32, 4 / WPT * a.nq * (CS + 16) * 4);   // the queries, then the waves' sums
   if (pieces) {

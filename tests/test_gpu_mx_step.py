@@ -175,3 +175,19 @@ def test_prompt_in_and_conversation_out():
     assert seq.cpu().tolist() == [n + 10 for n in lens] and torch.isfinite(out).all()
     for b, n in enumerate(lens):
         assert torch.equal(k16[b, :n], kr[cu_np[b]:cu_np[b + 1]]) and torch.equal(c16[b, :n], cr[cu_np[b]:cu_np[b + 1]])
+
+
+def test_tensors_that_are_not_on_the_device_are_refused():
+    s = Step("paper", [3, 0], 0)
+    s.run()
+    host = torch.zeros_like(s.q, device="cpu")
+    with pytest.raises(ValueError):
+        B.gta_qk_norm_rope(s.cfg, host, s.q.stride(0), s.k, s.k.stride(0), None, None, 1e-6, None, 2, s.qn, s.kn)
+    with pytest.raises(ValueError):
+        B.gta_mx_cache_append(s.cfg, s.cache.struct, None, s.kn, 64, s.c, 128, s.cu.cpu(), 2, 1)
+    with pytest.raises(ValueError):
+        B.gta_mx_cache_read(s.cfg, s.cache.struct, None, None, s.cu, 2, 1, s.kn, s.c.cpu())
+    with pytest.raises(ValueError):
+        B.gta_mx_decode_attention(s.cfg, s.qn, s.cache.struct, None, 2, 0, s.l, s.ws.cpu())
+    s.run()
+    torch.cuda.synchronize()
