@@ -24,9 +24,10 @@ inline MxView mx_view_of(const gta_mx_cache &c, const int32_t *slots) {
                 PageMap{c.block_table, c.page_size, c.pages_per_slot, c.num_pages}};
 }
 
-// Results of more bytes than the L2s hold (8 of 4 MiB) are stored past them (non-temporal): nothing of the beginning would be left
-// there when the next kernel asks for it, and the stores run faster (rows of 100 MB read back 42 -> 26 us, 44 MB of normed rows
-// 22 -> 19).  Smaller ones stay for whoever reads them next, in the same time.
+// Results of more bytes than the L2s hold (8 of 4 MiB) are stored past them (non-temporal) where a wave's stores fill whole lines,
+// which is where a thread has one 16-byte word: nothing of the beginning would be left in the L2s when the next kernel asks for
+// it, and the stores run faster (rows of 100 MB read back 42 -> 25 us, 44 MB of normed rows 22 -> 19).  Smaller ones stay for
+// whoever reads them next, in the same time.
 inline bool stream_past_caches(int64_t bytes) { return bytes > (32 << 20); }
 
 typedef __attribute__((ext_vector_type(4))) float mx_f32x4;
@@ -43,8 +44,9 @@ template <bool NT>
 __device__ __forceinline__ void store8(__bf16 *p, const mx_f32x8 &v) { store16<NT>(reinterpret_cast<mx_bf16x8 *>(p), __builtin_convertvector(v, mx_bf16x8)); }
 template <bool NT>
 __device__ __forceinline__ void store8(float *p, const mx_f32x8 &v) {
-  store16<NT>(reinterpret_cast<mx_f32x4 *>(p), __builtin_shufflevector(v, v, 0, 1, 2, 3));
-  store16<NT>(reinterpret_cast<mx_f32x4 *>(p + 4), __builtin_shufflevector(v, v, 4, 5, 6, 7));
+  static_assert(!NT, "two words a thread");
+  store16<false>(reinterpret_cast<mx_f32x4 *>(p), __builtin_shufflevector(v, v, 0, 1, 2, 3));
+  store16<false>(reinterpret_cast<mx_f32x4 *>(p + 4), __builtin_shufflevector(v, v, 4, 5, 6, 7));
 }
 
 // 2^e of a scale byte

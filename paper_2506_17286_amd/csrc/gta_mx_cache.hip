@@ -36,21 +36,21 @@ __device__ __forceinline__ f32x8 load8(const __bf16 *p) {
   return v;
 }
 
-// A workgroup's rows as words of eight elements, keys first: `per_row` of them a row, an inverse of it for divisions of numbers
-// below 2^16.
+// A workgroup's rows as words of ELEMS elements, keys first: `per_row` of them a row, and an inverse of it for divisions (exact for
+// the numbers that come up: below 2^12, or below per_row <= 2^15).
 struct Words {
   int kw, cw, per_row;
   unsigned inverse;
 };
-__device__ __forceinline__ int row_of(const Words &w, int i) { return (int)__umulhi((unsigned)i, w.inverse); }
-constexpr int kMostWords = 4096, kAtOnce = 2;   // words of a workgroup, words that a thread has on their way at once
+constexpr int kMostWords = 4096;   // of a workgroup
 
 // Where word i of the workgroup lies: its row there, its column, whether it is a key's.
 struct Place { int row, at, width; bool key; };
+template <int ELEMS>
 __device__ __forceinline__ Place place_of(const Words &w, int i) {
   Place p;
-  p.row = row_of(w, i);
-  const int col = (i - p.row * w.per_row) * 8;
+  p.row = (int)__umulhi((unsigned)i, w.inverse);
+  const int col = (i - p.row * w.per_row) * ELEMS;
   p.key = col < w.kw;
   p.at = p.key ? col : col - w.kw;
   p.width = p.key ? w.kw : w.cw;
@@ -64,29 +64,28 @@ __device__ __forceinline__ int mx_exponent(float amax) {
   return min(max(e, kMxMinExp), kMxMaxExp);
 }
 
-// Eight elements of a block, four lanes to a block: codes, and the block's exponent.
-__device__ __forceinline__ u32x2 quantise8(const f32x8 &x, int &e) {
+// Sixteen elements of a block, two lanes to a block: codes, and the block's exponent.
+__device__ __forceinline__ u32x4 quantise16(const f32x8 (&x)[2], int &e) {
   float amax = 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) { const float m = fabsf(x[i]); amax = fmaxf(amax, m < INFINITY ? m : 0.f); }
+  for (int i = 0; i < 16; ++i) { const float m = fabsf(x[i >> 3][i & 7]); amax = fmaxf(amax, m < INFINITY ? m : 0.f); }
   amax = fmaxf(amax, __shfl_xor(amax, 1));
-  amax = fmaxf(amax, __shfl_xor(amax, 2));
   e = mx_exponent(amax);
   const float inv = __uint_as_float((unsigned)(127 - e) << 23);
-  float y[8];
+  u32x4 w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const bool finite = fabsf(x[i]) < INFINITY;
-    const float s = fminf(fmaxf(x[i] * inv, -448.f), 448.f);   // beyond 448 only where e is at its upper end
-    y[i] = finite ? s : __builtin_nanf("");
-  }
-  unsigned w[2];
+  for (int i = 0; i < 4; ++i) {
+    float y[4];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i], y[4 * i + 1], 0, false);
-    w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * i + 2], y[4 * i + 3], r, true);
+    for (int j = 0; j < 4; ++j) {
+      const float v = x[i >> 1][(i & 1) * 4 + j];
+      const float s = fminf(fmaxf(v * inv, -448.f), 448.f);   // beyond 448 only where e is at its upper end
+      y[j] = fabsf(v) < INFINITY ? s : __builtin_nanf("");
+    }
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    w[i] = (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], r, true);
   }
-  return u32x2{w[0], w[1]};
+  return w;
 }
 
 // What sequence b adds, or why it does not: rows (0: nothing to do), slot, first row.
@@ -105,7 +104,10 @@ __device__ __forceinline__ AppendPlan append_plan(const MxView &cv, const int32_
   return a;
 }
 
-// rows_per_wg rows of sequence blockIdx.y from blockIdx.x * rows_per_wg on, a thread to eight elements and four threads to a block.
+// rows_per_wg rows of sequence blockIdx.y from blockIdx.x * rows_per_wg on, a thread to sixteen elements and two threads to a block:
+// a whole 16-byte word of codes to store (eight elements a thread: 16 sequences of 300..2048 rows of 2048 elements 39 us against 31).
+// Bound by memory, and by the chain of loads in front (lengths, slot, pages) where there are few rows; with a second word on its
+// way per thread it took as long.
 // COMMIT: the workgroup has the whole sequence and sets its length as well.
 template <typename T, bool COMMIT, bool VEC>
 __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_new, int64_t k_stride, const T *c_new, int64_t c_stride,
@@ -116,26 +118,15 @@ __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_ne
   if (a.n <= max_new && !a.full) {
     const int j0 = blockIdx.x * rows_per_wg, words = min(a.n - j0, rows_per_wg) * w.per_row;
     const int64_t src0 = (int64_t)cu_new[b] + j0;
-    for (int i0 = threadIdx.x; i0 < words; i0 += 256 * kAtOnce) {
-      f32x8 x[kAtOnce];
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int i = i0 + 256 * u;
-        if (i >= words) break;
-        const Place p = place_of(w, i);
-        x[u] = load8<VEC>(p.key ? k_new + (src0 + p.row) * k_stride + p.at : c_new + (src0 + p.row) * c_stride + p.at);
-      }
-#pragma unroll
-      for (int u = 0; u < kAtOnce; ++u) {
-        const int i = i0 + 256 * u;
-        if (i >= words) break;
-        const Place p = place_of(w, i);
-        const int64_t dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j0 + p.row);
-        int e;
-        const u32x2 codes = quantise8(x[u], e);
-        store16<!COMMIT>(reinterpret_cast<u32x2 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at), codes);   // (prompts: past the caches)
-        if ((p.at & 31) == 0) (p.key ? cv.ks : cv.cs)[dst * (p.width / kMxBlock) + p.at / kMxBlock] = (uint8_t)(e + 127);
-      }
+    for (int i = threadIdx.x; i < words; i += 256) {
+      const Place p = place_of<16>(w, i);
+      const T *src = p.key ? k_new + (src0 + p.row) * k_stride + p.at : c_new + (src0 + p.row) * c_stride + p.at;
+      const f32x8 x[2] = {load8<VEC>(src), load8<VEC>(src + 8)};
+      const int64_t dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j0 + p.row);
+      int e;
+      const u32x4 codes = quantise16(x, e);
+      store16<!COMMIT>(reinterpret_cast<u32x4 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at), codes);   // (prompts: past the caches)
+      if ((p.at & 31) == 0) (p.key ? cv.ks : cv.cs)[dst * (p.width / kMxBlock) + p.at / kMxBlock] = (uint8_t)(e + 127);
     }
   }
   if (COMMIT) {
@@ -159,6 +150,11 @@ __global__ __launch_bounds__(256) void mx_append_commit_kernel(MxView cv, const 
   else cv.seq_lens[a.slot] = a.p + a.n;
 }
 
+// Eight elements a thread: one 16-byte word of bf16 to store, next to its neighbours'.  Stores past the caches want that: with two
+// words a thread, 32 bytes apart, they take twice as long (41 000 rows 25 us against 46), and fp32, which has two, goes through
+// the caches (16 400 rows 17 us against 26).  Two words of codes on their way per thread.
+constexpr int kAtOnce = 2;
+
 template <typename T, bool NT>
 __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *first, const int32_t *cu_rows, Words w, int max_rows,
                                                       int rows_per_wg, T *k_out, T *c_out) {
@@ -179,7 +175,7 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = i0 + 256 * u;
       if (i >= words) break;
-      const Place p = place_of(w, i);
+      const Place p = place_of<8>(w, i);
       const int64_t row = row0 + p.row, src = row >= 0 && row < have ? cache_row(cv.pm, cv.max_seq, slot, (int)row) : -1;
       codes[u] = u32x2{0u, 0u};   // rows that are not there read as zeros
       scale[u] = 0.f;
@@ -192,7 +188,7 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = i0 + 256 * u;
       if (i >= words) break;
-      const Place p = place_of(w, i);
+      const Place p = place_of<8>(w, i);
       f32x8 v;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -206,22 +202,21 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
 
 }  // namespace
 
-// Rows of a workgroup: about `words` words of them, so that every thread has several loads on their way, and no more than the
-// division takes.
-static int rows_per_workgroup(const Words &w, int words) { return std::max(1, std::min(words, kMostWords) / w.per_row); }
+// Rows of a workgroup: about `words` words of them.
+static int rows_per_workgroup(const Words &w, int words) { return std::max(1, words / w.per_row); }
 
-static Words words_of(const Dims &d) {
-  const int per_row = (d.wk_w + d.wc_w) / 8;
+static Words words_of(const Dims &d, int elems) {
+  const int per_row = (d.wk_w + d.wc_w) / elems;
   return Words{d.wk_w, d.wc_w, per_row, (unsigned)(((uint64_t)1 << 32) / per_row + 1)};
 }
 
 int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t k_stride, const void *c_new, int64_t c_stride,
                      const int32_t *cu_new, int batch, int max_new, hipStream_t st) {
-  const Words w = words_of(d);
+  const Words w = words_of(d, 16);
   const int most = std::min(max_new, cv.max_seq);   // a sequence of more rows than a slot has stores none
   // few rows: a workgroup per sequence, which sets the length as well; otherwise the lengths need a launch behind this one
   const bool one = (int64_t)most * w.per_row <= kMostWords;
-  const int rows = one ? std::max(most, 1) : rows_per_workgroup(w, 1024);
+  const int rows = one ? std::max(most, 1) : rows_per_workgroup(w, 512);
   const dim3 grid(one ? 1u : (unsigned)(((int64_t)most + rows - 1) / rows), batch);
   if (grid.x >= (1u << 24)) return GTA_ERR_UNSUPPORTED;   // launch size
   auto run = [&](auto t) {
@@ -242,7 +237,7 @@ int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t
 
 int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const int32_t *cu_rows, int batch, int max_rows,
                    void *k_out, void *c_out, hipStream_t st) {
-  const Words w = words_of(d);
+  const Words w = words_of(d, 8);
   const int rows = rows_per_workgroup(w, 1024);
   const dim3 grid((unsigned)(((int64_t)max_rows + rows - 1) / rows), batch);
   if (grid.x == 0) return GTA_OK;
@@ -251,11 +246,9 @@ int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const 
     using T = decltype(t);
     mx_read_kernel<T, decltype(nt)::value><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (T *)k_out, (T *)c_out);
   };
-  if (stream_past_caches((int64_t)batch * max_rows * (d.wk_w + d.wc_w) * d.esize())) {
-    if (d.dtype == GTA_BF16) run(__bf16{}, std::true_type{}); else run(float{}, std::true_type{});
-  } else {
-    if (d.dtype == GTA_BF16) run(__bf16{}, std::false_type{}); else run(float{}, std::false_type{});
-  }
+  if (d.dtype != GTA_BF16) run(float{}, std::false_type{});
+  else if (stream_past_caches((int64_t)batch * max_rows * (d.wk_w + d.wc_w) * 2)) run(__bf16{}, std::true_type{});
+  else run(__bf16{}, std::false_type{});
   return check_launch();
 }
 

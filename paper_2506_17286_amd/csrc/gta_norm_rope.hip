@@ -140,7 +140,7 @@ static void launch_vector(const NormRopeArgs &a, hipStream_t st) {
   };
   // few tokens: a head to every group of lanes, so that its load is the only one waited for
   if (a.total * heads * LANES < (1 << 17)) run(std::integral_constant<int, 1>{}, std::false_type{});
-  else if (stream_past_caches(a.total * heads * a.dh * (int64_t)sizeof(T))) run(std::integral_constant<int, 4>{}, std::true_type{});
+  else if (sizeof(T) == 2 && stream_past_caches(a.total * heads * a.dh * 2)) run(std::integral_constant<int, 4>{}, std::bool_constant<sizeof(T) == 2>{});
   else run(std::integral_constant<int, 4>{}, std::false_type{});
 }
 
