@@ -30,23 +30,12 @@ inline MxView mx_view_of(const gta_mx_cache &c, const int32_t *slots) {
 // whoever reads them next, in the same time.
 inline bool stream_past_caches(int64_t bytes) { return bytes > (32 << 20); }
 
-typedef __attribute__((ext_vector_type(4))) float mx_f32x4;
-typedef __attribute__((ext_vector_type(8))) float mx_f32x8;
-typedef __attribute__((ext_vector_type(8))) __bf16 mx_bf16x8;
-
-// eight elements on 16 bytes
+// 16 bytes
 template <bool NT, typename V>
 __device__ __forceinline__ void store16(V *p, const V &v) {
+  static_assert(sizeof(V) == 16, "one word");
   if constexpr (NT) __builtin_nontemporal_store(v, p);
   else *p = v;
-}
-template <bool NT>
-__device__ __forceinline__ void store8(__bf16 *p, const mx_f32x8 &v) { store16<NT>(reinterpret_cast<mx_bf16x8 *>(p), __builtin_convertvector(v, mx_bf16x8)); }
-template <bool NT>
-__device__ __forceinline__ void store8(float *p, const mx_f32x8 &v) {
-  static_assert(!NT, "two words a thread");
-  store16<false>(reinterpret_cast<mx_f32x4 *>(p), __builtin_shufflevector(v, v, 0, 1, 2, 3));
-  store16<false>(reinterpret_cast<mx_f32x4 *>(p + 4), __builtin_shufflevector(v, v, 4, 5, 6, 7));
 }
 
 // 2^e of a scale byte

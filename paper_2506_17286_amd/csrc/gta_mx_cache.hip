@@ -37,7 +37,7 @@ __device__ __forceinline__ f32x8 load8(const __bf16 *p) {
 }
 
 // A workgroup's rows as words of ELEMS elements, keys first: `per_row` of them a row, and an inverse of it for divisions (exact for
-// the numbers that come up: below 2^12, or below per_row <= 2^15).
+// the numbers that come up: below 2^12, or below per_row <= 2^16).
 struct Words {
   int kw, cw, per_row;
   unsigned inverse;
@@ -150,10 +150,10 @@ __global__ __launch_bounds__(256) void mx_append_commit_kernel(MxView cv, const 
   else cv.seq_lens[a.slot] = a.p + a.n;
 }
 
-// Eight elements a thread: one 16-byte word of bf16 to store, next to its neighbours'.  Stores past the caches want that: with two
-// words a thread, 32 bytes apart, they take twice as long (41 000 rows 25 us against 46), and fp32, which has two, goes through
-// the caches (16 400 rows 17 us against 26).  Two words of codes on their way per thread.
+// A thread has the elements of one 16-byte word to store, next to its neighbours': stores past the caches want that (with two words
+// a thread, 32 bytes apart, 41 000 rows took 46 us against 25).  Two words of codes on their way per thread.
 constexpr int kAtOnce = 2;
+template <typename T> constexpr int kReadElems = 16 / (int)sizeof(T);
 
 template <typename T, bool NT>
 __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *first, const int32_t *cu_rows, Words w, int max_rows,
@@ -168,19 +168,28 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
   const int j0 = blockIdx.x * rows_per_wg, words = min(n - j0, rows_per_wg) * w.per_row;
   const int have = slot_ok ? min(cv.seq_lens[slot], cv.max_seq) : 0;
   const int64_t row0 = (int64_t)(first ? first[b] : 0) + j0, dst0 = (int64_t)cu_rows[b] + j0;
+  constexpr int E = kReadElems<T>;
   for (int i0 = threadIdx.x; i0 < words; i0 += 256 * kAtOnce) {
-    u32x2 codes[kAtOnce];
+    unsigned codes[kAtOnce][E / 4];
     float scale[kAtOnce];
 #pragma unroll
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = i0 + 256 * u;
       if (i >= words) break;
-      const Place p = place_of<8>(w, i);
+      const Place p = place_of<E>(w, i);
       const int64_t row = row0 + p.row, src = row >= 0 && row < have ? cache_row(cv.pm, cv.max_seq, slot, (int)row) : -1;
-      codes[u] = u32x2{0u, 0u};   // rows that are not there read as zeros
+#pragma unroll
+      for (int h = 0; h < E / 4; ++h) codes[u][h] = 0u;   // rows that are not there read as zeros
       scale[u] = 0.f;
       if (src >= 0) {
-        codes[u] = *reinterpret_cast<const u32x2 *>((p.key ? cv.k : cv.c) + src * p.width + p.at);
+        const uint8_t *at = (p.key ? cv.k : cv.c) + src * p.width + p.at;
+        if constexpr (E == 8) {
+          const u32x2 c = *reinterpret_cast<const u32x2 *>(at);
+          codes[u][0] = c.x;
+          codes[u][1] = c.y;
+        } else {
+          codes[u][0] = *reinterpret_cast<const unsigned *>(at);
+        }
         scale[u] = mx_scale((p.key ? cv.ks : cv.cs)[src * (p.width / kMxBlock) + p.at / kMxBlock]);
       }
     }
@@ -188,14 +197,16 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
     for (int u = 0; u < kAtOnce; ++u) {
       const int i = i0 + 256 * u;
       if (i >= words) break;
-      const Place p = place_of<8>(w, i);
-      f32x8 v;
+      const Place p = place_of<E>(w, i);
+      typedef __attribute__((ext_vector_type(E))) float Vf;
+      typedef __attribute__((ext_vector_type(E))) T Vt;
+      Vf v;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < E / 4; ++h) {
         const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)codes[u][h], true);
         v[4 * h] = lo[0] * scale[u]; v[4 * h + 1] = lo[1] * scale[u]; v[4 * h + 2] = hi[0] * scale[u]; v[4 * h + 3] = hi[1] * scale[u];
       }
-      store8<NT>((p.key ? k_out : c_out) + (dst0 + p.row) * p.width + p.at, v);
+      store16<NT>(reinterpret_cast<Vt *>((p.key ? k_out : c_out) + (dst0 + p.row) * p.width + p.at), __builtin_convertvector(v, Vt));
     }
   }
 }
@@ -237,7 +248,7 @@ int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t
 
 int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const int32_t *cu_rows, int batch, int max_rows,
                    void *k_out, void *c_out, hipStream_t st) {
-  const Words w = words_of(d, 8);
+  const Words w = words_of(d, d.dtype == GTA_BF16 ? kReadElems<__bf16> : kReadElems<float>);
   const int rows = rows_per_workgroup(w, 1024);
   const dim3 grid((unsigned)(((int64_t)max_rows + rows - 1) / rows), batch);
   if (grid.x == 0) return GTA_OK;
@@ -246,9 +257,11 @@ int launch_mx_read(const Dims &d, const MxView &cv, const int32_t *first, const 
     using T = decltype(t);
     mx_read_kernel<T, decltype(nt)::value><<<grid, 256, 0, st>>>(cv, first, cu_rows, w, max_rows, rows, (T *)k_out, (T *)c_out);
   };
-  if (d.dtype != GTA_BF16) run(float{}, std::false_type{});
-  else if (stream_past_caches((int64_t)batch * max_rows * (d.wk_w + d.wc_w) * 2)) run(__bf16{}, std::true_type{});
-  else run(__bf16{}, std::false_type{});
+  if (stream_past_caches((int64_t)batch * max_rows * (d.wk_w + d.wc_w) * d.esize())) {
+    if (d.dtype == GTA_BF16) run(__bf16{}, std::true_type{}); else run(float{}, std::true_type{});
+  } else {
+    if (d.dtype == GTA_BF16) run(__bf16{}, std::false_type{}); else run(float{}, std::false_type{});
+  }
   return check_launch();
 }
 

@@ -69,6 +69,15 @@ __device__ __forceinline__ f32x8 load8(const float *p) {
   return __builtin_shufflevector(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+template <bool NT>
+__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { store16<NT>(reinterpret_cast<bf16x8 *>(p), __builtin_convertvector(v, bf16x8)); }
+template <bool NT>
+__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
+  static_assert(!NT, "two words a thread");
+  *reinterpret_cast<f32x4 *>(p) = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+  *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+}
+
 struct Turns { uint64_t t[128]; };   // what one position turns pair j < d_h/2 by from the host
 
 // Heads of 16 * LANES elements, rows and rows' starts in whole 16 bytes.  A lane has eight elements j.. and their partners
