@@ -422,7 +422,10 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   auto buffer = [&](const uint8_t *pool, const At &at, int hf, int width, int skip) {
     return __builtin_amdgcn_make_buffer_rsrc((void *)(pool + at.row[hf] * width + skip), 0, max(at.rows[hf] * width - skip, 0), 0x00020000);
   };
-  constexpr int kNt = 2;   // streamed: not kept in the caches
+  // Latents are streamed past the caches; keys and scale bytes are not, whose lines are asked for more than once (64 bytes of a
+  // row's 128 at a time, one scale byte per lane).  All streamed: 32 x 16384 rows of 2112 bytes 217 us against 191, 64 x 8192 of
+  // 1056 95 against 92; none: 207 and 101.
+  constexpr int kPast = 2;
   auto my_half = [&](const At &at, int kh) {   // of the rows that this wave scores
     if constexpr (WPT == 1) return at;
     At r;
@@ -436,15 +439,15 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       const auto r = buffer(a.cv.ks, my_half(at, hf), hf, KB / 32, 0);
 #pragma unroll
       for (int i = 0; i < KW; ++i) {
-        if constexpr (KB >= 128) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(r, ksoff + i * 4, 0, kNt);
-        else ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b16(r, ksoff, 0, kNt);
+        if constexpr (KB >= 128) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(r, ksoff + i * 4, 0, 0);
+        else ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b16(r, ksoff, 0, 0);
       }
     }
   };
   auto load_keys = [&](const At &at, int p) {
 #pragma unroll
     for (int hf = 0; hf < KH; ++hf)
-      kb[hf][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer(a.cv.k, my_half(at, hf), hf, KB, 0), koff + p * 64, 0, kNt));
+      kb[hf][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer(a.cv.k, my_half(at, hf), hf, KB, 0), koff + p * 64, 0, 0));
   };
   auto load_latents = [&](const At &at, int c) {
 #pragma unroll
@@ -452,9 +455,9 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       const auto r = buffer(a.cv.c, at, hf, a.cw, col0), rs = buffer(a.cv.cs, at, hf, a.cw / 32, col0 / 32);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (LC == 16) cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b128(r, coff[j] + c * 256, 0, kNt));
-        else cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b64(r, coff[j] + c * 128, 0, kNt));
-        cs[hf][j][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, csoff[j] + c * LC / 2, 0, kNt);
+        if constexpr (LC == 16) cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b128(r, coff[j] + c * 256, 0, kPast));
+        else cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b64(r, coff[j] + c * 128, 0, kPast));
+        cs[hf][j][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, csoff[j] + c * LC / 2, 0, 0);
       }
     }
   };
@@ -632,7 +635,6 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
             d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{op[e][0], op[e][1], op[e][2], op[e][3]}),
                                                         __builtin_bit_cast(bf16x8, u32x4{pp[i][0], pp[i][1], pp[i][2], pp[i][3]}), d, 0, 0, 0);
           }
-        __builtin_amdgcn_sched_barrier(0);
       }
       load_latents(nxt, c);
       __builtin_amdgcn_sched_barrier(0);
