@@ -279,9 +279,15 @@ GTA_API int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, 
 /* Attention of one new token per sequence over the seq_lens[slot] rows in an 8-bit cache (its own row
  * appended before): l_out[b, g*d_l : (g+1)*d_l] = sum_t Softmax_t(q_g . k_{k(g)}[t] * scale) c_{c(g)}[t].
  *   q [batch, n_q*d_h] rotated queries, l_out [batch, n_q*d_l]; device, element type = cfg->dtype
- *   num_splits  context splits per sequence; 0 = library's choice;  workspace: mode MX_DECODE
- * Sums and softmax statistics are fp32.  A sequence without rows, or with a slot out of range, gets zeros.
- * l_out goes on into gta_prefill_decoder.  head_dim up to 1024 and latent_dim up to 4096. */
+ *   num_splits  context splits per sequence (fewer of short ones; batches of more than 1024 sequences may go
+ *               unsplit); 0 = library's choice, which shares a batch's rows out evenly
+ *   workspace   mode MX_DECODE
+ * Sums and softmax statistics are fp32; weights are relative to one score of a few hundred rows and may be
+ * up to 2^40, so that latents beyond 2^80 can overflow.  A sequence without rows, or with a slot out of
+ * range, gets zeros.  l_out goes on into gta_prefill_decoder.  head_dim up to 1024, latent_dim up to 4096,
+ * max_seq up to 2^30, batch * max_seq below 2^36 for batches of up to 1024 (GTA_ERR_UNSUPPORTED).
+ * Runs on the matrix-instruction kernel where gta_uses_tuned_kernels(cfg, GTA_MODE_MX_DECODE) is 1 and
+ * pages, if any, are of a power of two of at least 16 rows; otherwise on a general one, 3 to 8 times slower. */
 GTA_API int gta_mx_decode_attention(const gta_config *cfg, const void *q, const gta_mx_cache *cache, const int32_t *slots,
                                     int32_t batch, int32_t num_splits, void *l_out, void *workspace,
                                     size_t workspace_bytes, void *hip_stream);
@@ -372,7 +378,10 @@ GTA_API const char *gta_strerror(int code);
  * {6,10}.  fp32 configurations answer 0; stage by stage they run on fp32 MFMA kernels where the shape
  * allows (widths in units of 64, heads of at most 64; attention: heads of 32, 64 or 128, latents in units
  * of 64; decode: one key of 64 and one latent of 128 for at most 16 maps, rope_base at least 1).  With
- * GTA_DEBUG set in the environment a bf16 call that takes the generic kernels says so on stderr. */
+ * GTA_DEBUG set in the environment a bf16 call that takes the generic kernels says so on stderr.
+ * GTA_MODE_MX_DECODE (either dtype): at most 16 maps, heads a multiple of 64, and key rows of 64 or 128 elements
+ * with latent rows of 128, 256 or 512, of 256 with 256, 512 or 1024, of 512 with 512 or 1024, of 1024 with 1024
+ * (longer latent rows in slices of 1024 or 512); GTA_ERR_UNSUPPORTED where the widths are refused. */
 GTA_API int gta_uses_tuned_kernels(const gta_config *cfg, int mode);
 
 #ifdef __cplusplus

@@ -274,6 +274,7 @@ int gta_uses_tuned_kernels(const gta_config *cfg, int mode) {
   if (mode == GTA_MODE_PREFILL) return tuned_prefill_supported(d) ? 1 : 0;
   if (mode == GTA_MODE_DECODE) return tuned_decode_supported(d) ? 1 : 0;
   if (mode == GTA_MODE_PREFILL_CHUNK) return tuned_prefill_chunk_supported(d, 1) ? 1 : 0;   // up to the cache-size limit
+  if (mode == GTA_MODE_MX_DECODE) return !mx_decode_dims_ok(d) ? GTA_ERR_UNSUPPORTED : mx_decode_tuned(d) ? 1 : 0;   // up to the page size
   return GTA_ERR_DTYPE;
 }
 

@@ -10,13 +10,11 @@ namespace gta {
 namespace {
 
 typedef __attribute__((ext_vector_type(2))) float f32x2;
-
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(4))) short s16x4;
 
 struct MxAttnArgs {
   const void *q;
@@ -32,13 +30,6 @@ struct MxAttnArgs {
 __device__ __forceinline__ int mx_rows(const MxView &cv, int b, int &slot) {
   slot = cv.slots ? cv.slots[b] : b;
   return slot >= 0 && slot < cv.max_batch ? min(max(cv.seq_lens[slot], 0), cv.max_seq) : 0;
-}
-
-// rows [j0, j1) of split s of n rows, in units of `unit` rows
-__device__ __forceinline__ void mx_slice(int n, int s, int splits, int unit, int &j0, int &j1) {
-  const int64_t units = (n + unit - 1) / unit;
-  j0 = (int)min((int64_t)n, units * s / splits * unit);
-  j1 = (int)min((int64_t)n, units * (s + 1) / splits * unit);
 }
 
 __device__ __forceinline__ float to_f(float v) { return v; }
@@ -58,7 +49,8 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
   const int s = blockIdx.x, g = blockIdx.y, b = blockIdx.z, tid = threadIdx.x;
   int slot, j0, j1;
   const int n = mx_rows(a.cv, b, slot);
-  mx_slice(n, s, a.splits, 1, j0, j1);
+  j0 = (int)((int64_t)n * s / a.splits);
+  j1 = (int)((int64_t)n * (s + 1) / a.splits);
   const int kcol = g / a.qpk * a.dh, ccol = g / a.qpc * a.dl, nb = a.dh / kMxBlock;
   for (int i = tid; i < a.dh; i += 256) qs[i] = to_f(((const T *)a.q)[((int64_t)b * a.nq + g) * a.dh + i]);
   const int quads = a.dl / 4, lanes = min(quads, 256), groups = 256 / lanes;   // row groups where there are few latents
@@ -887,6 +879,8 @@ static void launch_decode(const Dims &d, const MxAttnArgs &a, bool tuned, int pi
 int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int requested, void *ws, size_t ws_bytes, void *l_out,
                      hipStream_t st) {
   const bool tuned = mx_decode_tuned(d) && mx_layout_tuned(cv);
+  // row numbers and their sums over a batch that is cut stay well inside 32 bits
+  if (cv.max_seq > (1 << 30) || (batch <= kShareBatch && (int64_t)batch * cv.max_seq >= ((int64_t)1 << 36))) return GTA_ERR_UNSUPPORTED;
   const size_t head = tuned ? prefix_bytes(batch) : 0;
   const int64_t fit = ws_bytes > head ? (int64_t)((ws_bytes - head) / piece_bytes(d)) : 0;
   int share = 0, splits = 0;

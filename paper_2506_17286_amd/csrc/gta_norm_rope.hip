@@ -35,28 +35,28 @@ __device__ __forceinline__ float wave_sum(float v) {
 template <typename T>
 __global__ __launch_bounds__(256) void norm_rope_any_kernel(NormRopeArgs a) {
   const int heads = a.nq + a.nk, lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (item >= a.total * heads) return;
-  const int64_t t = item / heads;
-  const int h = (int)(item % heads);
-  const bool is_q = h < a.nq;
-  const T *x = is_q ? (const T *)a.q + t * a.q_stride + (int64_t)h * a.dh : (const T *)a.k + t * a.k_stride + (int64_t)(h - a.nq) * a.dh;
-  T *y = is_q ? (T *)a.q_out + (t * a.nq + h) * a.dh : (T *)a.k_out + (t * a.nk + h - a.nq) * a.dh;
-  const T *gain = (const T *)(is_q ? a.q_gain : a.k_gain);
-  float ss = 0.f;
-  for (int j = lane; j < a.dh; j += 64) { const float v = to_f(x[j]); ss = fmaf(v, v, ss); }
-  const float r = rsqrtf(wave_sum(ss) / (float)a.dh + a.eps);
-  auto normed = [&](int j) { return to_f(x[j]) * r * (gain ? to_f(gain[j]) : 1.f); };
-  if (!a.rope) {
-    for (int j = lane; j < a.dh; j += 64) y[j] = (T)normed(j);
-    return;
-  }
-  const int half = a.dh / 2, p = a.positions ? a.positions[t] : (int)t;
-  for (int j = lane; j < half; j += 64) {
-    const float lo = normed(j), hi = normed(j + half);
-    const float2 cs = rope_cos_sin_any(p, pow(a.base, -2.0 * j / a.dh));
-    y[j] = (T)(lo * cs.x - hi * cs.y);
-    y[j + half] = (T)(hi * cs.x + lo * cs.y);
+  for (int64_t item = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); item < a.total * heads; item += (int64_t)gridDim.x * 4) {
+    const int64_t t = item / heads;
+    const int h = (int)(item % heads);
+    const bool is_q = h < a.nq;
+    const T *x = is_q ? (const T *)a.q + t * a.q_stride + (int64_t)h * a.dh : (const T *)a.k + t * a.k_stride + (int64_t)(h - a.nq) * a.dh;
+    T *y = is_q ? (T *)a.q_out + (t * a.nq + h) * a.dh : (T *)a.k_out + (t * a.nk + h - a.nq) * a.dh;
+    const T *gain = (const T *)(is_q ? a.q_gain : a.k_gain);
+    float ss = 0.f;
+    for (int j = lane; j < a.dh; j += 64) { const float v = to_f(x[j]); ss = fmaf(v, v, ss); }
+    const float r = rsqrtf(wave_sum(ss) / (float)a.dh + a.eps);
+    auto normed = [&](int j) { return to_f(x[j]) * r * (gain ? to_f(gain[j]) : 1.f); };
+    if (!a.rope) {
+      for (int j = lane; j < a.dh; j += 64) y[j] = (T)normed(j);
+      continue;
+    }
+    const int half = a.dh / 2, p = a.positions ? a.positions[t] : (int)t;
+    for (int j = lane; j < half; j += 64) {
+      const float lo = normed(j), hi = normed(j + half);
+      const float2 cs = rope_cos_sin_any(p, pow(a.base, -2.0 * j / a.dh));
+      y[j] = (T)(lo * cs.x - hi * cs.y);
+      y[j + half] = (T)(hi * cs.x + lo * cs.y);
+    }
   }
 }
 
@@ -175,7 +175,7 @@ int launch_qk_norm_rope(const Dims &d, const void *q, int64_t q_stride, const vo
                        d.rope_base};
   if (d.dtype == GTA_BF16 ? try_vector<__bf16>(a, st) : try_vector<float>(a, st)) return check_launch();
   const int64_t items = total * (d.nq + d.nk);
-  const dim3 grid((unsigned)((items + 3) / 4));
+  const dim3 grid((unsigned)std::min<int64_t>((items + 3) / 4, 1 << 20));
   if (d.dtype == GTA_BF16) norm_rope_any_kernel<__bf16><<<grid, 256, 0, st>>>(a);
   else norm_rope_any_kernel<float><<<grid, 256, 0, st>>>(a);
   return check_launch();

@@ -126,3 +126,8 @@ def test_many_tokens_across_2_31_elements():
         B.gta_qk_norm_rope(cfg, src, st, src[:, 5 * dh:], st, None, None, 1e-6, None, tokens, qo, ko)
         outs += [qo, ko]
     assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+
+
+def test_more_rows_than_a_launch_has_workgroups():
+    """4.5 million heads off the vector kernel's grid: workgroups go on to further ones."""
+    run(M.shape(2, 1, 1, 6, 32), "f32", 1_500_000, None, rope=True, base=500000.0)

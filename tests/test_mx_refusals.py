@@ -133,3 +133,21 @@ def test_norm_arguments():
 def test_struct_layout():
     assert ctypes.sizeof(B.gta_mx_cache) == 6 * 8 + 2 * 4 + 8 + 3 * 4 + 4
     assert B.gta_mx_cache.block_table.offset == 56 and B.gta_mx_cache.num_pages.offset == 72
+
+
+@pytest.mark.parametrize("dims,answer", [
+    ((4, 4, 1, 128, 512), 1), ((8, 8, 1, 128, 1024), 1), ((5, 1, 1, 64, 128), 1), ((10, 1, 2, 64, 128), 1), ((4, 4, 4, 128, 512), 1),
+    ((2, 1, 1, 256, 256), 1), ((2, 2, 1, 32, 64), 0), ((20, 20, 20, 64, 64), 0), ((6, 3, 2, 96, 160), 0), ((32, 1, 1, 64, 128), 0),
+    ((2, 1, 1, 48, 128), B.GTA_ERR_UNSUPPORTED), ((1, 1, 1, 2048, 2048), B.GTA_ERR_UNSUPPORTED)])
+def test_which_kernel(dims, answer):
+    nq, nk, nc, dh, dl = dims
+    for dtype in ("bf16", "f32"):
+        cfg = _cfg(n_heads=nq, n_qgroups=nq, n_kgroups=nk, n_cgroups=nc, head_dim=dh, latent_dim=dl, dtype=dtype)
+        assert B.gta_uses_tuned_kernels(cfg, B.GTA_MODE_MX_DECODE) == answer
+
+
+def test_slots_of_more_rows_than_row_numbers_take():
+    table = dict(block_table=FAKE, page_size=1 << 15, num_pages=1 << 20)
+    for seq, batch in (((1 << 31) - (1 << 15), 1), (1 << 30, 64), (1 << 27, 512)):
+        cache = _cache(max_seq=seq, pages_per_slot=seq >> 15, max_batch=1024, **table)
+        assert _attend(_cfg(), cache, batch=batch, size=1 << 40) == B.GTA_ERR_UNSUPPORTED
