@@ -116,7 +116,7 @@ __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_ne
   const AppendPlan a = append_plan(cv, cu_new, b, max_new);
   if (a.slot < 0) return;
   if (a.n <= max_new && !a.full) {
-    const int j0 = blockIdx.x * rows_per_wg, words = min(a.n - j0, rows_per_wg) * w.per_row;
+    const int j0 = blockIdx.x * rows_per_wg, words = min(max(a.n - j0, 0), rows_per_wg) * w.per_row;   // (behind the last row: 0, no product that wraps)
     const int64_t src0 = (int64_t)cu_new[b] + j0;
     for (int i = threadIdx.x; i < words; i += 256) {
       const Place p = place_of<16>(w, i);
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(256) void mx_read_kernel(MxView cv, const int32_t *
     if (slot_ok && blockIdx.x == 0 && threadIdx.x == 0) cv.status[slot] = GTA_ERR_SHAPE;
     return;
   }
-  const int j0 = blockIdx.x * rows_per_wg, words = min(n - j0, rows_per_wg) * w.per_row;
+  const int j0 = blockIdx.x * rows_per_wg, words = min(max(max(n, 0) - j0, 0), rows_per_wg) * w.per_row;
   const int have = slot_ok ? min(cv.seq_lens[slot], cv.max_seq) : 0;
   const int64_t row0 = (int64_t)(first ? first[b] : 0) + j0, dst0 = (int64_t)cu_rows[b] + j0;
   constexpr int E = kReadElems<T>;

@@ -203,3 +203,30 @@ def test_rows_behind_4_gib():
         q, s = M.quantise(src.double().cpu().numpy())
         np.testing.assert_array_equal(out.double().cpu().numpy(), q * np.repeat(2.0 ** (s.astype(float) - 127), 32, axis=1))
         assert codes[pages - 1].any() and codes[3].any() and not codes[pages - 2].any() and not codes[0].any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bounds_far_above_the_rows_there_are(dtype):
+    """max_new and max_rows of 2^24 and more rows of 2048 elements: launches whose last workgroups begin 2^31 words and more behind
+    the sequence's end, in a slot of 2^25 rows of which two pages are there."""
+    sh = M.SHAPES["wide"]
+    cache = M.MxCache(sh, 1, 2048, 1024)
+    table = torch.full((1, 1 << 15), -1, dtype=torch.int32, device="cuda")
+    table[:, :2] = cache.table
+    cache.struct = B.make_paged_mx_cache(cache.k, cache.c, cache.ks, cache.cs, cache.seq_lens, cache.status, table)
+    cache.seq_lens.fill_(1020)
+    rng = np.random.default_rng(3)
+    want = numbers(cache)
+    xk, xc = append(cache, sh, dtype, rng.standard_normal((9, cache.kw)), rng.standard_normal((9, cache.cw)), [0, 9], max_new=(1 << 25) - 1)
+    expect(want, cache, 0, 1020, xk, xc)
+    same(cache, want, cache.rows(0, 1020, 1029))
+    assert cache.seq_lens.tolist() == [1029] and cache.status.tolist() == [0]
+    host = cache.host()
+    cfg, dt, at = B.make_config(dtype=dtype, **sh), M.DT[dtype], cache.rows(0, 1021, 1029)
+    k, c = (torch.full((12, w), 9.0, dtype=dt, device="cuda") for w in (cache.kw, cache.cw))
+    B.gta_mx_cache_read(cfg, cache.struct, None, torch.tensor([1021], dtype=torch.int32, device="cuda"),
+                        torch.tensor([0, 10], dtype=torch.int32, device="cuda"), 1, (1 << 24) + 16, k, c)
+    for out, i in ((k, 0), (c, 1)):
+        got = out.double().cpu().numpy()
+        np.testing.assert_array_equal(got[:8], M.values(host[i][at], host[i + 2][at]))
+        assert (got[8:10] == 0).all() and (got[10:] == 9.0).all()
