@@ -313,8 +313,9 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   typedef typename Word<LC>::type CWord;
   __shared__ std::conditional_t<SHARED, Cut, int> cut;
   __shared__ float sm[NS][16], sl[NS][16];
-  __shared__ f32x4 handed[WPT > 1 ? 2 : 1][NS][2][WPT > 1 ? 64 : 1];
-  extern __shared__ char lds[];
+  typedef f32x4 Handed[NS][2][64];
+  extern __shared__ __attribute__((aligned(16))) char lds[];   // the queries and, behind them, the scores that pairs of waves hand over; then the waves' sums
+  Handed *const handed = reinterpret_cast<Handed *>(lds + (QREG ? 0 : KB * NQP * 32));
   const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), stream = wave / WPT, role = wave % WPT;
   const int z = blockIdx.y;
@@ -823,8 +824,8 @@ static int64_t mx_most_pieces(int batch, int share, int requested) {
 
 static int mx_equal_splits(const Dims &d, int batch, int max_seq, int requested) {
   if (requested > 0) return std::min(requested, 1024);
-  const int want = (1024 + batch * d.nq - 1) / (batch * d.nq), cap = max_seq / 256;
-  return std::max(1, std::min(std::min(want, cap), 256));
+  const int64_t maps = (int64_t)batch * d.nq, want = (1024 + maps - 1) / maps;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, max_seq / 256), 256));
 }
 
 static size_t piece_bytes(const Dims &d) { return (size_t)d.nq * ((size_t)d.dl + 2) * 4; }
@@ -841,7 +842,8 @@ template <typename T, int KB, int CS>
 static void launch_tuned(const MxAttnArgs &a, int pieces, int z, hipStream_t st) {
   constexpr int WPT = CS >= 512 ? 2 : 1;
   constexpr int OCC = mx_occupancy(CS);
-  const int lds = std::max(KB * Parts<T>::Q * 32, 4 / WPT * a.nq * (CS + 16) * 4);   // the queries, then the waves' sums
+  const int handed = WPT > 1 ? 2 * 4 / WPT * 2 * 64 * 16 : 0;
+  const int lds = std::max(KB * Parts<T>::Q * 32 + handed, 4 / WPT * a.nq * (CS + 16) * 4);   // (16 maps, 512 columns: two workgroups per CU)
   if (pieces) {
     if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true>, lds);
     mx_attn_kernel<T, KB, CS, WPT, OCC, true><<<dim3(pieces, z), 256, lds, st>>>(a);
