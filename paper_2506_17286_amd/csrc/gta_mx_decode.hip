@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
   const int64_t at = ((int64_t)b * a.splits + s) * a.nq + g;   // every split writes, those without rows too
   float *out = a.pacc + at * a.dl;
   if (groups == 1) {
-    for (int v = 0; v * 256 + my < quads; ++v)
+    for (int v = 0; grp == 0 && v * 256 + my < quads; ++v)   // (threads over: 129 to 255 quads)
       for (int e = 0; e < 4; ++e) out[(v * 256 + my) * 4 + e] = acc[v][e];
   } else {
     for (int e = 0; e < 4; ++e) accs[tid * 4 + e] = acc[0][e];

@@ -69,6 +69,11 @@ SHAPES = {
     "c2": shape(8, 4, 2, 128, 512), "c4": shape(4, 4, 4, 128, 512), "wide": shape(8, 8, 1, 128, 1024),
     "q16": shape(16, 2, 1, 64, 256), "one": shape(1, 1, 1, 128, 128), "mha": shape(20, 20, 20, 64, 64),
     "odd": shape(6, 3, 2, 96, 160), "head256": shape(2, 1, 1, 256, 256),
+    # more maps than a matrix instruction has columns, heads and rows that fill no tile, blocks of maps that end inside a key head's or
+    # a latent's, latents in slices with a short last one
+    "one32": shape(1, 1, 1, 32, 96), "q32": shape(32, 1, 1, 64, 128), "q20": shape(20, 1, 1, 64, 320), "w640": shape(1, 1, 1, 64, 640),
+    "h32": shape(20, 4, 2, 32, 640), "q18": shape(18, 1, 1, 128, 512), "q17": shape(17, 1, 1, 96, 1280), "k5": shape(15, 5, 1, 64, 512),
+    "w672": shape(12, 3, 3, 64, 672), "h160": shape(24, 8, 2, 160, 544), "q40": shape(40, 8, 4, 128, 256), "h544": shape(2, 1, 1, 544, 544),
 }
 
 

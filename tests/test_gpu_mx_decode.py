@@ -64,7 +64,8 @@ def test_groupings_pages_and_lengths(name, page, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("name,page", [("1b", 64), ("paper", 0), ("wide", 16), ("gta4", 64), ("odd", 0), ("c4", 0), ("tiny", 16)])
+@pytest.mark.parametrize("name,page", [("1b", 64), ("paper", 0), ("wide", 16), ("gta4", 64), ("odd", 0), ("c4", 0), ("tiny", 16),
+                                       ("q17", 64), ("h160", 0), ("mha", 64), ("h544", 0), ("1b", 40)])
 def test_long_contexts_and_splits(name, page, dtype):
     sh = M.SHAPES[name]
     lens = [5000, 1, 2047, 4097]
@@ -78,7 +79,7 @@ def test_long_contexts_and_splits(name, page, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("name", ["1b", "paper", "odd"])
+@pytest.mark.parametrize("name", ["1b", "paper", "odd", "h544"])
 @pytest.mark.parametrize("how", ["climb", "fall", "jump", "flat", "zero"])
 def test_scores_that_move_far_along_the_rows(name, how, dtype):
     """The running maximum climbs, falls or jumps by hundreds (in units of the exponent); all keys alike; all keys zero."""
@@ -101,7 +102,7 @@ def test_scores_that_move_far_along_the_rows(name, how, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("name", ["1b", "q8k4", "wide", "odd", "mha", "c2"])
+@pytest.mark.parametrize("name", ["1b", "q8k4", "wide", "odd", "mha", "c2", "k5", "h32", "h160", "w672", "q40", "h544"])
 def test_nan_reaches_the_maps_that_read_it(name, dtype):
     """A NaN key code: every latent of the maps of that key, no other map.  A NaN latent code: that latent of its maps."""
     sh = M.SHAPES[name]
@@ -213,11 +214,27 @@ def test_same_results_from_run_to_run_and_in_any_order_of_the_batch(name):
         np.testing.assert_array_equal(got[b], attend(cache, sh, "bf16", q, 8, None, 4)[1])
 
 
-def test_large_batches():
+@pytest.mark.parametrize("name", ["paper", "h32", "q17"])
+def test_large_batches(name):
     """More sequences than fill the chip, of a row or two and of none."""
-    sh = M.SHAPES["paper"]
+    sh = M.SHAPES[name]
     lens = [i % 5 for i in range(3000)]
     cache = M.MxCache(sh, 3000, 16).fill(lens, np.random.default_rng(14))
     q = queries(sh, "bf16", 3000)
     got = attend(cache, sh, "bf16", q, 3000)
     check(got, cache, sh, "bf16", q, range(3000), lens)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", sorted(M.SHAPES))
+def test_batches_that_are_not_cut(name, dtype):
+    """A workgroup per sequence: more than 1024 of them, of no rows to a few tiles."""
+    sh = M.SHAPES[name]
+    lens = [(0, 1, 3, 2)[i % 4] for i in range(1026)]
+    for i, n in ((5, 70), (500, 33), (1025, 95)):
+        lens[i] = n
+    cache = M.MxCache(sh, 1026, 96, 32).fill(lens, np.random.default_rng(16))
+    q = queries(sh, dtype, 1026)
+    got = attend(cache, sh, dtype, q, 1026)
+    picked = [0, 1, 2, 3, 4, 5, 6, 499, 500, 501, 1022, 1023, 1024, 1025]
+    check(got[picked], cache, sh, dtype, q[picked], picked, lens)
