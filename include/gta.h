@@ -287,7 +287,8 @@ GTA_API int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, 
  * range, gets zeros.  l_out goes on into gta_prefill_decoder.  head_dim up to 1024, latent_dim up to 4096,
  * max_seq up to 2^30, batch * max_seq below 2^36 for batches of up to 1024 (GTA_ERR_UNSUPPORTED).
  * Runs on the matrix-instruction kernel where gta_uses_tuned_kernels(cfg, GTA_MODE_MX_DECODE) is 1 and
- * pages, if any, are of a power of two of at least 16 rows; otherwise on a general one, 3 to 8 times slower. */
+ * pages, if any, are of a power of two of at least 16 rows; otherwise on a general one, which reads a row
+ * once for every map (a few times slower for few maps, up to 40 times for many). */
 GTA_API int gta_mx_decode_attention(const gta_config *cfg, const void *q, const gta_mx_cache *cache, const int32_t *slots,
                                     int32_t batch, int32_t num_splits, void *l_out, void *workspace,
                                     size_t workspace_bytes, void *hip_stream);
@@ -379,9 +380,10 @@ GTA_API const char *gta_strerror(int code);
  * allows (widths in units of 64, heads of at most 64; attention: heads of 32, 64 or 128, latents in units
  * of 64; decode: one key of 64 and one latent of 128 for at most 16 maps, rope_base at least 1).  With
  * GTA_DEBUG set in the environment a bf16 call that takes the generic kernels says so on stderr.
- * GTA_MODE_MX_DECODE (either dtype): at most 16 maps, heads a multiple of 64, and key rows of 64 or 128 elements
- * with latent rows of 128, 256 or 512, of 256 with 256, 512 or 1024, of 512 with 512 or 1024, of 1024 with 1024
- * (longer latent rows in slices of 1024 or 512); GTA_ERR_UNSUPPORTED where the widths are refused. */
+ * GTA_MODE_MX_DECODE (either dtype): heads of up to 512; GTA_ERR_UNSUPPORTED where the widths are refused.  Rows are
+ * read once with at most 16 maps, heads a multiple of 64, and key rows of 64 or 128 elements with latent rows of
+ * 128, 256 or 512, of 256 with 256, 512 or 1024, of 512 with 512 or 1024, of 1024 with 1024; others run in blocks
+ * of maps that each read their key heads and latents, and wider latents in slices that each read the keys. */
 GTA_API int gta_uses_tuned_kernels(const gta_config *cfg, int mode);
 
 #ifdef __cplusplus

@@ -19,7 +19,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 struct MxAttnArgs {
   const void *q;
   MxView cv;
-  int nq, qpk, qpc, dh, dl, kw, cw, batch, splits, share, ps_shift;
+  int nq, qpk, qpc, dh, dl, kw, cw, batch, splits, share, ps_shift, maps;   // maps: of a workgroup
   float scale_log2e;
   float *pacc, *pml;   // [pieces, n_q, d_l], [pieces, n_q, 2]
   int32_t *prefix;     // [batch + 1] pieces in front of each sequence (matrix-instruction kernel)
@@ -37,7 +37,7 @@ __device__ __forceinline__ float to_f(__bf16 v) { return (float)v; }
 
 constexpr int kAnyMaxHead = 1024, kAnyMaxLatent = 4096;
 
-// Any widths and page sizes: a workgroup per (split, map, sequence), a row per thread for the scores, four latents per
+// Any page sizes, heads of more than 512: a workgroup per (split, map, sequence), a row per thread for the scores, four latents per
 // thread for the sums.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
@@ -302,12 +302,17 @@ __device__ __forceinline__ int cut_lanes(const MxView &cv, int batch, int per_ro
 // sums alone would fill the accumulation registers (rows of 2112 bytes: 95 us against 67 for 8 x 8000..32768); with 512 one wave
 // can do it, but twice the waves for half the registers fill and drain sooner (one sequence of 8192 rows 17.3 -> 15.4 us, 64
 // of them the same).
-template <typename T, int KB, int CS, int WPT, int OCC, bool SHARED>
+// EDGE: rows of other widths than KB and CS, more than 16 maps, heads that end inside a piece.  A workgroup then has a.maps maps
+// from g0 on and reads the columns of their key heads and latents (blockIdx.z: which maps, blockIdx.y: which CS of their latents);
+// a head begins a piece of its own, and lanes without columns ask for what lies behind the buffer, zeros that cost nothing.  (64 x
+// 8192 rows of 5 keys of 64 and 512 latents for 15 maps: 2215 us in mx_attn_any_kernel, 89 here; rows of the widths KB and CS go
+// without: one scale byte a load in place of four alone takes 182 us for 32 x 16384 of 1024 + 1024 to 207.)
+template <typename T, int KB, int CS, int WPT, int OCC, bool SHARED, bool EDGE>
 __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int NQP = Parts<T>::Q, NPP = Parts<T>::P;
   constexpr int HF = 2, KH = HF / WPT, KP = KB / 64;                     // half tiles, those this wave scores, key pieces
   constexpr int CW = CS / WPT, LC = CW >= 256 ? 16 : CW / 16, NCH = CW / (16 * LC);   // this wave's columns, bytes per lane and load, chunks
-  constexpr int KW = KB >= 128 ? KB / 128 : 1;                           // scale words of a key row: four bytes (two for one piece)
+  constexpr int KW = EDGE ? KP : KB >= 128 ? KB / 128 : 1;               // scale words of a key row: four bytes (two for one piece; EDGE: a byte each)
   constexpr int NS = 4 / WPT;                                            // tiles worked on at a time
   constexpr bool QREG = KB * NQP <= 192;
   typedef typename Word<LC>::type CWord;
@@ -319,6 +324,11 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), stream = wave / WPT, role = wave % WPT;
   const int z = blockIdx.y;
+  const int g0 = EDGE ? blockIdx.z * a.maps : 0, nq = EDGE ? min(a.maps, a.nq - g0) : a.nq;
+  const int kh0 = EDGE ? g0 / a.qpk : 0, kheads = EDGE ? (g0 + nq - 1) / a.qpk - kh0 + 1 : 0;
+  const int latent0 = EDGE ? g0 / a.qpc * a.dl : 0, latents = EDGE ? ((g0 + nq - 1) / a.qpc + 1) * a.dl - latent0 : 0;
+  if (EDGE && z * CS >= latents) return;   // (other maps have more of them)
+  const bool first_here = z == 0 && (!EDGE || blockIdx.z == 0);
 
   // ---- this workgroup's piece: rows [j0, j1) of sequence b
   int b = blockIdx.x, slot, j0 = 0, j1, n;
@@ -329,7 +339,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     if (a.batch <= 64) {
       int before, mine, rows;
       const int pieces = cut_lanes(a.cv, a.batch, kTile * NS, a.splits, a.share, before, mine, rows);
-      if (wg == 0 && z == 0 && wave == 0) {
+      if (wg == 0 && first_here && wave == 0) {
         if (lane < a.batch) a.prefix[lane + 1] = before + mine;
         if (lane == 0) a.prefix[0] = 0;
       }
@@ -340,7 +350,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       n = __builtin_amdgcn_readlane(rows, b);
     } else {
       const int pieces = cut_batch(a.cv, a.batch, kTile * NS, a.splits, a.share, cut);
-      if (wg == 0 && z == 0)
+      if (wg == 0 && first_here)
         for (int i = tid; i <= a.batch; i += 256) a.prefix[i] = cut.prefix[i];
       if (wg >= pieces) return;
       for (int i = tid; i < a.batch; i += 256)
@@ -360,14 +370,14 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     n = mx_rows(a.cv, b, slot);
     j1 = n;
     if (n == 0) {
-      for (int i = tid; i < a.nq * CS; i += 256) {
-        const int g = i / CS, col = z * CS + i % CS - g / a.qpc * a.dl;
+      for (int i = tid; i < nq * CS; i += 256) {
+        const int g = g0 + i / CS, col = latent0 + z * CS + i % CS - g / a.qpc * a.dl;
         if (col >= 0 && col < a.dl) ((T *)a.l_out)[((int64_t)b * a.nq + g) * a.dl + col] = (T)0.f;
       }
       return;
     }
   }
-  const int64_t part = (int64_t)blockIdx.x * a.nq;   // where a piece that is not the whole sequence goes
+  const int64_t part = (int64_t)blockIdx.x * a.nq + g0;   // where a piece that is not the whole sequence goes
   const int nt = (j1 - j0 + kTile - 1) / kTile;
 
   // Where the rows of tile t are: the pool row of the first row of each half, and how many rows the half has.  Page numbers are
@@ -404,8 +414,26 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   unsigned ks[KH][KW];
   CWord cb[HF][4][NCH];
   unsigned cs[HF][4][NCH];
-  const int col0 = z * CS + role * CW;
-  const unsigned koff = x * KB + h * 16, ksoff = x * (KB / 32);
+  const int col0 = latent0 + z * CS + role * CW, mine = EDGE ? latents - z * CS - role * CW : 0;   // columns of this wave
+  const int key0 = EDGE ? kh0 * a.dh : 0, kwidth = EDGE ? a.kw : KB;
+  const int ppk = (a.dh + 63) / 64;   // pieces of a key head
+  const unsigned koff = x * kwidth + h * 16, ksoff = x * (kwidth / 32) + (EDGE ? h >> 1 : 0);
+  // EDGE: column of a key piece in the row's window, and what to add to the offset of lanes that have none (of a piece of no head; in
+  // the second half of a head's last): beyond any buffer, whose 16 rows have at most 2^18 columns.
+  constexpr unsigned kNone = 0x40000000;
+  unsigned key_at[EDGE ? KP : 1], key_end[EDGE ? KP : 1], late = 0, none[EDGE ? NCH : 1];
+  if constexpr (EDGE) {
+    late = a.dh % 64 && h >= 2 ? kNone : 0;
+    int head = 0, piece = 0;
+#pragma unroll
+    for (int p = 0; p < KP; ++p) {
+      key_at[p] = head * a.dh + piece * 64;
+      key_end[p] = (head < kheads ? 0 : kNone) + (piece == ppk - 1 ? late : 0);
+      if (++piece == ppk) { piece = 0; ++head; }
+    }
+#pragma unroll
+    for (int c = 0; c < NCH; ++c) none[c] = c * 16 * LC + x * (int)LC >= mine ? kNone : 0;
+  }
   unsigned coff[4], csoff[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -429,10 +457,11 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   auto load_key_scales = [&](const At &at) {
 #pragma unroll
     for (int hf = 0; hf < KH; ++hf) {
-      const auto r = buffer(a.cv.ks, my_half(at, hf), hf, KB / 32, 0);
+      const auto r = buffer(a.cv.ks, my_half(at, hf), hf, kwidth / 32, key0 / 32);
 #pragma unroll
       for (int i = 0; i < KW; ++i) {
-        if constexpr (KB >= 128) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(r, ksoff + i * 4, 0, 0);
+        if constexpr (EDGE) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b8(r, ksoff + key_at[i] / 32 + key_end[i], 0, 0);
+        else if constexpr (KB >= 128) ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b32(r, ksoff + i * 4, 0, 0);
         else ks[hf][i] = __builtin_amdgcn_raw_buffer_load_b16(r, ksoff, 0, 0);
       }
     }
@@ -440,7 +469,8 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   auto load_keys = [&](const At &at, int p) {
 #pragma unroll
     for (int hf = 0; hf < KH; ++hf)
-      kb[hf][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer(a.cv.k, my_half(at, hf), hf, KB, 0), koff + p * 64, 0, 0));
+      kb[hf][p] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buffer(a.cv.k, my_half(at, hf), hf, kwidth, key0),
+                                                                                  EDGE ? koff + key_at[p] + key_end[p] : koff + p * 64, 0, 0));
   };
   auto load_latents = [&](const At &at, int c) {
 #pragma unroll
@@ -448,23 +478,23 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       const auto r = buffer(a.cv.c, at, hf, a.cw, col0), rs = buffer(a.cv.cs, at, hf, a.cw / 32, col0 / 32);
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if constexpr (LC == 16) cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b128(r, coff[j] + c * 256, 0, kPast));
-        else cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b64(r, coff[j] + c * 128, 0, kPast));
-        cs[hf][j][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, csoff[j] + c * LC / 2, 0, 0);
+        const unsigned o = coff[j] + c * 16 * LC + (EDGE ? none[c] : 0);
+        if constexpr (LC == 16) cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, kPast));
+        else cb[hf][j][c] = __builtin_bit_cast(CWord, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, kPast));
+        cs[hf][j][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, csoff[j] + c * LC / 2 + (EDGE ? none[c] : 0), 0, 0);
       }
     }
   };
 
   // the queries are asked for first, then the first tile's rows: these are on their way while the queries are laid out
-  const int ppk = a.dh / 64;   // pieces of a key head
-  const int kg = x < a.nq ? x / a.qpk : -1;
+  const int kg = x < nq ? (g0 + x) / a.qpk - kh0 : -1;
   typedef __attribute__((ext_vector_type(8))) T Eight;
   constexpr int QF = QREG ? KP * 2 : KP / 2;   // fragments this wave lays out: all of them, or every fourth
   Eight qv[QF];
 #pragma unroll
   for (int i = 0; i < QF; ++i) {   // second operand for half a piece: dimensions h * 16 + (f & 1) * 8 .. of the piece
-    const int f = QREG ? i : wave + 4 * i, p = f >> 1;
-    qv[i] = *reinterpret_cast<const Eight *>((const T *)a.q + ((int64_t)b * a.nq + (kg == p / ppk ? x : 0)) * a.dh + (p % ppk) * 64 + h * 16 + (f & 1) * 8);
+    const int f = QREG ? i : wave + 4 * i, p = f >> 1, d0 = p % ppk * 64 + h * 16;
+    qv[i] = *reinterpret_cast<const Eight *>((const T *)a.q + ((int64_t)b * a.nq + g0 + (kg == p / ppk ? x : 0)) * a.dh + (EDGE && d0 >= a.dh ? 0 : d0) + (f & 1) * 8);
   }
   At nxt{};
   auto start = [&]() {
@@ -489,7 +519,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 v[NQP];
-      split_parts<NQP>(kg == (f >> 1) / ppk ? to_f(qv[i][e]) : 0.f, v);
+      split_parts<NQP>(kg == (f >> 1) / ppk && (!EDGE || (f >> 1) % ppk * 64 + h * 16 < a.dh) ? to_f(qv[i][e]) : 0.f, v);
 #pragma unroll
       for (int j = 0; j < NQP; ++j) out[j][e] = v[j];
     }
@@ -513,7 +543,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 #pragma unroll
     for (int hf = 0; hf < KH; ++hf)
 #pragma unroll
-      for (int i = 0; i < KW; ++i) kscale[hf][i] = ks[hf][i] >> (8 * (h >> 1));
+      for (int i = 0; i < KW; ++i) kscale[hf][i] = EDGE ? ks[hf][i] : ks[hf][i] >> (8 * (h >> 1));
     load_key_scales(nxt);
     auto fragments = [&](int p, bf16x8 (&out)[2][NQP]) {
 #pragma unroll
@@ -525,11 +555,11 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
         }
     };
     auto take = [&](int p) {
-      const bool mine = kg == p / ppk;
+      const bool of_map = kg == p / ppk;
 #pragma unroll
       for (int hf = 0; hf < KH; ++hf)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[hf][i] += mine ? before[hf][i] : 0.f;
+        for (int i = 0; i < 4; ++i) sc[hf][i] += of_map ? before[hf][i] : 0.f;
     };
     bf16x8 qf[2][NQP], qn[2][NQP];
     fragments(0, qf);
@@ -543,8 +573,8 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       for (int half = 0; half < 2; ++half)
 #pragma unroll
         for (int hf = 0; hf < KH; ++hf) {
-          const unsigned w = kscale[hf][p / 2];
-          const float s = __uint_as_float((p & 1 ? w << 7 : w << 23) & 0x7f800000u);
+          const unsigned w = kscale[hf][EDGE ? p : p / 2];
+          const float s = __uint_as_float((!EDGE && p & 1 ? w << 7 : w << 23) & 0x7f800000u);
           const u32x4 k4 = {cvt_lo(kb[hf][p][2 * half], s), cvt_hi(kb[hf][p][2 * half], s), cvt_lo(kb[hf][p][2 * half + 1], s),
                             cvt_hi(kb[hf][p][2 * half + 1], s)};
 #pragma unroll
@@ -676,7 +706,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     for (int w = 0; w < NS; ++w) v += sl[w][g] * __builtin_amdgcn_exp2f(fmaxf(sm[w][g], kLowest) - fmaxf(mg, kLowest));
     return v;
   };
-  if (!whole && z == 0 && tid < a.nq) {
+  if (!whole && z == 0 && tid < nq) {
     float mg;
     const float lg = joined(tid, mg);
     a.pml[(part + tid) * 2] = mg;
@@ -686,8 +716,8 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   // padded, so that the lanes of a store meet different banks.
   constexpr int ROW = CS + 16;
   auto place = [](int col) { return col ^ (((col / (4 * LC)) & 3) * 4); };
-  if (x < a.nq) {
-    float *dst = buf + (stream * a.nq + x) * ROW;
+  if (x < nq) {
+    float *dst = buf + (stream * nq + x) * ROW;
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
 #pragma unroll
@@ -700,16 +730,16 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
       }
   }
   __syncthreads();
-  for (int i = tid; i < a.nq * (CS / 4); i += 256) {
-    const int g = i / (CS / 4), cc = i % (CS / 4) * 4, col = z * CS + cc - g / a.qpc * a.dl;   // latent of the map's group
+  for (int i = tid; i < nq * (CS / 4); i += 256) {
+    const int g = i / (CS / 4), cc = i % (CS / 4) * 4, col = latent0 + z * CS + cc - (g0 + g) / a.qpc * a.dl;   // latent of the map's group
     if (col < 0 || col >= a.dl) continue;
     f32x4 v = *reinterpret_cast<const f32x4 *>(buf + g * ROW + place(cc));
 #pragma unroll
-    for (int w = 1; w < NS; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * a.nq + g) * ROW + place(cc));
+    for (int w = 1; w < NS; ++w) v += *reinterpret_cast<const f32x4 *>(buf + (w * nq + g) * ROW + place(cc));
     if (whole) {
       float mg;
       const float lg = joined(g, mg);
-      T *o = (T *)a.l_out + ((int64_t)b * a.nq + g) * a.dl + col;
+      T *o = (T *)a.l_out + ((int64_t)b * a.nq + g0 + g) * a.dl + col;
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = (T)(v[e] / lg);
     } else {
@@ -790,20 +820,38 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxAttnArgs a) {
 
 bool mx_decode_dims_ok(const Dims &d) { return mx_widths_ok(d) && d.dh <= kAnyMaxHead && d.dl <= kAnyMaxLatent && d.nq <= 65535; }
 
-// Latent columns of a workgroup: the whole row where it has an instantiation, else slices of it.
-static int mx_slice_width(const Dims &d) {
-  for (int cs = 1024; cs >= 128; cs /= 2)
-    if (d.wc_w % cs == 0 && (d.wc_w == cs || cs >= 512)) return cs;
-  return 0;
+// How the matrix-instruction kernel takes a shape.  Rows of instantiated widths and up to 16 maps in whole pieces of 64 go in one, or
+// in slices of their latents.  Anything else (EDGE) is cut into blocks of up to 16 maps, each with the key heads and latents that it
+// reads, by the fewest columns in all, padding included.  No blocks: heads of more than 512.
+struct MxPlan { int kb, cs, maps, blocks, slices; bool edge; };
+
+static MxPlan mx_plan(const Dims &d) {
+  int cs = 1024;
+  while (cs >= 128 && !(d.wc_w % cs == 0 && (d.wc_w == cs || cs >= 512))) cs /= 2;
+  const int kb = d.wk_w;
+  if (d.dh % 64 == 0 && d.nq <= 16 && cs >= 128 &&
+      ((kb == 64 && cs <= 512) || (kb == 128 && cs <= 512) || (kb == 256 && cs >= 256) || (kb == 512 && cs >= 512) || (kb == 1024 && cs == 1024)))
+    return MxPlan{kb, cs, d.nq, 1, d.wc_w / cs, false};
+  const int ppk = (d.dh + 63) / 64;
+  auto heads = [](int maps, int per, int most) { return std::min(most, maps % per == 0 ? maps / per : per % maps == 0 ? 1 : (maps + per - 2) / per + 1); };
+  MxPlan best{};
+  int64_t least = INT64_MAX;
+  for (int m = std::min(d.nq, 16); m >= 1; --m) {
+    const int pieces = heads(m, d.qpk, d.nk) * ppk, wide = heads(m, d.qpc, d.nc) * d.dl;
+    if (pieces > 8) continue;   // (1024 columns of keys: 114 registers spilled)
+    MxPlan p{64, 0, m, (d.nq + m - 1) / m, 1, true};
+    while (p.kb < pieces * 64) p.kb *= 2;
+    p.cs = wide <= 128 && p.kb <= 128 ? 128 : wide <= 512 || (wide % 1024 && wide % 512 == 0) ? 512 : 1024;
+    p.slices = (wide + p.cs - 1) / p.cs;
+    const int64_t cost = (int64_t)p.blocks * p.slices * (p.kb + p.cs);
+    if (cost < least) { least = cost; best = p; }
+  }
+  return best;
 }
 
-// The matrix-instruction kernel takes heads of whole pieces of 64, up to 16 maps, and the rows that are instantiated.
-bool mx_decode_tuned(const Dims &d) {
-  const int cs = mx_slice_width(d), kb = d.wk_w;
-  if (d.dh % 64 || d.nq > 16 || cs == 0) return false;
-  return (kb == 64 && cs <= 512) || (kb == 128 && cs <= 512) || (kb == 256 && cs >= 256) || (kb == 512 && cs >= 512) || (kb == 1024 && cs == 1024);
-}
+bool mx_decode_tuned(const Dims &d) { return mx_plan(d).blocks > 0; }
 
+// Pages that the matrix-instruction kernel takes: a power of two of at least half a tile.
 static bool mx_layout_tuned(const MxView &cv) {
   return !cv.pm.table || (cv.pm.page_size >= 16 && (cv.pm.page_size & (cv.pm.page_size - 1)) == 0);
 }
@@ -812,10 +860,7 @@ static bool mx_layout_tuned(const MxView &cv) {
 constexpr int mx_occupancy(int cs) { return cs >= 1024 ? 1 : cs >= 256 ? 2 : 3; }
 
 // Workgroups that the chip holds at once.
-static int mx_share(const Dims &d) {
-  const int cs = mx_slice_width(d);
-  return std::max(2, 256 * mx_occupancy(cs) / (d.wc_w / cs));
-}
+static int mx_share(const MxPlan &p) { return std::max(2, 256 * mx_occupancy(p.cs) / (p.slices * p.blocks)); }
 
 // Most pieces of a batch (Cut).
 static int64_t mx_most_pieces(int batch, int share, int requested) {
@@ -834,53 +879,70 @@ static size_t prefix_bytes(int batch) { return batch <= kShareBatch ? align_up((
 size_t mx_decode_bytes(const Dims &d, int batch, int max_seq, int requested) {
   // the call picks the kernel by the page size too: enough for either
   size_t n = piece_bytes(d) * batch * mx_equal_splits(d, batch, max_seq, requested);
-  if (mx_decode_tuned(d) && batch <= kShareBatch) n = std::max(n, prefix_bytes(batch) + piece_bytes(d) * mx_most_pieces(batch, mx_share(d), requested));
+  const MxPlan p = mx_plan(d);
+  if (p.blocks && batch <= kShareBatch) n = std::max(n, prefix_bytes(batch) + piece_bytes(d) * mx_most_pieces(batch, mx_share(p), requested));
   return n;
 }
 
-template <typename T, int KB, int CS>
-static void launch_tuned(const MxAttnArgs &a, int pieces, int z, hipStream_t st) {
+template <typename T, int KB, int CS, bool EDGE>
+static void launch_tuned(const MxAttnArgs &a, const MxPlan &p, int pieces, hipStream_t st) {
   constexpr int WPT = CS >= 512 ? 2 : 1;
   constexpr int OCC = mx_occupancy(CS);
   const int handed = WPT > 1 ? 2 * 4 / WPT * 2 * 64 * 16 : 0;
-  const int lds = std::max(KB * Parts<T>::Q * 32 + handed, 4 / WPT * a.nq * (CS + 16) * 4);   // (16 maps, 512 columns: two workgroups per CU)
+  const int lds = std::max(KB * Parts<T>::Q * 32 + handed, 4 / WPT * p.maps * (CS + 16) * 4);   // (16 maps, 512 columns: two workgroups per CU)
   if (pieces) {
-    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true>, lds);
-    mx_attn_kernel<T, KB, CS, WPT, OCC, true><<<dim3(pieces, z), 256, lds, st>>>(a);
+    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, true, EDGE>, lds);
+    mx_attn_kernel<T, KB, CS, WPT, OCC, true, EDGE><<<dim3(pieces, p.slices, p.blocks), 256, lds, st>>>(a);
     mx_join_kernel<T, true><<<dim3(a.nq, a.batch, (a.dl + 255) / 256), 256, 0, st>>>(a);
   } else {
-    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, false>, lds);
-    mx_attn_kernel<T, KB, CS, WPT, OCC, false><<<dim3(a.batch, z), 256, lds, st>>>(a);
+    if (lds > 40 * 1024) allow_dynamic_lds((const void *)mx_attn_kernel<T, KB, CS, WPT, OCC, false, EDGE>, lds);
+    mx_attn_kernel<T, KB, CS, WPT, OCC, false, EDGE><<<dim3(a.batch, p.slices, p.blocks), 256, lds, st>>>(a);
   }
 }
 
 template <typename T>
-static void launch_decode(const Dims &d, const MxAttnArgs &a, bool tuned, int pieces, hipStream_t st) {
+static void launch_decode(const Dims &d, const MxAttnArgs &a, bool tuned, const MxPlan &p, int pieces, hipStream_t st) {
   if (!tuned) {
     mx_attn_any_kernel<T><<<dim3(a.splits, d.nq, a.batch), 256, 0, st>>>(a);
     mx_join_kernel<T, false><<<dim3(d.nq, a.batch, (d.dl + 255) / 256), 256, 0, st>>>(a);
     return;
   }
-  const int cs = mx_slice_width(d), z = d.wc_w / cs;
-  switch (d.wk_w * 4096 + cs) {
-    case 64 * 4096 + 128: return launch_tuned<T, 64, 128>(a, pieces, z, st);
-    case 64 * 4096 + 256: return launch_tuned<T, 64, 256>(a, pieces, z, st);
-    case 64 * 4096 + 512: return launch_tuned<T, 64, 512>(a, pieces, z, st);
-    case 128 * 4096 + 128: return launch_tuned<T, 128, 128>(a, pieces, z, st);
-    case 128 * 4096 + 256: return launch_tuned<T, 128, 256>(a, pieces, z, st);
-    case 128 * 4096 + 512: return launch_tuned<T, 128, 512>(a, pieces, z, st);
-    case 256 * 4096 + 256: return launch_tuned<T, 256, 256>(a, pieces, z, st);
-    case 256 * 4096 + 512: return launch_tuned<T, 256, 512>(a, pieces, z, st);
-    case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024>(a, pieces, z, st);
-    case 512 * 4096 + 512: return launch_tuned<T, 512, 512>(a, pieces, z, st);
-    case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024>(a, pieces, z, st);
-    case 1024 * 4096 + 1024: return launch_tuned<T, 1024, 1024>(a, pieces, z, st);
+  const int which = p.kb * 4096 + p.cs;
+  if (p.edge) {
+    switch (which) {
+      case 64 * 4096 + 128: return launch_tuned<T, 64, 128, true>(a, p, pieces, st);
+      case 64 * 4096 + 512: return launch_tuned<T, 64, 512, true>(a, p, pieces, st);
+      case 64 * 4096 + 1024: return launch_tuned<T, 64, 1024, true>(a, p, pieces, st);
+      case 128 * 4096 + 128: return launch_tuned<T, 128, 128, true>(a, p, pieces, st);
+      case 128 * 4096 + 512: return launch_tuned<T, 128, 512, true>(a, p, pieces, st);
+      case 128 * 4096 + 1024: return launch_tuned<T, 128, 1024, true>(a, p, pieces, st);
+      case 256 * 4096 + 512: return launch_tuned<T, 256, 512, true>(a, p, pieces, st);
+      case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024, true>(a, p, pieces, st);
+      case 512 * 4096 + 512: return launch_tuned<T, 512, 512, true>(a, p, pieces, st);
+      case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024, true>(a, p, pieces, st);
+    }
+    return;
+  }
+  switch (which) {
+    case 64 * 4096 + 128: return launch_tuned<T, 64, 128, false>(a, p, pieces, st);
+    case 64 * 4096 + 256: return launch_tuned<T, 64, 256, false>(a, p, pieces, st);
+    case 64 * 4096 + 512: return launch_tuned<T, 64, 512, false>(a, p, pieces, st);
+    case 128 * 4096 + 128: return launch_tuned<T, 128, 128, false>(a, p, pieces, st);
+    case 128 * 4096 + 256: return launch_tuned<T, 128, 256, false>(a, p, pieces, st);
+    case 128 * 4096 + 512: return launch_tuned<T, 128, 512, false>(a, p, pieces, st);
+    case 256 * 4096 + 256: return launch_tuned<T, 256, 256, false>(a, p, pieces, st);
+    case 256 * 4096 + 512: return launch_tuned<T, 256, 512, false>(a, p, pieces, st);
+    case 256 * 4096 + 1024: return launch_tuned<T, 256, 1024, false>(a, p, pieces, st);
+    case 512 * 4096 + 512: return launch_tuned<T, 512, 512, false>(a, p, pieces, st);
+    case 512 * 4096 + 1024: return launch_tuned<T, 512, 1024, false>(a, p, pieces, st);
+    case 1024 * 4096 + 1024: return launch_tuned<T, 1024, 1024, false>(a, p, pieces, st);
   }
 }
 
 int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, int requested, void *ws, size_t ws_bytes, void *l_out,
                      hipStream_t st) {
-  const bool tuned = mx_decode_tuned(d) && mx_layout_tuned(cv);
+  const MxPlan plan = mx_plan(d);
+  const bool tuned = plan.blocks && mx_layout_tuned(cv);
   // row numbers and their sums over a batch that is cut stay well inside 32 bits
   if (cv.max_seq > (1 << 30) || (batch <= kShareBatch && (int64_t)batch * cv.max_seq >= ((int64_t)1 << 36))) return GTA_ERR_UNSUPPORTED;
   const size_t head = tuned ? prefix_bytes(batch) : 0;
@@ -889,7 +951,7 @@ int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, 
   int64_t pieces = 0;
   if (ws_bytes < head) return GTA_ERR_WORKSPACE;
   if (tuned && batch <= kShareBatch) {
-    share = mx_share(d);
+    share = mx_share(plan);
     splits = std::min(requested, 1024);
     pieces = mx_most_pieces(batch, share, requested);
     if (fit < pieces) {   // a smaller workspace: as many pieces as it holds, or whole sequences
@@ -909,10 +971,10 @@ int launch_mx_decode(const Dims &d, const void *q, const MxView &cv, int batch, 
   int shift = 0;
   if (cv.pm.table) while ((1 << shift) < cv.pm.page_size && shift < 30) ++shift;
   float *acc = (float *)((char *)ws + head);
-  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, batch, splits, share, shift, d.scale * 1.4426950408889634f,
+  const MxAttnArgs a{q, cv, d.nq, d.qpk, d.qpc, d.dh, d.dl, d.wk_w, d.wc_w, batch, splits, share, shift, plan.maps, d.scale * 1.4426950408889634f,
                      acc, acc + std::min(pieces, fit) * d.nq * d.dl, (int32_t *)ws, l_out};
-  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, tuned, (int)pieces, st);
-  else launch_decode<float>(d, a, tuned, (int)pieces, st);
+  if (d.dtype == GTA_BF16) launch_decode<__bf16>(d, a, tuned, plan, (int)pieces, st);
+  else launch_decode<float>(d, a, tuned, plan, (int)pieces, st);
   return check_launch();
 }
 

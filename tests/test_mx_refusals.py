@@ -137,7 +137,8 @@ def test_struct_layout():
 
 @pytest.mark.parametrize("dims,answer", [
     ((4, 4, 1, 128, 512), 1), ((8, 8, 1, 128, 1024), 1), ((5, 1, 1, 64, 128), 1), ((10, 1, 2, 64, 128), 1), ((4, 4, 4, 128, 512), 1),
-    ((2, 1, 1, 256, 256), 1), ((2, 2, 1, 32, 64), 0), ((20, 20, 20, 64, 64), 0), ((6, 3, 2, 96, 160), 0), ((32, 1, 1, 64, 128), 0),
+    ((2, 1, 1, 256, 256), 1), ((2, 2, 1, 32, 64), 1), ((20, 20, 20, 64, 64), 1), ((6, 3, 2, 96, 160), 1), ((32, 1, 1, 64, 128), 1),
+    ((2, 1, 1, 512, 1024), 1), ((2, 1, 1, 544, 544), 0), ((4096, 1, 1, 32, 32), 1),
     ((2, 1, 1, 48, 128), B.GTA_ERR_UNSUPPORTED), ((1, 1, 1, 2048, 2048), B.GTA_ERR_UNSUPPORTED)])
 def test_which_kernel(dims, answer):
     nq, nk, nc, dh, dl = dims
