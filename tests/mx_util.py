@@ -115,14 +115,14 @@ class MxCache:
     def fill(self, lens, rng, spread=2.0):
         """Random rows in front of every slot's end: codes of ordinary numbers under scales 2^-spread .. 2^spread."""
         host = self.host()
-        for slot, n in enumerate(lens):
-            at = self.rows(slot, 0, n)
-            for codes, scale, w in ((host[0], host[2], self.kw), (host[1], host[3], self.cw)):
-                q, sc = quantise(rng.standard_normal((n, w)) * np.repeat(2.0 ** rng.uniform(-spread, spread, (n, w // BLOCK)), BLOCK, axis=1))
-                # codes of exact e4m3 numbers
-                order = np.argsort(E4M3[:127])
-                mag = order[np.searchsorted(E4M3[:127][order], np.abs(q))]
-                codes[at], scale[at] = (mag + 128 * np.signbit(q)).astype(np.uint8), sc
+        at = np.concatenate([self.rows(slot, 0, n) for slot, n in enumerate(lens)])
+        n = len(at)
+        for codes, scale, w in ((host[0], host[2], self.kw), (host[1], host[3], self.cw)):
+            q, sc = quantise(rng.standard_normal((n, w)) * np.repeat(2.0 ** rng.uniform(-spread, spread, (n, w // BLOCK)), BLOCK, axis=1))
+            # codes of exact e4m3 numbers
+            order = np.argsort(E4M3[:127])
+            mag = order[np.searchsorted(E4M3[:127][order], np.abs(q))]
+            codes[at], scale[at] = (mag + 128 * np.signbit(q)).astype(np.uint8), sc
         for t, h in zip((self.k, self.c, self.ks, self.cs), host):
             t.copy_(torch.from_numpy(h).view(t.shape))
         self.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
