@@ -237,8 +237,8 @@ GTA_API int gta_cache_append(const gta_config *cfg, const gta_cache *cache, cons
 
 /* RMS norm of every query and key head, then its rotation, in one pass:
  *   y_j = x_j / sqrt(mean_i x_i^2 + eps) * gain_j  (i, j within one head), then, with cfg->rope, the
- *   pair (j, j + d_h/2) turned by position * rope_base^(-2j/d_h).  Computed in fp32 (angles in fp64) and
- *   rounded once.  For models that norm their queries and keys: project with rope = 0
+ *   pair (j, j + d_h/2) turned by position * rope_base^(-2j/d_h).  Computed in fp32 and rounded once; the
+ *   sines of fp32 rows are rounded once from fp64, those of bf16 rows are within 1e-7.  For models that norm their queries and keys: project with rope = 0
  *   (gta_prefill_projection, for a decode step with one token per sequence), then call this.
  *   q, k        device, rows of n_q*d_h and n_k*d_h elements, q_stride and k_stride elements apart (at
  *               least the width): columns of one wide projection's output will do.  Aligned to an

@@ -1,6 +1,7 @@
 // RMS norm of every query and key head with its rotation (App. B.1.1) in the same pass:
 //   y_j = x_j / sqrt(mean_i x_i^2 + eps) * gain_j,   then (y_j, y_{j + d/2}) turned by position * base^(-2j/d).
-// Sums, the norm and the rotation are fp32 (angles fp64); the only rounding to 16 bits is that of the result.
+// Sums, the norm and the rotation are fp32, sines of fp32 rows are rounded once from fp64, those of bf16 rows are fp32; the only
+// rounding to 16 bits is that of the result.
 #include <math.h>
 
 #include <type_traits>
@@ -78,14 +79,18 @@ __device__ __forceinline__ void store8(float *p, const f32x8 &v) {
   *reinterpret_cast<f32x4 *>(p + 4) = __builtin_shufflevector(v, v, 4, 5, 6, 7);
 }
 
-struct Turns { uint64_t t[128]; };   // what one position turns pair j < d_h/2 by from the host
+// What one position turns pair j < d_h/2 by, from the host: 64-bit fractions of a turn for bf16 rows, radians for fp32 rows.
+template <typename T> struct Angles { uint64_t at[128]; };
+template <> struct Angles<float> { double at[128]; };
+__device__ __forceinline__ float2 cos_sin_of(int p, uint64_t turn) { return rope_cos_sin_turn(p, turn); }
+__device__ __forceinline__ float2 cos_sin_of(int p, double freq) { return rope_cos_sin(p, freq); }
 
 // Heads of 16 * LANES elements, rows and rows' starts in whole 16 bytes.  A lane has eight elements j.. and their partners
 // j + d_h/2 of HEADS heads of one token: their sines are the same and worked out once, a head's sum of squares is taken over
 // LANES neighbours, and loads and stores are 16 bytes.  Bound by memory where there are many tokens and by the launch where there
 // are few.
 template <typename T, int LANES, int HEADS, bool NT>
-__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, Turns turns) {
+__global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, Angles<T> angles) {
   constexpr int DH = 16 * LANES, HALF = DH / 2;
   const int heads = a.nq + a.nk, groups = (heads + HEADS - 1) / HEADS;
   const unsigned item = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, row = item / groups;   // token and group of heads
@@ -107,7 +112,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, Turns tu
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     float2 c = make_float2(1.f, 0.f);
-    if (a.rope) c = rope_cos_sin_turn(p, turns.t[j + e]);
+    if (a.rope) c = cos_sin_of(p, angles.at[j + e]);
     cs[e] = c.x;
     sn[e] = c.y;
   }
@@ -139,13 +144,16 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormRopeArgs a, Turns tu
 
 template <typename T, int LANES>
 static void launch_vector(const NormRopeArgs &a, hipStream_t st) {
-  Turns turns{};
-  if (a.rope) rope_turns(a.base, a.dh, a.dh / 2, turns.t);
+  Angles<T> angles{};
+  if (a.rope) {
+    if constexpr (sizeof(T) == 4) rope_freqs(a.base, a.dh, a.dh / 2, angles.at);
+    else rope_turns(a.base, a.dh, a.dh / 2, angles.at);
+  }
   const int heads = a.nq + a.nk;
   auto run = [&](auto n, auto nt) {
     constexpr int HEADS = decltype(n)::value;
     const int64_t threads = a.total * ((heads + HEADS - 1) / HEADS) * LANES;
-    norm_rope_kernel<T, LANES, HEADS, decltype(nt)::value><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(a, turns);
+    norm_rope_kernel<T, LANES, HEADS, decltype(nt)::value><<<dim3((unsigned)((threads + 255) / 256)), 256, 0, st>>>(a, angles);
   };
   // few tokens: a head to every group of lanes, so that its load is the only one waited for
   if (a.total * heads * LANES < (1 << 17)) run(std::integral_constant<int, 1>{}, std::false_type{});
@@ -153,9 +161,10 @@ static void launch_vector(const NormRopeArgs &a, hipStream_t st) {
   else run(std::integral_constant<int, 4>{}, std::false_type{});
 }
 
-// Heads of 32, 64, 128 or 256 and 16-byte rows.
+// Heads of 32, 64, 128 or 256 and 16-byte rows; fp32 rows as far as their angles stay in the reduction's range.
 template <typename T>
 static bool try_vector(const NormRopeArgs &a, hipStream_t st) {
+  if (sizeof(T) == 4 && !rope_angles_small(a.rope, a.base)) return false;
   const int64_t per = 16 / (int)sizeof(T);
   if (a.q_stride % per || a.k_stride % per || (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.q_gain | (uintptr_t)a.k_gain) & 15u))
     return false;
