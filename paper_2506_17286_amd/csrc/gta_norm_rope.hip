@@ -168,6 +168,7 @@ static bool try_vector(const NormRopeArgs &a, hipStream_t st) {
   const int64_t per = 16 / (int)sizeof(T);
   if (a.q_stride % per || a.k_stride % per || (((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.q_gain | (uintptr_t)a.k_gain) & 15u))
     return false;
+  if (a.total * ((a.nq + a.nk + 3) / 4) * (a.dh / 16) >= ((int64_t)1 << 32) - 256) return false;   // threads of a launch
   switch (a.dh) {
     case 32: launch_vector<T, 2>(a, st); return true;
     case 64: launch_vector<T, 4>(a, st); return true;

@@ -1,0 +1,27 @@
+"""What the 8-bit cache's and the norm's calls launch, looked at without a GPU (tests/launch_spy.py)."""
+import shutil
+
+import pytest
+
+import launch_spy as S
+
+pytestmark = pytest.mark.skipif(shutil.which("gcc") is None, reason="gcc not found")
+
+
+def test_norms_of_more_rows_than_a_launch_has_threads():
+    """A launch has fewer than 2^32 threads along x: more rows than that gives the vector kernel go to the one whose workgroups go on."""
+    out = S.run("""
+for dt in ("bf16", "f32"):
+    for nq, nk, dh in ((1, 1, 256), (1, 1, 128), (1, 1, 32), (4, 4, 256), (6, 3, 64), (1, 1, 96)):
+        cfg = B.make_config(d_model=256, n_heads=nq, n_qgroups=nq, n_kgroups=nk, n_cgroups=1, head_dim=dh, latent_dim=dh, dtype=dt)
+        for n in (1, 5000, 1 << 20, 1 << 27, 1 << 28, (1 << 28) + 1, (1 << 31) // (nq + nk), (1 << 31) // (nq + nk) + 1):
+            rc = B.load().gta_qk_norm_rope(R(cfg), FAKE, nq * dh, FAKE, nk * dh, None, None, 1e-6, None, n, FAKE, FAKE, None)
+            out.append([rc, n * (nq + nk), events()])
+""")
+    assert len(out) == 96
+    for rc, heads, text in out:
+        ev = S.parse(text)
+        if heads > 1 << 31:
+            assert rc == -5 and not ev                      # GTA_ERR_UNSUPPORTED
+        else:
+            assert rc == 0 and len(ev) == 1 and ev[0].grid[0] * ev[0].threads < 1 << 32
