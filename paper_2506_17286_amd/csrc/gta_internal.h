@@ -13,20 +13,23 @@
 
 namespace gta {
 
-// A kernel that takes more than 64 KiB of dynamic LDS needs the limit raised once per device it runs
-// on (the attribute belongs to the kernel's image on the current device).  Fixed table, no allocation.
+// A kernel that takes more than 64 KiB of dynamic LDS needs the limit raised on each device it runs on (the attribute
+// belongs to the kernel's image on the current device), and again for a launch that takes more than those before it.
+// Fixed table, no allocation.
 inline void allow_dynamic_lds(const void *fn, int bytes) {
-  struct Entry { const void *fn; int dev; };
+  struct Entry { const void *fn; int dev, bytes; };
   static Entry seen[256];
   static int n = 0;
   static std::mutex mu;
   int dev = 0;
   (void)hipGetDevice(&dev);
   std::lock_guard<std::mutex> lock(mu);
-  for (int i = 0; i < n; ++i)
-    if (seen[i].fn == fn && seen[i].dev == dev) return;
+  int i = 0;
+  while (i < n && !(seen[i].fn == fn && seen[i].dev == dev)) ++i;
+  if (i < n && seen[i].bytes >= bytes) return;
   (void)hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (n < 256) seen[n++] = Entry{fn, dev};   // table full: the attribute is simply set again next time
+  if (i == n && n < 256) ++n;
+  if (i < n) seen[i] = Entry{fn, dev, bytes};   // table full: the attribute is simply set again next time
 }
 
 // Validated, derived view of a gta_config.

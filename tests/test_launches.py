@@ -25,3 +25,31 @@ for dt in ("bf16", "f32"):
             assert rc == -5 and not ev                      # GTA_ERR_UNSUPPORTED
         else:
             assert rc == 0 and len(ev) == 1 and ev[0].grid[0] * ev[0].threads < 1 << 32
+
+
+def test_lds_is_asked_for_before_every_launch_that_needs_it():
+    """Calls of one kernel after each other that take more and more dynamic LDS: above 64 KiB the limit has to have been raised to what
+    the launch takes, by this call or one before, and not by every call."""
+    out = S.run("""
+import mx_util as M
+shapes = [M.SHAPES["h32"], M.SHAPES["q17"]]               # blocks of 10 maps, of 16
+shapes += [M.shape(m, 1, 1, 64, 256) for m in (1, 11, 16, 12)] + [M.shape(m, 1, 1, 128, 1024) for m in (2, 9, 16, 16)]
+shapes += [M.shape(m, m, 1, 64, 1024) for m in (1, 2, 4, 8, 16)] + list(M.SHAPES.values())
+for sh in shapes:
+    for dt in ("bf16", "f32"):
+        for batch in (1, 1025):
+            cfg = B.make_config(dtype=dt, **sh)
+            cache = B.gta_mx_cache(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, batch, 4096, None, 0, 0, 0)
+            rc = B.load().gta_mx_decode_attention(R(cfg), FAKE, R(cache), None, batch, 0, FAKE, FAKE, 1 << 40, None)
+            out.append([rc, events()])
+""")
+    limit, raised = {}, 0
+    for rc, text in out:
+        assert rc == 0
+        for ev in S.parse(text):
+            if isinstance(ev, S.Attr):
+                assert ev.lds > limit.get(ev.kernel, 0)
+                limit[ev.kernel], raised = ev.lds, raised + 1
+            else:
+                assert ev.lds <= max(64 << 10, limit.get(ev.kernel, 0)) and ev.lds <= 160 << 10, ev.kernel
+    assert raised
