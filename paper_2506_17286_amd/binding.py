@@ -190,17 +190,58 @@ def make_paged_cache(k_pool, c_pool, seq_lens, status, block_table) -> gta_cache
                      _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0])
 
 
+def _mx_cache(k, c, k_scale, c_scale, seq_lens, status, slots: int, max_seq: int, table=None) -> gta_mx_cache:
+    """Refuses arrays that the kernels would read past the end of or as something else."""
+    import torch
+    parts = {"k": k, "c": c, "k_scale": k_scale, "c_scale": c_scale, "seq_lens": seq_lens, "status": status}
+    if table is not None:
+        parts["block_table"] = table
+    codes, scales = (torch.float8_e4m3fn, torch.uint8, torch.int8), (torch.uint8, torch.float8_e8m0fnu)
+    for name, t in parts.items():
+        kinds = codes if name in ("k", "c") else scales if name.endswith("scale") else (torch.int32,)
+        if t.dtype not in kinds:
+            raise ValueError(f"{name} is {t.dtype}")
+        if not t.is_contiguous():
+            raise ValueError(f"{name} is not contiguous")
+        if t.device != k.device:
+            raise ValueError(f"{name} on {t.device}, k on {k.device}")
+    for name, t, scale in (("k", k, k_scale), ("c", c, c_scale)):
+        if t.shape[:2] != k.shape[:2] or scale.shape[:2] != k.shape[:2] or scale.numel() * GTA_MX_BLOCK != t.numel():
+            raise ValueError(f"{name} {tuple(t.shape)} with scales {tuple(scale.shape)} next to k {tuple(k.shape)}")
+    for name in ("seq_lens", "status"):
+        if parts[name].numel() < slots:
+            raise ValueError(f"{name} has {parts[name].numel()} entries for {slots} slots")
+    cache = gta_mx_cache(_ptr(k), _ptr(c), _ptr(k_scale), _ptr(c_scale), _ptr(seq_lens), _ptr(status), slots, max_seq)
+    if table is not None:
+        cache.block_table, cache.page_size, cache.pages_per_slot, cache.num_pages = _ptr(table), k.shape[1], table.shape[1], k.shape[0]
+    cache.device = k.get_device()
+    cache.widths = tuple(t.shape[2:].numel() for t in (k, c))
+    return cache
+
+
 def make_mx_cache(k, c, k_scale, c_scale, seq_lens, status) -> gta_mx_cache:
     """k [slots, max_seq, n_k*d_h] and c [slots, max_seq, n_c*d_l] of 8 bits (float8_e4m3fn or uint8), k_scale and c_scale
-    uint8 with one byte per 32 elements of a row, seq_lens/status int32 [slots] (device)."""
-    return gta_mx_cache(_ptr(k), _ptr(c), _ptr(k_scale), _ptr(c_scale), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1])
+    uint8 with one byte per 32 elements of a row, seq_lens/status int32 [slots]; contiguous, on one device."""
+    return _mx_cache(k, c, k_scale, c_scale, seq_lens, status, k.shape[0], k.shape[1])
 
 
 def make_paged_mx_cache(k_pool, c_pool, k_scale, c_scale, seq_lens, status, block_table) -> gta_mx_cache:
     """The same in pools [num_pages, page_size, width], with a block_table as make_paged_cache takes it."""
     slots, pps = block_table.shape
-    return gta_mx_cache(_ptr(k_pool), _ptr(c_pool), _ptr(k_scale), _ptr(c_scale), _ptr(seq_lens), _ptr(status), slots,
-                        pps * k_pool.shape[1], _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0])
+    return _mx_cache(k_pool, c_pool, k_scale, c_scale, seq_lens, status, slots, pps * k_pool.shape[1], block_table)
+
+
+def _mx(device: int, cfg: gta_config, cache: Optional[gta_mx_cache]):
+    """The cache as the library takes it, if it is on the current device and has the widths of cfg (one whose fields the caller
+    filled in is taken as it is)."""
+    if cache is None:
+        return None
+    if getattr(cache, "device", device) != device:
+        raise ValueError(f"cache on {'cpu' if cache.device < 0 else f'cuda:{cache.device}'}, current device is cuda:{device}")
+    widths = (cfg.n_kgroups * cfg.head_dim, cfg.n_cgroups * cfg.latent_dim)
+    if getattr(cache, "widths", widths) != widths:
+        raise ValueError(f"cache of rows of {cache.widths}, config of {widths}")
+    return ctypes.byref(cache)
 
 
 def _check(rc: int, where: str) -> None:
@@ -345,7 +386,7 @@ def gta_qk_norm_rope(cfg: gta_config, q, q_stride: int, k, k_stride: int, q_gain
 def gta_mx_cache_append(cfg: gta_config, cache: gta_mx_cache, slots, k_new, k_stride: int, c_new, c_stride: int, cu_new,
                         batch: int, max_new: int, stream=None, check: bool = True) -> int:
     d = _device()
-    rc = load().gta_mx_cache_append(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _on(d, slots),
+    rc = load().gta_mx_cache_append(ctypes.byref(cfg), _mx(d, cfg, cache), _on(d, slots),
                                     _on(d, k_new), k_stride, _on(d, c_new), c_stride, _on(d, cu_new), batch, max_new,
                                     _stream(stream))
     if check:
@@ -356,7 +397,7 @@ def gta_mx_cache_append(cfg: gta_config, cache: gta_mx_cache, slots, k_new, k_st
 def gta_mx_cache_read(cfg: gta_config, cache: gta_mx_cache, slots, first, cu_rows, batch: int, max_rows: int, k_out, c_out,
                       stream=None, check: bool = True) -> int:
     d = _device()
-    rc = load().gta_mx_cache_read(ctypes.byref(cfg), ctypes.byref(cache) if cache is not None else None, _on(d, slots),
+    rc = load().gta_mx_cache_read(ctypes.byref(cfg), _mx(d, cfg, cache), _on(d, slots),
                                   _on(d, first), _on(d, cu_rows), batch, max_rows, _on(d, k_out), _on(d, c_out),
                                   _stream(stream))
     if check:
@@ -367,7 +408,7 @@ def gta_mx_cache_read(cfg: gta_config, cache: gta_mx_cache, slots, first, cu_row
 def gta_mx_decode_attention(cfg: gta_config, q, cache: gta_mx_cache, slots, batch: int, num_splits: int, l_out, workspace,
                             stream=None, check: bool = True) -> int:
     d = _device()
-    rc = load().gta_mx_decode_attention(ctypes.byref(cfg), _on(d, q), ctypes.byref(cache) if cache is not None else None,
+    rc = load().gta_mx_decode_attention(ctypes.byref(cfg), _on(d, q), _mx(d, cfg, cache),
                                         _on(d, slots), batch, num_splits, _on(d, l_out), _on(d, workspace),
                                         0 if workspace is None else workspace.numel() * workspace.element_size(),
                                         _stream(stream))
