@@ -16,6 +16,14 @@ static size_t used;
 const char *spy_text(void) { return text; }
 void spy_clear(void) { text[used = 0] = 0; }
 
+/* the library's kernels */
+const char *spy_names(void) {
+  static char all[1 << 20];
+  size_t n = 0;
+  for (int i = 0; i < n_kernels; ++i) n += snprintf(all + n, n < sizeof all ? sizeof all - n : 0, "%s ", kernels[i].name);
+  return all;
+}
+
 static const char *name_of(const void *fn) {
   for (int i = 0; i < n_kernels; ++i)
     if (kernels[i].fn == fn) return kernels[i].name;

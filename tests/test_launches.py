@@ -53,3 +53,23 @@ for sh in shapes:
             else:
                 assert ev.lds <= max(64 << 10, limit.get(ev.kernel, 0)) and ev.lds <= 160 << 10, ev.kernel
     assert raised
+
+
+def test_every_attention_kernel_is_run_by_some_layer_of_the_tests():
+    """The kernels that the library has are the ones that the tests' layers take, in both types, in batches that are cut and that are not."""
+    registered, taken = S.run("""
+import mx_util as M, mx_layers
+taken = ""
+for sh in {**M.SHAPES, **mx_layers.WIDTHS}.values():
+    for dt in ("bf16", "f32"):
+        for batch in (8, 1026):
+            cfg = B.make_config(dtype=dt, **sh)
+            cache = B.gta_mx_cache(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, batch, 384, None, 0, 0, 0)
+            assert B.load().gta_mx_decode_attention(R(cfg), FAKE, R(cache), None, batch, 0, FAKE, FAKE, 1 << 40, None) == 0
+            taken += events()
+spy.spy_names.restype = ctypes.c_char_p
+out += [spy.spy_names().decode().split(), taken]
+""")
+    registered = {S.attention_kernel(n) for n in registered} - {None}
+    taken = {S.attention_kernel(e.kernel) for e in S.parse(taken)} - {None}
+    assert len(registered) == 88 and taken == registered, sorted(registered - taken)
