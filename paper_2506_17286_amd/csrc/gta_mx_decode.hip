@@ -488,13 +488,17 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 
   // the queries are asked for first, then the first tile's rows: these are on their way while the queries are laid out
   const int kg = x < nq ? (g0 + x) / a.qpk - kh0 : -1;
-  typedef __attribute__((ext_vector_type(8))) T Eight;
+  constexpr int PER = 16 / (int)sizeof(T);   // in words of 16 bytes, which is what queries are aligned to
+  typedef __attribute__((ext_vector_type(PER))) T QWord;
+  struct Eight { QWord w[8 / PER]; };
   constexpr int QF = QREG ? KP * 2 : KP / 2;   // fragments this wave lays out: all of them, or every fourth
   Eight qv[QF];
 #pragma unroll
   for (int i = 0; i < QF; ++i) {   // second operand for half a piece: dimensions h * 16 + (f & 1) * 8 .. of the piece
     const int f = QREG ? i : wave + 4 * i, p = f >> 1, d0 = p % ppk * 64 + h * 16;
-    qv[i] = *reinterpret_cast<const Eight *>((const T *)a.q + ((int64_t)b * a.nq + g0 + (kg == p / ppk ? x : 0)) * a.dh + (EDGE && d0 >= a.dh ? 0 : d0) + (f & 1) * 8);
+    const T *from = (const T *)a.q + ((int64_t)b * a.nq + g0 + (kg == p / ppk ? x : 0)) * a.dh + (EDGE && d0 >= a.dh ? 0 : d0) + (f & 1) * 8;
+#pragma unroll
+    for (int w = 0; w < 8 / PER; ++w) qv[i].w[w] = reinterpret_cast<const QWord *>(from)[w];
   }
   At nxt{};
   auto start = [&]() {
@@ -519,7 +523,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 v[NQP];
-      split_parts<NQP>(kg == (f >> 1) / ppk && (!EDGE || (f >> 1) % ppk * 64 + h * 16 < a.dh) ? to_f(qv[i][e]) : 0.f, v);
+      split_parts<NQP>(kg == (f >> 1) / ppk && (!EDGE || (f >> 1) % ppk * 64 + h * 16 < a.dh) ? to_f(qv[i].w[e / PER][e % PER]) : 0.f, v);
 #pragma unroll
       for (int j = 0; j < NQP; ++j) out[j][e] = v[j];
     }

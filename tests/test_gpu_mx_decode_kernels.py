@@ -212,3 +212,15 @@ def test_fp32_weights_keep_24_bits(name):
     # result 2
     worst = (np.abs(got - ref) / np.maximum(16 * 2.0 ** -24 * np.abs(ref), 1e-300)).max()
     assert worst <= 1, f"{worst:.3g} of the bound"
+
+
+@pytest.mark.parametrize("name", sorted(ALL))
+def test_fp32_queries_on_any_16_bytes(name):
+    sh = ALL[name]
+    lens = [300, 17, 1]
+    cache = M.MxCache(sh, 3, 320).fill(lens, np.random.default_rng(25))
+    q = D.queries(sh, "f32", 3)
+    moved = torch.zeros(q.numel() + 4, device="cuda")[4:].view(q.shape)
+    moved.copy_(q)
+    assert q.data_ptr() % 32 == 0 and moved.data_ptr() % 32 == 16
+    np.testing.assert_array_equal(D.attend(cache, sh, "f32", moved, 3), D.attend(cache, sh, "f32", q, 3))
