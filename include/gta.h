@@ -282,8 +282,8 @@ GTA_API int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, 
  *   num_splits  context splits per sequence (fewer of short ones; batches of more than 1024 sequences may go
  *               unsplit); 0 = library's choice, which shares a batch's rows out evenly
  *   workspace   mode MX_DECODE
- * Sums and softmax statistics are fp32; weights are relative to one score of a few hundred rows and may be
- * up to 2^40, so that latents beyond 2^80 can overflow.  A sequence without rows, or with a slot out of
+ * Sums and softmax statistics are fp32; the average of finite latents is finite, up to the largest that the
+ * format holds (rows are gone through twice where some are of about 2^56 and more).  A sequence without rows, or with a slot out of
  * range, gets zeros.  l_out goes on into gta_prefill_decoder.  head_dim up to 1024, latent_dim up to 4096,
  * max_seq up to 2^30, batch * max_seq below 2^36 for batches of up to 1024 (GTA_ERR_UNSUPPORTED).
  * Runs on the matrix-instruction kernel where gta_uses_tuned_kernels(cfg, GTA_MODE_MX_DECODE) is 1 and

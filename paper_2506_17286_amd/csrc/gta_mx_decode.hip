@@ -38,7 +38,7 @@ __device__ __forceinline__ float to_f(__bf16 v) { return (float)v; }
 constexpr int kAnyMaxHead = 1024, kAnyMaxLatent = 4096;
 
 // Any page sizes, heads of more than 512: a workgroup per (split, map, sequence), a row per thread for the scores, four latents per
-// thread for the sums.
+// thread for the sums, which are averages over the rows so far: the largest finite latents stay finite.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
   __shared__ float qs[kAnyMaxHead];
@@ -89,13 +89,15 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
     for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
     if ((tid & 63) == 0) red2[tid >> 6] = sum;
     __syncthreads();
-    l = l * corr + (red2[0] + red2[1]) + (red2[2] + red2[3]);
+    const float before = l * corr;
+    l = before + (red2[0] + red2[1]) + (red2[2] + red2[3]);
     m = mn;
+    const float per = l > 0.f ? 1.f / l : 0.f, kept = before * per;
     for (int v = 0; v * 256 + my < quads; ++v)
-      for (int e = 0; e < 4; ++e) acc[v][e] *= corr;
+      for (int e = 0; e < 4; ++e) acc[v][e] *= kept;
     if (grp < groups)
       for (int r = grp; r < cnt; r += groups) {
-        const float pr = ps[r];
+        const float pr = ps[r] * per;
         const int64_t row = rowid[r];
         for (int v = 0; v * 256 + my < quads; ++v) {
           const int col = ccol + (v * 256 + my) * 4;
@@ -148,6 +150,9 @@ __global__ __launch_bounds__(256) void mx_attn_any_kernel(MxAttnArgs a) {
 // their range.  A wave that meets a score more than 40 above (28 in units of the natural exponent) goes through its rows once
 // more with the maximum it has found by then.  Rescaling the sums in the loop instead keeps two copies of them in registers
 // (64 latents of 256 and 1 key of 64: 125 registers spilled).
+// Sums of weights and latents stay below 2^127 as long as latents do below 2^57: a weight is at most 2^40, rows are 2^30.  A piece
+// with larger ones, which its scale bytes tell, is gone through once more, too, with weights of at most 2^-32 and sums below 2^126:
+// the average of finite latents is finite.  (Such weights are good to 2^-18, the rounding of an exponent of 32 and more.)
 template <typename T> struct Parts { static constexpr int Q = 1, P = 2; };
 template <> struct Parts<float> { static constexpr int Q = 3, P = 3; };
 
@@ -171,6 +176,8 @@ template <> struct Word<16> { typedef u32x4 type; };
 
 constexpr float kLowest = -3e38f;   // stands for "no score yet" where a difference is taken
 constexpr float kMostAbove = 40.f;
+constexpr unsigned kLargeScale = 127 + 48;   // latents of blocks below it are less than 2^57
+constexpr float kLower = 32.f;               // how far such a piece's weights are lowered
 
 constexpr int kTile = 32;           // rows of a tile
 constexpr int kShareBatch = 1024;   // a larger batch has a workgroup per sequence
@@ -449,7 +456,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int kPast = 2;
   auto my_half = [&](const At &at, int kh) {   // of the rows that this wave scores
     if constexpr (WPT == 1) return at;
-    At r;
+    At r{};
     r.row[kh] = role ? at.row[1] : at.row[0];
     r.rows[kh] = role ? at.rows[1] : at.rows[0];
     return r;
@@ -537,6 +544,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 
   f32x4 acc[NCH][LC];
   float m = -INFINITY, l = 0.f, seen = -INFINITY;   // what weights refer to, their sum, the largest score of this lane's rows
+  unsigned most = 0;   // largest scale byte of its latents
 
   auto tile = [&](int t, int turn) {
     // ---- scores; a piece's query fragments are asked for a piece ahead, its sums are taken a piece later
@@ -635,7 +643,13 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
           p1 -= (float)v[1];
         }
       }
-    // ---- sums
+    // ---- sums; the scale bytes first (looked at among the products: 64 x 2048 fp32 rows of the paper's layer 13.8 -> 14.1 us)
+#pragma unroll
+    for (int c = 0; c < NCH; ++c)
+#pragma unroll
+      for (int hf = 0; hf < HF; ++hf)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) most = max(most, cs[hf][j][c]);
     const Pages then = ask(t + 2 * NS);   // (no LDS is read from here on, whose waits would be waits for these loads)
 #pragma unroll
     for (int c = 0; c < NCH; ++c) {
@@ -669,6 +683,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     nxt = settle(t + 2 * NS, then);
   };
 
+  bool lowered = false;
   while (true) {
 #pragma unroll
     for (int c = 0; c < NCH; ++c)
@@ -682,10 +697,13 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
     }
     seen = fmaxf(seen, __shfl_xor(seen, 16));
     seen = fmaxf(seen, __shfl_xor(seen, 32));
-    bool again = __any(seen > m + kMostAbove);   // (never the second time)
+    bool large = !lowered && __any(most >= kLargeScale);
+    bool again = large || __any(seen > m + kMostAbove);   // (never a second time)
     if constexpr (WPT > 1) again = __syncthreads_or(again);
     if (!again) break;
-    m = fmaxf(m, seen);
+    if constexpr (WPT > 1) large = __syncthreads_or(large);   // (a pair's waves have the same scores, but different latents)
+    m = fmaxf(m, seen) + (large ? kLower : 0.f);
+    lowered |= large;
     start();
   }
 
@@ -754,7 +772,7 @@ __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
 
 // Joins the pieces of a map: a workgroup per (map, sequence, 256 latents), four latents per thread and the pieces dealt to as
 // many groups of threads as there are.  SHARED: the pieces that mx_attn_kernel left (it has written sequences of one piece itself); otherwise
-// a.splits of them for every sequence.
+// a.splits of them for every sequence, which are averages.
 constexpr int kMaxPieces = 2560;   // of a sequence: at most twice the workgroups that the chip holds, and one, or 1024 splits
 
 template <typename T, bool SHARED>
@@ -805,6 +823,11 @@ __global__ __launch_bounds__(256) void mx_join_kernel(MxAttnArgs a) {
   if ((tid & 63) == 0) red2[tid >> 6] = l;
   __syncthreads();
   l = (red2[0] + red2[1]) + (red2[2] + red2[3]);
+  if constexpr (!SHARED) {
+    for (int i = tid; i < pieces; i += 256) wt[i] = wt[i] * a.pml[at(i) * 2 + 1] / l;
+    __syncthreads();
+    l = 1.f;
+  }
   // 64 threads for 256 latents (fewer where there are fewer), the pieces dealt to the others
   const int c0 = blockIdx.z * 256, lanes = min(a.dl - c0, 256) / 4, groups = 256 / lanes, my = tid % lanes, grp = tid / lanes;
   f32x4 v = {0.f, 0.f, 0.f, 0.f};

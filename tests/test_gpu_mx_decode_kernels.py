@@ -144,6 +144,28 @@ def test_block_exponents_over_the_range(name, dtype):
         held(D.attend(cache, sh, dtype, q, 1, None, splits), cache, sh, dtype, q, n)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", sorted(ALL))
+@pytest.mark.parametrize("how", ["level", "climb"])
+def test_the_largest_latents(name, how, dtype):
+    """Blocks up to the largest exponent, 119, next to ordinary ones, with one sign and with both: the result is an average and
+    finite.  climb: scores that rise along the rows, so that weights are taken relative to far lower ones."""
+    sh, n = ALL[name], 300
+    rng = np.random.default_rng(22)
+    cache = M.MxCache(sh, 1, 320).fill([n], rng)
+    e = np.array((119, 0, 100, 60, 119, 90, 70, 80))[np.arange(cache.cw // 32) % 8]
+    c = np.clip(rng.standard_normal((n, cache.cw)) * 150, -448, 448)
+    c[:, ::2] = np.abs(c[:, ::2])
+    c[:, :32] = 448.0                                       # the largest there is, in every row
+    size = 0.2 * np.ones(n) if how == "level" else np.arange(n) / 8
+    store(cache, np.repeat(size[:, None], cache.kw, axis=1) * (1 if how == "climb" else rng.standard_normal((n, cache.kw))),
+          c * np.repeat(2.0 ** e, 32))
+    x = np.abs(rng.standard_normal((1, sh["n_qgroups"] * sh["head_dim"]))) * 3 / np.sqrt(sh["head_dim"])
+    q = torch.from_numpy(x).to("cuda", M.DT[dtype])
+    for splits in (1, 4):
+        held(D.attend(cache, sh, dtype, q, 1, None, splits), cache, sh, dtype, q, n)
+
+
 @pytest.mark.parametrize("name", sorted(ALL))
 def test_fp32_queries_keep_24_bits(name):
     """Keys K in one element and -K in another (K a power of two), queries 1 + a 2^-20 and 1 there, a scale of 2^20: the scores are a K, and the
