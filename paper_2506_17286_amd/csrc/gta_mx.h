@@ -27,7 +27,7 @@ inline MxView mx_view_of(const gta_mx_cache &c, const int32_t *slots) {
 // Results of more bytes than the L2s hold (8 of 4 MiB) are stored past them (non-temporal) where a wave's stores fill whole lines,
 // which is where a thread has one 16-byte word: nothing of the beginning would be left in the L2s when the next kernel asks for
 // it, and the stores run faster (rows of 100 MB read back 42 -> 25 us, 44 MB of normed rows 22 -> 19).  Smaller ones stay for
-// whoever reads them next, in the same time.
+// whoever reads them next, in the same time.  (Appended prompts have a rule of their own.)
 inline bool stream_past_caches(int64_t bytes) { return bytes > (32 << 20); }
 
 // 16 bytes

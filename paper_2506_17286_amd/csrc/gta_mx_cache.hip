@@ -37,12 +37,15 @@ __device__ __forceinline__ f32x8 load8(const __bf16 *p) {
 }
 
 // A workgroup's rows as words of ELEMS elements, keys first: `per_row` of them a row, and an inverse of it for divisions (exact for
-// the numbers that come up: below 2^12, or below per_row <= 2^16).
+// the numbers that come up: below 2^11, or below per_row <= 2^16).
 struct Words {
   int kw, cw, per_row;
   unsigned inverse;
 };
-constexpr int kMostWords = 4096;   // of a workgroup
+// Most words of a sequence that one workgroup stores, setting the length as well, in place of a launch of many and one behind it for
+// the lengths: 1 to 64 sequences of 2048 words (32 rows of 1024 elements) 6.7 to 7.4 us against 9.1, of 3072 9.5 to 10.8 against 9.5
+// to 10.0, of 4096 10.2 to 14.4 against 8.8 to 9.4; 300 sequences of 1024 words 6.8 to 7.5 against 9.1, of 2048 10.7 to 11.5 against 9.1 to 12.6.
+constexpr int kMostWords = 2048;
 
 // Where word i of the workgroup lies: its row there, its column, whether it is a key's.
 struct Place { int row, at, width; bool key; };
@@ -107,7 +110,9 @@ __device__ __forceinline__ AppendPlan append_plan(const MxView &cv, const int32_
 // rows_per_wg rows of sequence blockIdx.y from blockIdx.x * rows_per_wg on, a thread to sixteen elements and two threads to a block:
 // a whole 16-byte word of codes to store (eight elements a thread: 16 sequences of 300..2048 rows of 2048 elements 39 us against 31).
 // Bound by memory, and by the chain of loads in front (lengths, slot, pages) where there are few rows; with a second word on its
-// way per thread it took as long.
+// way per thread it took as long.  Codes of prompts go past the caches whatever their size: below 20 MB that takes as long as keeping
+// them, an attention over the rows right behind included (8 x 512 rows of 1024 elements 13.3 us, with it 21.7 against 22.0); fp32 prompts
+// of 35 to 70 MB 30 to 65 us against 35 to 72.
 // COMMIT: the workgroup has the whole sequence and sets its length as well.
 template <typename T, bool COMMIT, bool VEC>
 __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_new, int64_t k_stride, const T *c_new, int64_t c_stride,
@@ -125,7 +130,7 @@ __global__ __launch_bounds__(256) void mx_append_kernel(MxView cv, const T *k_ne
       const int64_t dst = cache_row(cv.pm, cv.max_seq, a.slot, a.p + j0 + p.row);
       int e;
       const u32x4 codes = quantise16(x, e);
-      store16<!COMMIT>(reinterpret_cast<u32x4 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at), codes);   // (prompts: past the caches)
+      store16<!COMMIT>(reinterpret_cast<u32x4 *>((p.key ? cv.k : cv.c) + dst * p.width + p.at), codes);   // (prompts: past the caches, at any size)
       if ((p.at & 31) == 0) (p.key ? cv.ks : cv.cs)[dst * (p.width / kMxBlock) + p.at / kMxBlock] = (uint8_t)(e + 127);
     }
   }
@@ -225,7 +230,7 @@ int launch_mx_append(const Dims &d, const MxView &cv, const void *k_new, int64_t
                      const int32_t *cu_new, int batch, int max_new, hipStream_t st) {
   const Words w = words_of(d, 16);
   const int most = std::min(max_new, cv.max_seq);   // a sequence of more rows than a slot has stores none
-  // few rows: a workgroup per sequence, which sets the length as well; otherwise the lengths need a launch behind this one
+  // few rows: a workgroup per sequence; otherwise the lengths need a launch behind this one (every workgroup reads the old one)
   const bool one = (int64_t)most * w.per_row <= kMostWords;
   const int rows = one ? std::max(most, 1) : rows_per_workgroup(w, 512);
   const dim3 grid(one ? 1u : (unsigned)(((int64_t)most + rows - 1) / rows), batch);

@@ -73,3 +73,24 @@ out += [spy.spy_names().decode().split(), taken]
     registered = {S.attention_kernel(n) for n in registered} - {None}
     taken = {S.attention_kernel(e.kernel) for e in S.parse(taken)} - {None}
     assert len(registered) == 88 and taken == registered, sorted(registered - taken)
+
+
+def test_appends_of_few_rows_are_one_launch():
+    """Up to 2048 words of 16 elements a sequence: one workgroup each, which sets the length; above, a second launch does."""
+    out = S.run("""
+import mx_util as M
+for name in ("paper", "1b", "wide"):
+    sh = M.SHAPES[name]
+    width = sh["n_kgroups"] * sh["head_dim"] + sh["n_cgroups"] * sh["latent_dim"]
+    for dt in ("bf16", "f32"):
+        for rows in (0, 1, 16, 32, 2048 * 16 // width, 2048 * 16 // width + 1, 64 * 1024 // width, 4000):
+            cfg = B.make_config(dtype=dt, **sh)
+            cache = B.gta_mx_cache(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 8, 4096, None, 0, 0, 0)
+            kw = sh["n_kgroups"] * sh["head_dim"]
+            rc = B.load().gta_mx_cache_append(R(cfg), R(cache), None, FAKE, kw, FAKE, width - kw, FAKE, 8, rows, None)
+            out.append([rc, rows * width // 16, events()])
+""")
+    for rc, words, text in out:
+        ev = S.parse(text)
+        assert rc == 0 and all(e.grid[1] == 8 for e in ev[:1])
+        assert len(ev) == (1 if words <= 2048 else 2) and (words > 2048 or ev[0].grid == (1, 8, 1))
