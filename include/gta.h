@@ -128,7 +128,8 @@ typedef struct {
  * code * 2^e.  e is the least exponent with which the block's largest finite magnitude is at most
  * 448 * 2^e, kept within -117 .. 119: every stored value is zero or a normal bf16 number, and a code is
  * the element rounded once, to 3 bits behind the leading one (2^-4 relative at most for magnitudes from
- * 2^-6 * 2^e on, half of 2^-9 * 2^e absolute below).  NaN and infinities are stored as NaN and do not enter e.
+ * 2^-6 * 2^e on, half of 2^-9 * 2^e absolute below); magnitudes above 448 * 2^119 = 1.75 * 2^127 are stored as
+ * that.  NaN and infinities are stored as NaN and do not enter e.
  * head_dim and latent_dim must be multiples of GTA_MX_BLOCK, a key and a latent row together at most 2^18
  * elements (GTA_ERR_UNSUPPORTED otherwise).  Struct host, arrays device, all
  * 16-byte aligned (lengths, status and table 4).  Layouts and block table as in gta_cache: row p of a
@@ -269,7 +270,7 @@ GTA_API int gta_mx_cache_append(const gta_config *cfg, const gta_mx_cache *cache
  * become rows [cu_rows[b], cu_rows[b+1]) of k_out [total, n_k*d_h] and c_out [total, n_c*d_l] (element
  * type = cfg->dtype; nothing is rounded).  Rows outside 0 .. seq_lens[slot] - 1, rows without a page and
  * slots out of range read as zeros.  A sequence of more than max_rows rows is skipped and its slot's
- * status set to GTA_ERR_SHAPE.
+ * status set to GTA_ERR_SHAPE; with max_rows 0 the call does nothing, and flags nothing.
  *   first   device [batch], or NULL for zeros;  cu_rows device [batch+1];  slots device [batch] or NULL
  * With gta_cache_append the rows go on into a gta_cache, e.g. for gta_prefill_chunk. */
 GTA_API int gta_mx_cache_read(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const int32_t *first,

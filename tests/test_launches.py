@@ -94,3 +94,15 @@ for name in ("paper", "1b", "wide"):
         ev = S.parse(text)
         assert rc == 0 and all(e.grid[1] == 8 for e in ev[:1])
         assert len(ev) == (1 if words <= 2048 else 2) and (words > 2048 or ev[0].grid == (1, 8, 1))
+
+
+def test_reads_bounded_to_no_rows_launch_nothing():
+    out = S.run("""
+import mx_util as M
+cfg = B.make_config(dtype="bf16", **M.SHAPES["1b"])
+cache = B.gta_mx_cache(FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 8, 4096, None, 0, 0, 0)
+for most in (0, 1):
+    rc = B.load().gta_mx_cache_read(R(cfg), R(cache), None, None, FAKE, 8, most, FAKE, FAKE, None)
+    out.append([rc, len(events())])
+""")
+    assert out[0] == [0, 0] and out[1][0] == 0 and out[1][1] > 0
