@@ -180,7 +180,9 @@ constexpr unsigned kLargeScale = 127 + 48;   // latents of blocks below it are l
 constexpr float kLower = 32.f;               // how far such a piece's weights are lowered
 
 constexpr int kTile = 32;           // rows of a tile
-constexpr int kShareBatch = 1024;   // a larger batch has a workgroup per sequence
+// A larger batch has a workgroup per sequence.  1024 and 1025 sequences of 256 rows of the paper's layer 24.6 and 14.0 us (1B shape 60.8 and
+// 53.7), one of 16384 among others of 64 23.5 and 104.7: the cut is for lengths that differ.
+constexpr int kShareBatch = 1024;
 
 // inclusive sums over the lanes of a wave
 __device__ __forceinline__ int wave_scan(int v) {
@@ -312,8 +314,11 @@ __device__ __forceinline__ int cut_lanes(const MxView &cv, int batch, int per_ro
 // EDGE: rows of other widths than KB and CS, more than 16 maps, heads that end inside a piece.  A workgroup then has a.maps maps
 // from g0 on and reads the columns of their key heads and latents (blockIdx.z: which maps, blockIdx.y: which CS of their latents);
 // a head begins a piece of its own, and lanes without columns ask for what lies behind the buffer, zeros that cost nothing.  (64 x
-// 8192 rows of 5 keys of 64 and 512 latents for 15 maps: 2215 us in mx_attn_any_kernel, 89 here; rows of the widths KB and CS go
-// without: one scale byte a load in place of four alone takes 182 us for 32 x 16384 of 1024 + 1024 to 207.)
+// 8192 rows of 5 keys of 64 and 512 latents for 15 maps: 2215 us in mx_attn_any_kernel, 94 here.)  Rows of the widths KB and CS go
+// without: one scale byte a load in place of four alone takes 182 us for 32 x 16384 of 1024 + 1024 to 207.  With and without, 64 x 8192
+// bf16 rows: 64 + 128 26.2 / 25.5 us, + 256 42.3 / 35.4, + 512 69.5 / 69.0; 128 + 128 32.4 / 30.2, + 256 45.7 / 39.0, + 512 71.9 / 67.7; 256 + 256
+// 56.6 / 49.5, + 512 85.9 / 85.5, + 1024 131.9 / 130.6; 512 + 512 113.5 / 112.0, + 1024 163.7 / 161.5; 1024 + 1024 247 / 205; 64 x 1024 and one of 4096
+// rows 3 to 20 % apart, but for one of 1024 + 1024 (17.9 / 19.1).
 template <typename T, int KB, int CS, int WPT, int OCC, bool SHARED, bool EDGE>
 __global__ __launch_bounds__(256, OCC) void mx_attn_kernel(MxAttnArgs a) {
   constexpr int NQP = Parts<T>::Q, NPP = Parts<T>::P;
