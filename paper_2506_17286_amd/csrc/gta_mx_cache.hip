@@ -43,8 +43,8 @@ struct Words {
   unsigned inverse;
 };
 // Most words of a sequence that one workgroup stores, setting the length as well, in place of a launch of many and one behind it for
-// the lengths: 1 to 64 sequences of 2048 words (32 rows of 1024 elements) 6.7 to 7.4 us against 9.1, of 3072 9.5 to 10.8 against 9.5
-// to 10.0, of 4096 10.2 to 14.4 against 8.8 to 9.4; 300 sequences of 1024 words 6.8 to 7.5 against 9.1, of 2048 10.7 to 11.5 against 9.1 to 12.6.
+// the lengths: 1 to 64 sequences of 2048 words (32 rows of 1024 elements) 6.7 to 7.4 us against 9.1, half as much again level,
+// of 4096 words 10.2 to 14.4 against 8.8 to 9.4; 300 sequences of 1024 words 6.8 to 7.5 against 9.1, of 2048 10.7 to 11.5 against 9.1 to 12.6.
 constexpr int kMostWords = 2048;
 
 // Where word i of the workgroup lies: its row there, its column, whether it is a key's.
