@@ -246,3 +246,28 @@ def test_fp32_queries_on_any_16_bytes(name):
     moved.copy_(q)
     assert q.data_ptr() % 32 == 0 and moved.data_ptr() % 32 == 16
     np.testing.assert_array_equal(D.attend(cache, sh, "f32", moved, 3), D.attend(cache, sh, "f32", q, 3))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_captured_call_that_takes_more_lds_than_those_before(dtype):
+    """Maps in blocks of 10, then of 16 on the same kernel: the second call asks for more LDS, here for the first time within a capture."""
+    small, sh = M.shape(20, 4, 2, 32, 640), M.shape(16, 1, 1, 96, 1280)
+    warm = M.MxCache(small, 2, 64).fill([40, 3], np.random.default_rng(26))
+    D.attend(warm, small, dtype, D.queries(small, dtype, 2), 2)
+    lens = [300, 17, 0]
+    cache = M.MxCache(sh, 3, 320, 16).fill(lens, np.random.default_rng(27))
+    q, cfg = D.queries(sh, dtype, 3), B.make_config(dtype=dtype, **sh)
+    ws = B.alloc_workspace(B.gta_workspace_bytes(cfg, B.GTA_MODE_MX_DECODE, 3, 0, 320))
+    out = torch.zeros((3, 16 * 1280), dtype=M.DT[dtype], device="cuda")
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side), torch.cuda.graph(graph, stream=side):
+        B.gta_mx_decode_attention(cfg, q, cache.struct, None, 3, 0, out, ws, stream=side)
+    for _ in range(3):
+        out.fill_(7.0)
+        ws.view(torch.uint8).fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.double().cpu().numpy()
+        np.testing.assert_array_equal(got, D.attend(cache, sh, dtype, q, 3))
+        D.check(got, cache, sh, dtype, q, range(3), lens)
