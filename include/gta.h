@@ -62,7 +62,8 @@ typedef enum {
 
 enum { GTA_F32 = 0, GTA_BF16 = 1 };            /* gta_config.dtype */
 enum { GTA_GATE_SIGMOID = 0, GTA_GATE_OFF = 1, GTA_GATE_SILU = 2, GTA_GATE_RELU2 = 3 }; /* gta_config.gate  */
-enum { GTA_MODE_PREFILL = 0, GTA_MODE_DECODE = 1, GTA_MODE_PREFILL_CHUNK = 2, GTA_MODE_MX_DECODE = 3 };
+enum { GTA_MODE_PREFILL = 0, GTA_MODE_DECODE = 1, GTA_MODE_PREFILL_CHUNK = 2, GTA_MODE_MX_DECODE = 3, GTA_MODE_PREFILL_MASKED = 4,
+       GTA_MODE_PREFIX_DECODE = 5 };
 
 /* Hyper-parameters of one GTA layer (Sec. 3.2).  Host memory. */
 typedef struct {
@@ -150,6 +151,51 @@ typedef struct {
   int32_t  num_pages;
 } gta_mx_cache;
 
+/* How heads are rotated by gta_qk_rope, as a model's configuration states it.  Host memory.
+ *   The first r = rotary_dim elements of a head turn in pairs, pair j by position * f_j; the others are copied. */
+enum { GTA_ROPE_HALF = 0, GTA_ROPE_INTERLEAVED = 1 };   /* pairs (j, j + r/2) or (2j, 2j + 1) */
+enum {
+  GTA_ROPE_PLAIN = 0,   /* f_j = base^(-2j/r) */
+  GTA_ROPE_LINEAR = 1,  /* f_j / factor: positions of a context `factor` times as long fall between the trained ones */
+  GTA_ROPE_BASE = 2,    /* base * factor^(r/(r-2)) in place of base: the slowest pair is slowed down by factor, the fastest is kept */
+  GTA_ROPE_BANDS = 3,   /* by how often pair j turns over the trained length, t = trained_len * f_j / (2 pi): up to slow_turns
+                           f_j / factor, from fast_turns on f_j, between them blended linearly in t */
+  GTA_ROPE_GIVEN = 4    /* f_j = frequency[j] */
+};
+#define GTA_ROPE_MAX_PAIRS 256
+typedef struct {
+  int32_t layout;          /* GTA_ROPE_HALF | GTA_ROPE_INTERLEAVED */
+  int32_t rotary_dim;      /* r: even, at most head_dim and 2 * GTA_ROPE_MAX_PAIRS; 0 = head_dim */
+  int32_t scaling;
+  float   base;            /* > 0; not read with GTA_ROPE_GIVEN */
+  float   factor;          /* > 0; read by LINEAR, BASE (r > 2) and BANDS */
+  float   trained_len, slow_turns, fast_turns;   /* BANDS: > 0, slow_turns < fast_turns */
+  float   magnitude;       /* the turned elements are multiplied by it (> 0); 0 = 1 */
+  const double *frequency; /* GTA_ROPE_GIVEN: host, [r/2], finite */
+} gta_rope_spec;
+
+/* The same, worked out: what gta_qk_rope takes.  Plain host memory without pointers, filled in by gta_make_rotation. */
+typedef struct {
+  int32_t  layout, rotary_dim;
+  float    magnitude;
+  int32_t  reserved;                 /* 0 */
+  uint64_t turn[GTA_ROPE_MAX_PAIRS]; /* f_j / (2 pi) modulo 1, in units of 2^-64 */
+} gta_rotation;
+
+/* What happens to the scores of gta_prefill_masked_attention and gta_prefix_decode_attention between the product and the
+ * softmax, and which keys a token sees.  Struct host, arrays device; a NULL struct or all fields 0 / NULL: nothing, and every
+ * key up to the token itself.
+ *   s = softmax_scale * q . k;  with cap > 0  s = cap * tanh(s / cap);  with slopes  s = s - slopes[g] * |p - j|
+ * (p the token's position, j the key's, g the map).  A token sees the keys j with first <= j <= last, first taken as 0 where it
+ * is less, last as the last key there is where it is more.  One that sees none gets a row of zeros.  What is not seen is not read
+ * into the result, NaN and infinities included. */
+typedef struct {
+  float          cap;     /* 0 = off; finite and not negative */
+  const float   *slopes;  /* [n_q] fp32, finite, or NULL */
+  const int32_t *first;   /* per token, or NULL: 0 */
+  const int32_t *last;    /* per token, or NULL: the token's own position */
+} gta_score_rules;
+
 /* Bytes of device workspace the call described by the arguments needs.
  *   mode PREFILL: batch sequences, total_tokens packed tokens, longest sequence <= max_len.
  *   mode DECODE : batch sequences, max_len = cache->max_seq, num_splits as passed to gta_decode
@@ -158,6 +204,8 @@ typedef struct {
  *   mode PREFILL_CHUNK: as PREFILL, for gta_prefill_chunk (max_len = max_chunk).
  *   mode MX_DECODE: for gta_mx_decode_attention (max_len = cache->max_seq, num_splits as passed there;
  *                 with 0, a smaller workspace that holds one split is used with the splits it holds).
+ *   mode PREFILL_MASKED: as PREFILL, for gta_prefill_masked_attention.
+ *   mode PREFIX_DECODE: for gta_prefix_decode_attention; total_tokens = prefix->max_seq, max_len = cache->max_seq.
  * Returns 0 if cfg is NULL or invalid. */
 GTA_API size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64_t total_tokens,
                            int32_t max_len, int32_t num_splits);
@@ -254,6 +302,25 @@ GTA_API int gta_qk_norm_rope(const gta_config *cfg, const void *q, int64_t q_str
                              const void *q_gain, const void *k_gain, float eps, const int32_t *positions,
                              int64_t total_tokens, void *q_out, void *k_out, void *hip_stream);
 
+/* Works a rotation out (on the host; no device is touched).  GTA_ERR_SHAPE for values outside what gta_rope_spec allows or
+ * frequencies that are not finite, GTA_ERR_DTYPE for an unknown layout or scaling, GTA_ERR_UNSUPPORTED for more than
+ * GTA_ROPE_MAX_PAIRS pairs.  Of cfg only the widths are read here and in gta_qk_rope, not rope and rope_base. */
+GTA_API int gta_make_rotation(const gta_config *cfg, const gta_rope_spec *spec, gta_rotation *out);
+
+/* Rotates every query and key head: (a, b) of pair j become m * (a cos t - b sin t, b cos t + a sin t), t = position * f_j, and
+ * with `transposed` 1 the same with -t: the gradient of the rotation, and with m = 1 its inverse.  Computed in fp32 and
+ * rounded once; sines as in gta_qk_norm_rope, for positions of either sign.  For models that rotate otherwise than
+ * gta_config's rope does: project with rope = 0, then call this.
+ *   q, k          device, rows of n_q*d_h and n_k*d_h elements, q_stride and k_stride elements apart; either may be NULL, with
+ *                 its output
+ *   positions     device [total_tokens], or NULL: 0 .. total_tokens - 1
+ *   q_out, k_out  device, rows q_out_stride and k_out_stride elements apart.  An output may be its own input with the same
+ *                 stride; otherwise outputs and inputs must not overlap
+ * All aligned to an element, strides at least the widths; rows of 16-byte aligned chunks run faster. */
+GTA_API int gta_qk_rope(const gta_config *cfg, const gta_rotation *rotation, const void *q, int64_t q_stride, const void *k,
+                        int64_t k_stride, const int32_t *positions, int64_t total_tokens, int32_t transposed, void *q_out,
+                        int64_t q_out_stride, void *k_out, int64_t k_out_stride, void *hip_stream);
+
 /* gta_cache_append for 8-bit caches: rows [cu_new[b], cu_new[b+1]) of k_new / c_new (element type =
  * cfg->dtype) are quantised (see gta_mx_cache) into slot slots[b] behind its seq_lens[slot] rows, then
  * seq_lens[slot] += their count.  A sequence that does not fit stores nothing and is flagged
@@ -330,6 +397,42 @@ GTA_API int gta_output_projection(const gta_config *cfg, const gta_weights *weig
 GTA_API int gta_prefill_attention(const gta_config *cfg, const void *q, const void *k, const void *c,
                                   const int32_t *cu_seqlens, int32_t batch, int64_t total_tokens,
                                   int32_t max_seqlen, void *l_out, void *hip_stream);
+
+/* gta_prefill_attention with rules for the scores (gta_score_rules): for every map group g and token i of a sequence
+ *   l_out[i, g*d_l : (g+1)*d_l] = sum_j Softmax_j(rule(q_g[i] . k_{k(g)}[j])) c_{c(g)}[j]   over the keys j that i sees.
+ * first, last [total_tokens] and positions count from 0 within a sequence.  Causal: both NULL.  Packed documents: first = start
+ * of the token's document.  A prefix seen from everywhere: last = max(i, prefix - 1).  A window of w: first = i - w + 1.
+ * Both directions: last = INT32_MAX.  Padding: first > last, a row of zeros.
+ *   q, k, c  device, rows of n_q*d_h, n_k*d_h and n_c*d_l elements (element type = cfg->dtype), q_stride, k_stride and c_stride
+ *            elements apart: columns of one wide projection's output will do.  Aligned to an element
+ *   cu_seqlens, batch, total_tokens, max_seqlen  as for gta_prefill.  Rows of l_out behind the last sequence are left as they are
+ *   l_out    device [total_tokens, n_q*d_l], dense, 16-byte aligned; must not overlap the inputs
+ *   workspace  mode PREFILL_MASKED
+ * Sums and softmax statistics are fp32.  head_dim up to 1024, latent_dim up to 4096 (GTA_ERR_UNSUPPORTED).  Runs on the matrix
+ * instructions where gta_uses_tuned_kernels(cfg, GTA_MODE_PREFILL_MASKED) is 1, rows consist of 16-byte aligned chunks and a
+ * sequence's key / latent rows stay below 2 GiB, on a general kernel otherwise. */
+GTA_API int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                                         const void *c, int64_t c_stride, const int32_t *cu_seqlens, int32_t batch,
+                                         int64_t total_tokens, int32_t max_seqlen, const gta_score_rules *rules, void *l_out,
+                                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Attention of one new token per sequence over a prefix that the whole batch shares, read once for all, and over the sequence's
+ * own cached rows behind it (the token's own row appended before, e.g. by gta_cache_append):
+ *   l_out[b, g*d_l : (g+1)*d_l] = sum_j Softmax_j(rule(q_g . k_{k(g)}[j])) c_{c(g)}[j]
+ * over j = 0 .. P-1, the rows of slot prefix_slot of `prefix`, and P .. P+n-1, the n = seq_lens[slot] rows of the sequence's slot in
+ * `cache`; both lengths are read on the device.  The token's position is P + n - 1.
+ *   q [batch, n_q*d_h] queries, rotated at their positions, l_out [batch, n_q*d_l]; device, element type = cfg->dtype
+ *   prefix     caches of the same widths; may be `cache` itself (nothing is written to either)
+ *   slots      device [batch] or NULL for slot b = b; a sequence whose slot is out of range has no rows of its own
+ *   rules      first, last [batch], over positions 0 .. P+n-1 (first = P: without the prefix)
+ *   workspace  mode PREFIX_DECODE
+ * A sequence that sees no row gets zeros.  l_out goes on into gta_prefill_decoder.  head_dim up to 1024, latent_dim up to 4096,
+ * max_seq of each cache up to 2^30 (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where
+ * gta_uses_tuned_kernels(cfg, GTA_MODE_PREFIX_DECODE) is 1 and pages, if any, are of a power of two of at least 16 rows, on a
+ * general kernel otherwise. */
+GTA_API int gta_prefix_decode_attention(const gta_config *cfg, const void *q, const gta_cache *prefix, int32_t prefix_slot,
+                                        const gta_cache *cache, const int32_t *slots, int32_t batch, const gta_score_rules *rules,
+                                        void *l_out, void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /* Split-K attention stage of the decode step (App. B.1.3) over the seq_lens[slot] rows ALREADY in
  * the caches (nothing is appended): leaves one un-normalised partial (accumulator, running max,

@@ -18,16 +18,20 @@ GTA_GATE_SIGMOID, GTA_GATE_OFF, GTA_GATE_SILU, GTA_GATE_RELU2 = 0, 1, 2, 3
 GATE_CODES = {True: GTA_GATE_SIGMOID, "sigmoid": GTA_GATE_SIGMOID, False: GTA_GATE_OFF, "off": GTA_GATE_OFF,
               "silu": GTA_GATE_SILU, "relu2": GTA_GATE_RELU2}
 GTA_MODE_PREFILL, GTA_MODE_DECODE, GTA_MODE_PREFILL_CHUNK, GTA_MODE_MX_DECODE = 0, 1, 2, 3
+GTA_MODE_PREFILL_MASKED, GTA_MODE_PREFIX_DECODE = 4, 5
 GTA_OK = 0
 GTA_ERR_NULL, GTA_ERR_SHAPE, GTA_ERR_ALIGN, GTA_ERR_DTYPE = -1, -2, -3, -4
 GTA_ERR_UNSUPPORTED, GTA_ERR_WORKSPACE, GTA_ERR_HIP, GTA_ERR_CACHE_FULL = -5, -6, -7, -8
 
 GTA_STATIC_SCRATCH_BYTES = 32 << 20
 GTA_MX_BLOCK = 32
+GTA_ROPE_MAX_PAIRS = 256
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3, "given": 4}
 EXPORTS = ["gta_workspace_bytes", "gta_prefill", "gta_prefill_chunk", "gta_decode", "gta_decode_static", "gta_cache_append", "gta_strerror",
            "gta_uses_tuned_kernels", "gta_prefill_projection", "gta_prefill_decoder", "gta_output_projection", "gta_prefill_attention", "gta_decode_attention", "gta_decode_combine", "gta_calibration_copy",
            "gta_calibration_read", "gta_calibration_mfma", "gta_qk_norm_rope", "gta_mx_cache_append", "gta_mx_cache_read",
-           "gta_mx_decode_attention"]
+           "gta_mx_decode_attention", "gta_make_rotation", "gta_qk_rope", "gta_prefill_masked_attention", "gta_prefix_decode_attention"]
 
 
 class gta_config(ctypes.Structure):
@@ -53,6 +57,21 @@ class gta_mx_cache(ctypes.Structure):
                 ("seq_lens", ctypes.c_void_p), ("status", ctypes.c_void_p), ("max_batch", ctypes.c_int32),
                 ("max_seq", ctypes.c_int32), ("block_table", ctypes.c_void_p), ("page_size", ctypes.c_int32),
                 ("pages_per_slot", ctypes.c_int32), ("num_pages", ctypes.c_int32)]
+
+
+class gta_rope_spec(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_float),
+                ("factor", ctypes.c_float), ("trained_len", ctypes.c_float), ("slow_turns", ctypes.c_float),
+                ("fast_turns", ctypes.c_float), ("magnitude", ctypes.c_float), ("frequency", ctypes.c_void_p)]
+
+
+class gta_rotation(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("magnitude", ctypes.c_float),
+                ("reserved", ctypes.c_int32), ("turn", ctypes.c_uint64 * GTA_ROPE_MAX_PAIRS)]
+
+
+class gta_score_rules(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("first", ctypes.c_void_p), ("last", ctypes.c_void_p)]
 
 
 class GtaError(RuntimeError):
@@ -118,6 +137,15 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.gta_mx_cache_read.argtypes = [cfgp, mp, vp, vp, vp, i32, i32, vp, vp, vp]
     lib.gta_mx_decode_attention.restype = ctypes.c_int
     lib.gta_mx_decode_attention.argtypes = [cfgp, vp, mp, vp, i32, i32, vp, vp, sz, vp]
+    rp, sp = ctypes.POINTER(gta_rotation), ctypes.POINTER(gta_score_rules)
+    lib.gta_make_rotation.restype = ctypes.c_int
+    lib.gta_make_rotation.argtypes = [cfgp, ctypes.POINTER(gta_rope_spec), rp]
+    lib.gta_qk_rope.restype = ctypes.c_int
+    lib.gta_qk_rope.argtypes = [cfgp, rp, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp]
+    lib.gta_prefill_masked_attention.restype = ctypes.c_int
+    lib.gta_prefill_masked_attention.argtypes = [cfgp, vp, i64, vp, i64, vp, i64, vp, i32, i64, i32, sp, vp, vp, sz, vp]
+    lib.gta_prefix_decode_attention.restype = ctypes.c_int
+    lib.gta_prefix_decode_attention.argtypes = [cfgp, vp, cp, i32, cp, vp, i32, sp, vp, vp, sz, vp]
     lib.gta_strerror.restype = ctypes.c_char_p
     lib.gta_strerror.argtypes = [ctypes.c_int]
     lib.gta_uses_tuned_kernels.restype = ctypes.c_int
@@ -242,6 +270,50 @@ def _mx(device: int, cfg: gta_config, cache: Optional[gta_mx_cache]):
     if getattr(cache, "widths", widths) != widths:
         raise ValueError(f"cache of rows of {cache.widths}, config of {widths}")
     return ctypes.byref(cache)
+
+
+def make_rotation(cfg: gta_config, *, layout="half", rotary_dim: int = 0, base: float = 10000.0, scaling="plain", factor: float = 1.0,
+                  trained_len: float = 0.0, slow_turns: float = 0.0, fast_turns: float = 0.0, magnitude: float = 1.0,
+                  frequencies=None) -> gta_rotation:
+    """What gta_qk_rope turns by (gta_rope_spec in include/gta.h); frequencies: radians per position of every pair, with
+    scaling="given"."""
+    given, at = None, None
+    if frequencies is not None:
+        pairs = (rotary_dim or cfg.head_dim) // 2
+        given = (ctypes.c_double * len(frequencies))(*(float(f) for f in frequencies))
+        if len(given) != pairs:
+            raise ValueError(f"{len(given)} frequencies for {pairs} pairs")
+        at = ctypes.addressof(given)
+    spec = gta_rope_spec(ROPE_LAYOUTS.get(layout, layout), rotary_dim, ROPE_SCALINGS.get(scaling, scaling), base, factor, trained_len,
+                         slow_turns, fast_turns, magnitude, at)
+    out = gta_rotation()
+    _check(load().gta_make_rotation(ctypes.byref(cfg), ctypes.byref(spec), ctypes.byref(out)), "gta_make_rotation")
+    return out
+
+
+def make_score_rules(*, cap: float = 0.0, slopes=None, first=None, last=None) -> gta_score_rules:
+    """cap of the scores, slopes fp32 [n_q] of the distance's bias, first / last int32 per token: what it sees (device tensors)."""
+    import torch
+    parts = {"slopes": (slopes, torch.float32), "first": (first, torch.int32), "last": (last, torch.int32)}
+    for name, (t, kind) in parts.items():
+        if t is not None and (t.dtype != kind or not t.is_contiguous()):
+            raise ValueError(f"{name} is {t.dtype}, {'' if t.is_contiguous() else 'not '}contiguous")
+    rules = gta_score_rules(cap, _ptr(slopes), _ptr(first), _ptr(last))
+    rules.tensors = {name: t for name, (t, _) in parts.items() if t is not None}   # kept alive with the struct
+    return rules
+
+
+def _rules(device: int, cfg: gta_config, rules: Optional[gta_score_rules], tokens: int):
+    """The rules as the library takes them, if their arrays are on the current device and of the call's sizes (one whose fields the
+    caller filled in is taken as it is)."""
+    if rules is None:
+        return None
+    for name, t in getattr(rules, "tensors", {}).items():
+        need = cfg.n_qgroups if name == "slopes" else tokens
+        if t.numel() < need:
+            raise ValueError(f"{name} has {t.numel()} entries for {need}")
+        _on(device, t)
+    return ctypes.byref(rules)
 
 
 def _check(rc: int, where: str) -> None:
@@ -414,6 +486,43 @@ def gta_mx_decode_attention(cfg: gta_config, q, cache: gta_mx_cache, slots, batc
                                         _stream(stream))
     if check:
         _check(rc, "gta_mx_decode_attention")
+    return rc
+
+
+def gta_qk_rope(cfg: gta_config, rotation: gta_rotation, q, q_stride: int, k, k_stride: int, positions, total_tokens: int,
+                transposed: bool, q_out, q_out_stride: int, k_out, k_out_stride: int, stream=None, check: bool = True) -> int:
+    d = _device()
+    rc = load().gta_qk_rope(ctypes.byref(cfg), ctypes.byref(rotation), _on(d, q), q_stride, _on(d, k), k_stride, _on(d, positions),
+                            total_tokens, int(transposed), _on(d, q_out), q_out_stride, _on(d, k_out), k_out_stride, _stream(stream))
+    if check:
+        _check(rc, "gta_qk_rope")
+    return rc
+
+
+def gta_prefill_masked_attention(cfg: gta_config, q, q_stride: int, k, k_stride: int, c, c_stride: int, cu_seqlens, batch: int,
+                                 total_tokens: int, max_seqlen: int, rules: Optional[gta_score_rules], l_out, workspace, stream=None,
+                                 check: bool = True) -> int:
+    d = _device()
+    rc = load().gta_prefill_masked_attention(ctypes.byref(cfg), _on(d, q), q_stride, _on(d, k), k_stride, _on(d, c), c_stride,
+                                             _on(d, cu_seqlens), batch, total_tokens, max_seqlen, _rules(d, cfg, rules, total_tokens),
+                                             _on(d, l_out), _on(d, workspace),
+                                             0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                             _stream(stream))
+    if check:
+        _check(rc, "gta_prefill_masked_attention")
+    return rc
+
+
+def gta_prefix_decode_attention(cfg: gta_config, q, prefix: gta_cache, prefix_slot: int, cache: gta_cache, slots, batch: int,
+                                rules: Optional[gta_score_rules], l_out, workspace, stream=None, check: bool = True) -> int:
+    d = _device()
+    rc = load().gta_prefix_decode_attention(ctypes.byref(cfg), _on(d, q), ctypes.byref(prefix) if prefix is not None else None,
+                                            prefix_slot, ctypes.byref(cache) if cache is not None else None, _on(d, slots), batch,
+                                            _rules(d, cfg, rules, batch), _on(d, l_out), _on(d, workspace),
+                                            0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                            _stream(stream))
+    if check:
+        _check(rc, "gta_prefix_decode_attention")
     return rc
 
 

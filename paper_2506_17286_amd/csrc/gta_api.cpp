@@ -6,6 +6,7 @@
 #include <algorithm>
 #include "gta_internal.h"
 #include "gta_mx.h"
+#include "gta_rules.h"
 #include "gta_tuned.h"
 
 namespace gta {
@@ -203,6 +204,12 @@ static int check_mx_cache(const gta_mx_cache *c) {
 // A row stride in elements: at least the width, and no product with a row number that leaves 64 bits.
 static bool bad_stride(int64_t stride, int width) { return stride < width || stride > ((int64_t)1 << 28); }
 
+static int check_rules(const gta_score_rules *r) {
+  if (!r) return GTA_OK;
+  if (!(r->cap >= 0.f) || !(r->cap <= 3e38f)) return GTA_ERR_SHAPE;
+  return (((uintptr_t)r->slopes | (uintptr_t)r->first | (uintptr_t)r->last) & 3u) ? GTA_ERR_ALIGN : GTA_OK;
+}
+
 static const int kMaxBatch = 65535;  // grid.y / grid.z limit
 
 // ---- fixed scratch of gta_decode_static ---------------------------------------------------------
@@ -275,6 +282,7 @@ int gta_uses_tuned_kernels(const gta_config *cfg, int mode) {
   if (mode == GTA_MODE_DECODE) return tuned_decode_supported(d) ? 1 : 0;
   if (mode == GTA_MODE_PREFILL_CHUNK) return tuned_prefill_chunk_supported(d, 1) ? 1 : 0;   // up to the cache-size limit
   if (mode == GTA_MODE_MX_DECODE) return !mx_decode_dims_ok(d) ? GTA_ERR_UNSUPPORTED : mx_decode_tuned(d) ? 1 : 0;   // up to the page size
+  if (mode == GTA_MODE_PREFILL_MASKED || mode == GTA_MODE_PREFIX_DECODE) return rules_dims_ok(d) ? 0 : GTA_ERR_UNSUPPORTED;
   return GTA_ERR_DTYPE;
 }
 
@@ -297,6 +305,10 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
   if (mode == GTA_MODE_MX_DECODE) {
     if (!mx_decode_dims_ok(d) || num_splits < 0) return 0;
     return mx_decode_bytes(d, batch, max_len, num_splits) + 256;
+  }
+  if (mode == GTA_MODE_PREFILL_MASKED || mode == GTA_MODE_PREFIX_DECODE) {
+    if (!rules_dims_ok(d) || total_tokens < 0) return 0;
+    return 256;
   }
   if (mode == GTA_MODE_DECODE) {
     int splits = choose_splits(d, batch, max_len, num_splits);
@@ -497,6 +509,76 @@ int gta_qk_norm_rope(const gta_config *cfg, const void *q, int64_t q_stride, con
   if (total_tokens == 0) return GTA_OK;
   return launch_qk_norm_rope(d, q, q_stride, k, k_stride, q_gain, k_gain, eps, positions, total_tokens, q_out, k_out,
                              (hipStream_t)hip_stream);
+}
+
+int gta_make_rotation(const gta_config *cfg, const gta_rope_spec *spec, gta_rotation *out) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!spec || !out) return GTA_ERR_NULL;
+  return make_rotation(d, *spec, out);
+}
+
+int gta_qk_rope(const gta_config *cfg, const gta_rotation *rotation, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                const int32_t *positions, int64_t total_tokens, int32_t transposed, void *q_out, int64_t q_out_stride, void *k_out,
+                int64_t k_out_stride, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!rotation || (!q && !k) || !q != !q_out || !k != !k_out) return GTA_ERR_NULL;
+  if ((rotation->layout != GTA_ROPE_HALF && rotation->layout != GTA_ROPE_INTERLEAVED) || (transposed != 0 && transposed != 1)) return GTA_ERR_DTYPE;
+  const int r = rotation->rotary_dim;
+  if (r <= 0 || r % 2 || r > d.dh || r > 2 * GTA_ROPE_MAX_PAIRS || !(rotation->magnitude > 0.f) || !(rotation->magnitude <= 3e38f))
+    return GTA_ERR_SHAPE;
+  if (total_tokens < 0 || total_tokens > INT32_MAX) return GTA_ERR_SHAPE;
+  if ((q && (bad_stride(q_stride, d.wq_w) || bad_stride(q_out_stride, d.wq_w))) ||
+      (k && (bad_stride(k_stride, d.wk_w) || bad_stride(k_out_stride, d.wk_w))))
+    return GTA_ERR_SHAPE;
+  if ((q && q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride)) return GTA_ERR_SHAPE;   // rows would overlap
+  const uintptr_t el = (uintptr_t)d.esize() - 1;
+  if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out) & el) || ((uintptr_t)positions & 3u)) return GTA_ERR_ALIGN;
+  if (total_tokens * (int64_t)(d.nq + d.nk) > ((int64_t)1 << 31)) return GTA_ERR_UNSUPPORTED;   // launch size
+  if (total_tokens == 0) return GTA_OK;
+  return launch_qk_rope(d, *rotation, q, q_stride, k, k_stride, positions, total_tokens, transposed != 0, q_out, q_out_stride, k_out,
+                        k_out_stride, (hipStream_t)hip_stream);
+}
+
+int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride, const void *c,
+                                 int64_t c_stride, const int32_t *cu_seqlens, int32_t batch, int64_t total_tokens, int32_t max_seqlen,
+                                 const gta_score_rules *rules, void *l_out, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!q || !k || !c || !l_out) return GTA_ERR_NULL;
+  if (!rules_dims_ok(d) || d.nq > 65535) return GTA_ERR_UNSUPPORTED;
+  if (batch <= 0 || batch > kMaxBatch || total_tokens < 0 || total_tokens > INT32_MAX || max_seqlen < 0) return GTA_ERR_SHAPE;
+  if (!cu_seqlens && (total_tokens % batch != 0 || total_tokens / batch > max_seqlen)) return GTA_ERR_SHAPE;
+  if (bad_stride(q_stride, d.wq_w) || bad_stride(k_stride, d.wk_w) || bad_stride(c_stride, d.wc_w)) return GTA_ERR_SHAPE;
+  if ((rc = check_rules(rules)) != GTA_OK) return rc;
+  const uintptr_t el = (uintptr_t)d.esize() - 1;
+  if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)c) & el) || misaligned(l_out) || ((uintptr_t)cu_seqlens & 3u)) return GTA_ERR_ALIGN;
+  if (total_tokens == 0 || max_seqlen == 0) return GTA_OK;
+  if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
+  const MaskedArgs m{q, k, c, q_stride, k_stride, c_stride, cu_seqlens, batch, total_tokens, max_seqlen, rules_of(d, rules), l_out};
+  return launch_masked_any(d, m, (hipStream_t)hip_stream);
+}
+
+int gta_prefix_decode_attention(const gta_config *cfg, const void *q, const gta_cache *prefix, int32_t prefix_slot, const gta_cache *cache,
+                                const int32_t *slots, int32_t batch, const gta_score_rules *rules, void *l_out, void *workspace,
+                                size_t workspace_bytes, void *hip_stream) {
+  Dims d;
+  int rc = make_dims(cfg, &d);
+  if (rc != GTA_OK) return rc;
+  if (!q || !prefix || !cache || !l_out) return GTA_ERR_NULL;
+  if ((rc = check_cache(prefix)) != GTA_OK || (rc = check_cache(cache)) != GTA_OK) return rc;
+  if (!rules_dims_ok(d) || d.nq > 65535 || prefix->max_seq > (1 << 30) || cache->max_seq > (1 << 30)) return GTA_ERR_UNSUPPORTED;
+  if (batch <= 0 || batch > kMaxBatch || (!slots && batch > cache->max_batch)) return GTA_ERR_SHAPE;
+  if (prefix_slot < 0 || prefix_slot >= prefix->max_batch) return GTA_ERR_SHAPE;
+  if ((rc = check_rules(rules)) != GTA_OK) return rc;
+  if (misaligned(q) || misaligned(l_out) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
+  if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
+  const PrefixArgs p{q, view_of(prefix, nullptr), view_of(cache, slots), prefix_slot, batch, rules_of(d, rules), l_out};
+  return launch_prefix_any(d, p, (hipStream_t)hip_stream);
 }
 
 int gta_mx_cache_append(const gta_config *cfg, const gta_mx_cache *cache, const int32_t *slots, const void *k_new,

@@ -86,4 +86,14 @@ __device__ __forceinline__ float2 rope_cos_sin_turn(int p, uint64_t turn) {
   return make_float2((q + 1) & 2 ? -b : b, q & 2 ? -a : a);
 }
 
+// The same from all 64 bits, with the series of rope_cos_sin: rounded once from fp64, for fp32 rows.
+__device__ __forceinline__ float2 rope_cos_sin_turn_f64(int p, uint64_t turn) {
+  const uint64_t f = (uint64_t)(int64_t)p * turn, q = (f + 0x2000000000000000ull) >> 62;
+  const double x = (double)(int64_t)(f - (q << 62)) * 3.4061215800865545e-19, y = x * x;   // 2 pi / 2^64
+  const double s = fma(x * y, fma(y, fma(y, fma(y, fma(y, -1. / 39916800., 1. / 362880.), -1. / 5040.), 1. / 120.), -1. / 6.), x);
+  const double c = fma(y, fma(y, fma(y, fma(y, fma(y, fma(y, 1. / 479001600., -1. / 3628800.), 1. / 40320.), -1. / 720.), 1. / 24.), -0.5), 1.);
+  const float a = (float)(q & 1 ? c : s), b = (float)(q & 1 ? s : c);
+  return make_float2((q + 1) & 2 ? -b : b, q & 2 ? -a : a);
+}
+
 }  // namespace gta

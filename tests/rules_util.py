@@ -1,0 +1,155 @@
+"""Plain float64 forms of the rotation and of attention with rules on its scores, with the errors that fp32 arithmetic and the
+roundings of the kernels may make, element by element."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import torch
+
+from paper_2506_17286_amd import binding as B
+
+HALF_STEP = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}   # largest rounding error relative to the value
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+INT_MAX = 2 ** 31 - 1
+
+
+def shape(nq, nk, nc, dh, dl):
+    return dict(d_model=256, n_heads=nq, n_qgroups=nq, n_kgroups=nk, n_cgroups=nc, head_dim=dh, latent_dim=dl)
+
+
+# layers that take different kernels: the paper's, the 1B shape, the wide one, shared keys and several latents, other widths
+SHAPES = {
+    "paper": shape(5, 1, 1, 64, 128), "paper768": shape(3, 1, 1, 64, 128), "1b": shape(4, 4, 1, 128, 512), "wide": shape(8, 8, 1, 128, 1024),
+    "c2": shape(6, 1, 2, 64, 128), "q8k4c2": shape(8, 4, 2, 128, 512), "q6k2c3": shape(6, 2, 3, 64, 64), "l256": shape(4, 2, 1, 128, 256),
+    "l128": shape(2, 1, 2, 128, 128), "l192": shape(3, 3, 1, 64, 192), "maps20": shape(20, 1, 1, 64, 128), "maps40": shape(40, 4, 1, 64, 128),
+    "h32": shape(4, 2, 1, 32, 64), "odd": shape(6, 3, 2, 20, 44), "h96": shape(2, 1, 1, 96, 160), "mha": shape(4, 4, 4, 64, 64),
+}
+
+
+def config(name, dtype, **kw):
+    return B.make_config(dtype=dtype, **SHAPES[name], **kw)
+
+
+# ------------------------------------------------------------------------------------------ rotation
+def frequencies(r, scaling="plain", base=10000.0, factor=1.0, trained_len=0.0, slow_turns=0.0, fast_turns=0.0, given=None):
+    """Radians per position, pair by pair, in extended precision."""
+    L = np.longdouble
+    j = np.arange(r // 2).astype(L)
+    if scaling == "given":
+        return np.asarray(given, dtype=np.float64).astype(L)
+    f = np.exp(-2 * j / r * np.log(L(base)))
+    if scaling == "linear":
+        f = f / L(factor)
+    elif scaling == "base":
+        f = np.exp(-2 * j / r * (np.log(L(base)) + np.log(L(factor)) * r / (r - 2)))
+    elif scaling == "bands":
+        turns = L(trained_len) * f / (2 * L(np.pi) + L(2.4492935982947064e-16))   # 2 pi to 2^-64 and better
+        kept = np.clip((turns - L(slow_turns)) / (L(fast_turns) - L(slow_turns)), 0, 1)
+        f = (1 - kept) * f / L(factor) + kept * f
+    return f
+
+
+def rotate(x, heads, dh, r, freq, positions, interleaved, transposed, magnitude=1.0):
+    """x [tokens, heads * dh] float64 -> rotated, and what the kernels' fp32 arithmetic may be off by (before the last rounding), in
+    units of (|a| + |b|) m of each element's pair."""
+    ang = positions.astype(np.longdouble)[:, None] * freq[None, :]
+    cos, sin = np.cos(ang).astype(np.float64)[:, None, :], np.sin(ang).astype(np.float64)[:, None, :]
+    if transposed:
+        sin = -sin
+    v = x.reshape(-1, heads, dh)
+    y, size = v.copy(), np.zeros_like(v)
+    lo, hi = (slice(0, r, 2), slice(1, r, 2)) if interleaved else (slice(0, r // 2), slice(r // 2, r))
+    a, b = v[..., lo], v[..., hi]
+    y[..., lo], y[..., hi] = magnitude * (a * cos - b * sin), magnitude * (b * cos + a * sin)
+    size[..., lo] = size[..., hi] = (np.abs(a) + np.abs(b)) * magnitude
+    return y.reshape(x.shape), size.reshape(x.shape)
+
+
+# ------------------------------------------------------------------------------------------ attention
+def attend(cfg, q, k, c, own, lo, hi, cap=0.0, slopes=None):
+    """Queries [m, nq*dh] at positions own [m] over rows k [n, nk*dh], c [n, nc*dl], seeing keys lo .. hi [m]; float64 tensors.
+    Returns the averages [m, nq*dl], the averages of |c| and the scores' sizes (what fp32 sums may be off by, in units of 2^-24)."""
+    nq, nk, nc, dh, dl = cfg.n_qgroups, cfg.n_kgroups, cfg.n_cgroups, cfg.head_dim, cfg.latent_dim
+    scale = cfg.softmax_scale or 1 / math.sqrt(dh)
+    m, n = q.shape[0], k.shape[0]
+    j = torch.arange(n, device=q.device)
+    seen = (j[None, :] >= lo[:, None]) & (j[None, :] <= hi[:, None])
+    out, mean_abs = torch.zeros((m, nq * dl), dtype=torch.float64, device=q.device), torch.zeros((m, nq * dl), dtype=torch.float64, device=q.device)
+    off = torch.zeros((m, nq), dtype=torch.float64, device=q.device)
+    rows = seen.any(dim=1)
+    if n == 0 or not bool(rows.any()):
+        return out, mean_abs, off
+    for g in range(nq):
+        kg, cg = k[:, g * nk // nq * dh:][:, :dh], c[:, g * nc // nq * dl:][:, :dl]
+        qg = q[:, g * dh:(g + 1) * dh]
+        s = qg @ kg.T.contiguous() * scale
+        size = qg.abs() @ kg.abs().T.contiguous() * scale * (dh + 4)
+        if cap:
+            s = cap * torch.tanh(s / cap)
+            size = size + 4 * cap
+        if slopes is not None:
+            bias = slopes[g].double() * (own[:, None] - j[None, :]).abs().double()
+            s, size = s - bias, size + 4 * bias.abs()
+        size = size + 8 * s.abs()          # the factor log2(e), the difference from the maximum, the exponential
+        s = torch.where(seen, s, -math.inf)
+        p = torch.softmax(s, dim=1)
+        p[~rows] = 0
+        cz = torch.where(torch.isnan(cg) | torch.isinf(cg), 0.0, cg) if not torch.isfinite(cg).all() else cg
+        o = p @ cz
+        if cz is not cg:                   # what is not finite reaches the rows that see it
+            for at in torch.nonzero(~torch.isfinite(cg).all(dim=1)).flatten().tolist():
+                w = torch.where(seen[:, at], p[:, at], 0.0)
+                bad = torch.where(torch.isfinite(cg[at]), 0.0, cg[at])
+                o = torch.where(seen[:, at][:, None] & (bad != 0)[None, :], o + w[:, None] * bad[None, :], o)
+        cols = slice(g * dl, (g + 1) * dl)
+        out[:, cols], mean_abs[:, cols] = o, p @ cz.abs()
+        # a score that is off by size 2^-24 has a weight off by that factor's exponential: keys that no such factor brings to 1e-12
+        # do not matter, however large their scores
+        matters = p.log() + size * 2.0 ** -24 > math.log(1e-12)
+        off[:, g] = torch.where(matters & seen, size, 0.0).amax(dim=1)
+    out[~rows] = 0
+    return out, mean_abs, off
+
+
+def tolerance(cfg, dtype, out, mean_abs, off, keys):
+    """Elementwise bound.  The result's own rounding; weights of 16 bits (half a step each in the sum, and in what it is divided by);
+    scores off by `off` 2^-24 change a weight by that factor, above and below the line; fp32 sums over `keys` terms."""
+    dl, e = cfg.latent_dim, 2.0 ** -24
+    h = HALF_STEP[dtype]
+    weights = 2 * 2.0 ** -8 if dtype == "bf16" else 0.0
+    return h * out.abs() + (weights + 2 * e * (off.repeat_interleave(dl, dim=1) + keys + 8)) * mean_abs * 1.05 + 1e-30
+
+
+def check(cfg, dtype, got, out, mean_abs, off, keys, what=""):
+    """Element by element.  Scores that fp32 leaves open (off by a tenth and more, where products are so large that their sums cancel
+    or pass its range) say nothing about the result: such maps of a row are left out."""
+    got = got.double()
+    open_ = (off * 2.0 ** -24 >= 0.1).repeat_interleave(cfg.latent_dim, dim=1)
+    got, out = torch.where(open_, 0.0, got), torch.where(open_, 0.0, out)
+    fin = torch.isfinite(out)
+    assert bool((torch.isfinite(got) == fin).all()), f"{what}: finite where the formula is not, or the other way round"
+    bad = torch.isnan(out)
+    assert bool((torch.isnan(got) == bad).all()), f"{what}: NaN"
+    inf = torch.isinf(out)
+    assert bool((got[inf] == out[inf]).all()), f"{what}: infinities"
+    diff, tol = (got - out).abs()[fin], tolerance(cfg, dtype, out, mean_abs, off, keys)[fin]
+    if diff.numel() == 0:
+        return
+    worst = (diff / tol).max().item()
+    assert worst <= 1, f"{what}: {worst:.2f} of the bound, largest difference {diff.max().item():.3e}"
+    size = out[fin].square().mean().sqrt().item()
+    rms = diff.square().mean().sqrt().item()
+    # roundings are even over their range: a result's and a weight's half step are 1 / sqrt(3) of it at most each
+    assert rms <= (5e-3 if dtype == "bf16" else 1e-5) * max(size, 1e-30), f"{what}: rel rms {rms / max(size, 1e-30):.2e}"
+
+
+def rows(gen, n, width, dtype, scale=1.0):
+    x = torch.empty((n, width), dtype=torch.float32, device="cuda").normal_(0.0, 1.0, generator=gen) * scale
+    return x.to(DT[dtype])
+
+
+def generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
