@@ -4,7 +4,9 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
+#include "gta_mx.h"
 #include "gta_rope.h"
 #include "gta_rules.h"
 
@@ -46,6 +48,107 @@ __global__ __launch_bounds__(256) void rope_any_kernel(RopeArgs a, gta_rotation 
     if (x != y)
       for (int j = a.r + lane; j < a.dh; j += 64) y[j] = x[j];
   }
+}
+
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+__device__ __forceinline__ f32x8 load8(const __bf16 *p) { return __builtin_convertvector(*reinterpret_cast<const bf16x8 *>(p), f32x8); }
+__device__ __forceinline__ f32x8 load8(const float *p) {
+  return __builtin_shufflevector(*reinterpret_cast<const f32x4 *>(p), *reinterpret_cast<const f32x4 *>(p + 4), 0, 1, 2, 3, 4, 5, 6, 7);
+}
+template <bool NT>
+__device__ __forceinline__ void store8(__bf16 *p, const f32x8 &v) { store16<NT>(reinterpret_cast<bf16x8 *>(p), __builtin_convertvector(v, bf16x8)); }
+template <bool NT>
+__device__ __forceinline__ void store8(float *p, const f32x8 &v) {
+  store16<NT>(reinterpret_cast<f32x4 *>(p), __builtin_shufflevector(v, v, 0, 1, 2, 3));
+  store16<NT>(reinterpret_cast<f32x4 *>(p + 4), __builtin_shufflevector(v, v, 4, 5, 6, 7));
+}
+
+template <int PAIRS> struct Turns { uint64_t at[PAIRS]; };
+
+// Heads and their turning parts in whole units of 16 elements, rows and rows' starts in whole 16 bytes.  A thread has one unit of
+// HEADS heads of a token: eight pairs, whose sines it works out once, or 16 elements to copy; loads and stores are 16 bytes.  Bound
+// by memory where there are many tokens, by the launch where there are few.
+template <typename T, int PAIRS, int HEADS, bool INTER, bool NT>
+__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, Turns<PAIRS> turns) {
+  const unsigned heads = a.q.heads + a.k.heads, groups = (heads + HEADS - 1) / HEADS, units = a.dh / 16, per = groups * units;
+  const unsigned item = blockIdx.x * 256 + threadIdx.x, row = item / per, rest = item - row * per, grp = rest / units, u = rest - grp * units;
+  const int64_t t = row;
+  if (t >= a.total) return;
+  const bool turns_here = (int)u * 16 < a.r;
+  const int lo = INTER || !turns_here ? u * 16 : u * 8, hi = INTER || !turns_here ? lo + 8 : lo + a.r / 2;
+  const int p = a.positions ? a.positions[t] : (int)t;
+  f32x8 x[HEADS], y[HEADS];
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = min(grp * HEADS + i, heads - 1), hk = h - a.q.heads;   // (a last group may be short: it repeats a head and stores nothing for it)
+    const T *in = hk < 0 ? (const T *)a.q.in + t * a.q.in_stride + h * a.dh : (const T *)a.k.in + t * a.k.in_stride + hk * a.dh;
+    x[i] = load8(in + lo);
+    y[i] = load8(in + hi);
+  }
+  f32x8 cs, sn;
+  if (turns_here) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float2 c = cos_sin(T(), p, turns.at[u * 8 + e]);
+      cs[e] = c.x * a.magnitude;
+      sn[e] = (a.back ? -c.y : c.y) * a.magnitude;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < HEADS; ++i) {
+    const int h = grp * HEADS + i, hk = h - a.q.heads;
+    if (h >= (int)heads) break;
+    T *out = hk < 0 ? (T *)a.q.out + t * a.q.out_stride + h * a.dh : (T *)a.k.out + t * a.k.out_stride + hk * a.dh;
+    f32x8 v = x[i], w = y[i];
+    if (turns_here) {
+      if constexpr (INTER) {   // v: pairs 0 .. 3, w: 4 .. 7
+        const f32x8 a0 = __builtin_shufflevector(v, w, 0, 2, 4, 6, 8, 10, 12, 14), b0 = __builtin_shufflevector(v, w, 1, 3, 5, 7, 9, 11, 13, 15);
+        const f32x8 a1 = a0 * cs - b0 * sn, b1 = b0 * cs + a0 * sn;
+        v = __builtin_shufflevector(a1, b1, 0, 8, 1, 9, 2, 10, 3, 11);
+        w = __builtin_shufflevector(a1, b1, 4, 12, 5, 13, 6, 14, 7, 15);
+      } else {
+        const f32x8 a0 = v;
+        v = a0 * cs - w * sn;
+        w = w * cs + a0 * sn;
+      }
+    }
+    store8<NT>(out + lo, v);
+    store8<NT>(out + hi, w);
+  }
+}
+
+template <typename T, int PAIRS>
+void launch_vector(const RopeArgs &a, const gta_rotation &r, hipStream_t st) {
+  Turns<PAIRS> turns;
+  for (int j = 0; j < PAIRS; ++j) turns.at[j] = r.turn[j];
+  const int heads = a.q.heads + a.k.heads;
+  auto run = [&](auto n, auto nt) {
+    constexpr int HEADS = decltype(n)::value;
+    constexpr bool NT = decltype(nt)::value;
+    const int64_t threads = a.total * ((heads + HEADS - 1) / HEADS) * (a.dh / 16);
+    const dim3 grid((unsigned)((threads + 255) / 256));
+    if (a.interleaved) rope_kernel<T, PAIRS, HEADS, true, NT><<<grid, 256, 0, st>>>(a, turns);
+    else rope_kernel<T, PAIRS, HEADS, false, NT><<<grid, 256, 0, st>>>(a, turns);
+  };
+  // few tokens: a head to a thread, so that its load is the only one waited for
+  if (a.total * heads * (a.dh / 16) < (1 << 17)) run(std::integral_constant<int, 1>{}, std::false_type{});
+  else if (stream_past_caches(a.total * heads * a.dh * sizeof(T))) run(std::integral_constant<int, 4>{}, std::true_type{});
+  else run(std::integral_constant<int, 4>{}, std::false_type{});
+}
+
+template <typename T>
+bool try_vector(const RopeArgs &a, const gta_rotation &r, hipStream_t st) {
+  const int64_t per = 16 / (int)sizeof(T);
+  if (a.dh % 16 || a.r % 16 || a.r > 512) return false;
+  if ((a.q.heads && (a.q.in_stride % per || a.q.out_stride % per)) || (a.k.heads && (a.k.in_stride % per || a.k.out_stride % per))) return false;
+  if (((uintptr_t)a.q.in | (uintptr_t)a.q.out | (uintptr_t)a.k.in | (uintptr_t)a.k.out) & 15u) return false;
+  if (a.total * (a.q.heads + a.k.heads) * (a.dh / 16) >= ((int64_t)1 << 32) - 256) return false;   // threads of a launch
+  if (a.r <= 64) launch_vector<T, 32>(a, r, st);
+  else if (a.r <= 128) launch_vector<T, 64>(a, r, st);
+  else launch_vector<T, 256>(a, r, st);
+  return true;
 }
 
 }  // namespace
@@ -91,6 +194,7 @@ int launch_qk_rope(const Dims &d, const gta_rotation &r, const void *q, int64_t 
                    int64_t k_out_stride, hipStream_t st) {
   const RopeArgs a{{q, q_out, q_stride, q_out_stride, q ? d.nq : 0}, {k, k_out, k_stride, k_out_stride, k ? d.nk : 0},
                    positions, total, d.dh, r.rotary_dim, r.layout == GTA_ROPE_INTERLEAVED, transposed, r.magnitude};
+  if (d.dtype == GTA_BF16 ? try_vector<__bf16>(a, r, st) : try_vector<float>(a, r, st)) return check_launch();
   const int64_t items = total * (a.q.heads + a.k.heads);
   const dim3 grid((unsigned)std::min<int64_t>((items + 3) / 4, 1 << 20));
   if (d.dtype == GTA_BF16) rope_any_kernel<__bf16><<<grid, 256, 0, st>>>(a, r);
