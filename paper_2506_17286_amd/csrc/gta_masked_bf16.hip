@@ -1,0 +1,751 @@
+// bf16 attention of rows of queries with rules on their scores (gta_score_rules), on matrix instructions:
+//   s = scale q . k,  capped by a tanh,  less slope * |distance|,  keys first .. last,  softmax,  times the latents.
+//
+// A workgroup has a tile of 128, 64 or 32 rows (gta_rows_attn.h) and 32 keys a step; both products are taken transposed, as
+//   S^T[key][row] = K Q^T,   L^T[column][row] += C^T P^T,
+// so that a row's statistics live in a pair of lanes, its weights go from the scores' accumulators into the second product
+// without leaving registers, and its slope, position and interval are scalars of a lane.  Key and latent tiles go from memory
+// straight into LDS through three stages.  Blocks go from the last one seen to the first: with a bias the largest scores come
+// first.  A wave skips the blocks none of its rows sees, masks those that some rows see, and takes the others, whose softmax is dealt
+// out between the matrix instructions, without looking at their maximum: weights refer to the maximum a row has, whatever their size,
+// and a row sum beyond 2^32 sends the wave through the full step.
+// Weights are rounded to bf16 for the second product (their sum is that of the rounded ones); everything else is fp32.
+//
+// A masked weight is 0, but 0 times a latent that is not finite is NaN: a wave whose sums are not finite in the end goes through
+// its rows once more, one by one, over the keys that each sees (wave_row).
+#include <math.h>
+
+#include <type_traits>
+
+#include "gta_lds_load.h"
+#include "gta_rows_attn.h"
+
+namespace gta {
+namespace {
+
+typedef __bf16 bf16;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+// QW groups of 32 rows times 4 / QW groups of columns, a wave each.  Layout of a tile in LDS: a load instruction fetches 1 KiB in
+// lane order, so rows that it fetches cannot be padded apart and it fetches rows that are not read together: keys a + K_INSTR i
+// with instruction a, 16 bytes further per a, every second i with its halves swapped (k_sel); latents 4 a + r with instruction
+// 4 b + r, 64 bytes further per r.  Reads then fall into different columns of banks, at one (keys: two) addresses a lane plus
+// constants.
+template <int DH_, int DLW_, int QW_>
+struct Tile {
+  static constexpr int DH = DH_, DLW = DLW_, QW = QW_, CG = 4 / QW, BK = 32, BQ = 32 * QW, NW = 4, NT = 256;
+  static constexpr int NDLB = DLW / 32 / CG;   // blocks of 32 columns of a wave
+  static constexpr int K_ROW = DH * 2, C_ROW = DLW * 2, K_CPR = K_ROW / 16, C_CPR = C_ROW / 16;
+  static constexpr int K_INSTR = BK * K_ROW / 1024, C_INSTR = BK * C_ROW / 1024, C_RPI = 1024 / C_ROW;
+  static constexpr int K_PITCH = 1024 + 16, C_PITCH = 1024 + 64, C_GROUP = 4 * C_PITCH;
+  static constexpr int K_BYTES = K_INSTR * K_PITCH, STAGE = K_BYTES + C_INSTR * C_PITCH, NSTAGE = 3;
+  static constexpr int OUT_PITCH = DLW * 2 + 16;
+  static constexpr int SMEM = NSTAGE * STAGE > BQ * OUT_PITCH ? NSTAGE * STAGE : BQ * OUT_PITCH;
+  static constexpr int BLOCKS = SMEM > 80 * 1024 ? 1 : DH == 64 && SMEM <= 53 * 1024 ? 3 : 2;   // workgroups of a CU
+  static_assert(K_INSTR >= NW && C_INSTR >= NW && C_RPI >= 1 && NDLB >= 1 && SMEM <= 160 * 1024, "tile");
+  __device__ static constexpr int k_sel(int i) { return K_CPR == 16 ? i & 1 : (i ^ (i >> 1)) & 1; }
+  __device__ static constexpr int c_row(int a) { return a / C_RPI * C_GROUP + a % C_RPI * C_ROW; }
+};
+
+constexpr float kLazyThreshold = 8.0f;          // log2 units
+constexpr float kRowSumLimit = 4294967296.0f;   // 2^32
+enum { kCap = 1, kBias = 2 };
+
+// f(0), .., f(N - 1) as constants: loops over the accumulators.  (Unrolled loops in their place leave accumulators of 256 columns
+// in memory: 4 x 4096 tokens of packed documents, 1B shape, 1600 us.)
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+#define EACH(i) [&](auto i) __attribute__((always_inline))
+
+__device__ __forceinline__ float pair_max(float v) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float v) {
+  const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ int wave_min(int v) {
+#pragma unroll
+  for (int i = 32; i; i >>= 1) v = min(v, __shfl_xor(v, i));
+  return __builtin_amdgcn_readfirstlane(v);
+}
+__device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
+
+// A scalar load, waited for in place: a vector load would make the compiler wait for every load in flight.
+__device__ __forceinline__ int load_uniform(const int32_t *p) {
+  int v;
+  asm volatile("s_load_dword %0, %1, 0x0\n\ts_waitcnt lgkmcnt(0)" : "=s"(v) : "s"(p));
+  return v;
+}
+
+// Row `tok`'s map g over keys lo .. hi by one wave, a key a lane for the scores, columns lane, lane + 64, .. of `cols` for the sums;
+// rows(j): pool row of key j.  Returns maximum and weight.
+template <int MODS, int COLS, class F>
+__device__ float2 wave_row(const RowsArgs &a, const bf16 *q, int dh, const bf16 *k, const bf16 *c, float slope, int own, int lo, int hi, F rows,
+                           float (&acc)[COLS]) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+  Rules r = a.rules;
+  if (!(MODS & kCap)) r.cap = 0.f;
+#pragma unroll 1
+  for (int64_t j0 = lo; j0 <= hi; j0 += 64) {
+    const int cnt = (int)min((int64_t)64, hi - j0 + 1);
+    float sc = -INFINITY;
+    int64_t row = 0;
+    if (lane < cnt) {
+      row = rows((int)j0 + lane);
+      const bf16 *kr = k + row * a.ks;
+      float dot = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < dh; ++i) dot = fmaf((float)kr[i], (float)q[i], dot);
+      sc = ruled_score(r, dot, slope, fabsf((float)(own - ((int)j0 + lane))));
+    }
+    float mx = sc;
+    for (int i = 32; i; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
+    const float mn = fmaxf(m, mx), ref = mn > -INFINITY ? mn : 0.f, corr = __builtin_amdgcn_exp2f(m - ref);
+    const float p = lane < cnt ? __builtin_amdgcn_exp2f(sc - ref) : 0.f;
+    float sum = p;
+    for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
+    m = mn;
+    l = fmaf(l, corr, sum);
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) acc[i] *= corr;
+#pragma unroll 1
+    for (int t = 0; t < cnt; ++t) {
+      const float pt = __shfl(p, t);
+      const int64_t at = ((int64_t)__shfl((int)(row >> 32), t) << 32) | (unsigned)__shfl((int)row, t);
+      const bf16 *cr = c + at * a.cs;
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) acc[i] = fmaf(pt, (float)cr[i * 64 + lane], acc[i]);
+    }
+  }
+  return make_float2(m, l);
+}
+
+template <class T, int MODS, bool CACHE>
+__global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ int span[8];
+  const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, ln = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = wave % T::QW, cg = wave / T::QW;
+  const int per = a.cells * a.slices;
+  int u, r;   // which tile (or piece), workgroup of it
+  if (a.tiles < 64) { u = (int)blockIdx.x / per; r = (int)blockIdx.x - u * per; }
+  else {   // eight tiles at a time, one per XCD: a tile's workgroups read the same keys and latents
+    const int at = (int)blockIdx.x >> 3, round = at / per;
+    r = at - round * per;
+    u = round * 8 + ((int)blockIdx.x & 7);
+  }
+  if (u >= a.tiles) return;
+  int b, tile, piece = 0, pieces = 1, slot = 0;
+  if constexpr (CACHE) {
+    b = 0; tile = u / a.pieces; piece = u - tile * a.pieces; pieces = a.pieces; slot = tile * a.pieces;
+  } else if (a.list) {
+    if (u >= load_uniform(a.count)) return;
+    const Piece *e = a.list + u;
+    b = load_uniform(&e->b); tile = load_uniform(&e->tile); piece = load_uniform(&e->piece); pieces = load_uniform(&e->pieces);
+    slot = load_uniform(&e->slot);
+  } else {
+    const int per_level = a.batch, lvl = u / per_level;
+    b = u - lvl * per_level; tile = a.tiles / a.batch - 1 - lvl;
+    if (tile < 0) return;
+  }
+  const int slice = r % a.slices, cell = r / a.slices;
+  int64_t start = 0;
+  int Tb = CACHE ? a.batch : a.per_seq, keys;
+  if constexpr (CACHE) keys = slot_rows(a.prefix, a.prefix_slot);
+  else {
+    start = (int64_t)b * a.per_seq;
+    if (a.cu) {
+      start = load_uniform(a.cu + b);
+      Tb = load_uniform(a.cu + b + 1) - (int)start;
+    }
+    keys = Tb;
+  }
+  const int R = Tb * a.mpc, r0 = tile * T::BQ;               // rows of the sequence, first of this tile
+  if (!CACHE && r0 >= R) return;
+  const int wr0 = r0 + qw * 32, row = min(wr0 + ln, R - 1);  // (rows past the last repeat it and are not stored)
+  const int tok = row / a.mpc, g = cell * a.mpc + (row - tok * a.mpc);
+  int lo, hi, own;
+  if constexpr (CACHE) prefix_seen(a, tok, keys, lo, hi, own);
+  else {
+    own = tok;
+    seen_by(a.rules, start + tok, tok, keys, lo, hi);
+  }
+  const float slope = MODS & kBias ? a.rules.slopes[g] : 0.f, slope2 = slope * kLog2e;
+  const bool sees = lo <= hi;
+  // blocks of 32 keys: those that some row of the wave sees (w0 .. w1), those that all of them see (i0 .. i1)
+  const bool idle = wr0 >= R;
+  const int wlo = wave_min(sees && !idle ? lo : INT_MAX), whi = wave_max(sees && !idle ? hi : -1);
+  const int ilo = wave_max(sees ? lo : 0), ihi = wave_min(sees ? hi : INT_MAX);
+  const int w0 = wlo == INT_MAX ? INT_MAX : wlo >> 5, w1 = whi >> 5;   // -1 >> 5 = -1: none
+  if (lane == 0) { span[wave] = w0; span[4 + wave] = w1; }
+  __syncthreads();
+  const int first = min(min(span[0], span[1]), min(span[2], span[3])), last = max(max(span[4], span[5]), max(span[6], span[7]));
+  const int blocks = __builtin_amdgcn_readfirstlane(last < 0 ? 0 : last - first + 1);
+  const int base = __builtin_amdgcn_readfirstlane(last < 0 ? 0 : first);
+  const int b0 = base + (int)((int64_t)blocks * piece / pieces), b1 = base + (int)((int64_t)blocks * (piece + 1) / pieces);
+  const int nsteps = b1 - b0;                                // step t: block b1 - 1 - t
+  const int ta = max(b1 - 1 - w1, 0), tb = w1 < 0 ? -1 : min(b1 - 1 - w0, nsteps - 1);   // this wave's steps
+
+  int64_t krow0 = start;
+  const int32_t *table = nullptr;
+  if constexpr (CACHE) {
+    krow0 = a.prefix.pm.table ? 0 : (int64_t)a.prefix_slot * a.prefix.max_seq;
+    if (a.prefix.pm.table) table = a.prefix.pm.table + (int64_t)a.prefix_slot * a.prefix.pm.pages_per_slot;
+  }
+  const bf16 *kcol = (const bf16 *)a.k + (cell / a.kdiv) * T::DH, *ccol = (const bf16 *)a.c + (int64_t)(cell / a.cdiv) * a.dl + slice * T::DLW;
+  const char *Kb = (const char *)(kcol + krow0 * a.ks), *Cb = (const char *)(ccol + krow0 * a.cs);
+  const unsigned wk2 = (unsigned)a.ks * 2, wc2 = (unsigned)a.cs * 2;
+  const float sc2 = a.rules.scale * kLog2e;                                   // score in units of log 2 without a cap
+  const float ck = a.rules.scale * a.rules.inv_cap, cap2 = a.rules.cap * kLog2e;
+
+  bf16x8 qf[T::DH / 16];
+  f32x16 acc[T::NDLB];
+  each<T::NDLB>(EACH(i) { acc[i] = f32x16{}; });
+  float m_run = -INFINITY, l_run = 0.f;
+
+  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  constexpr int KI = T::K_INSTR / T::NW, CI = T::C_INSTR / T::NW;
+  unsigned kv[KI], cv[CI];
+  {
+    const int i = lane / T::K_CPR;
+#pragma unroll
+    for (int j = 0; j < KI; ++j)
+      kv[j] = (wave + T::NW * j + T::K_INSTR * i) * wk2 + ((lane % T::K_CPR) ^ (T::k_sel(i) * (T::K_CPR / 2))) * 16;
+#pragma unroll
+    for (int j = 0; j < CI; ++j) {
+      const int q = wave + T::NW * j;
+      cv[j] = (4 * (q / 4 * T::C_RPI + lane / T::C_CPR) + q % 4) * wc2 + (lane % T::C_CPR) * 16;
+    }
+  }
+  unsigned fill = lds0;
+  int blk_next = b1 - 1;
+  // requests the next step; rows past the last key, and steps past the last, read as zeros
+  auto issue = [&]() __attribute__((always_inline)) {
+    const int j0 = blk_next * 32, rows = blk_next >= b0 ? min(keys - j0, 32) : 0;
+    const unsigned kbytes = rows > 0 ? (rows - 1) * wk2 + T::K_ROW : 0u, cbytes = rows > 0 ? (rows - 1) * wc2 + T::C_ROW : 0u;
+    if (CACHE && table) {   // two runs of 16 rows, each in one page
+      const int pages = a.prefix.pm.num_pages, end = max(keys - 1, 0) & ~15, jt = min(max(j0, 0), end), ju = min(jt + 16, end);
+      auto at = [&](int j) {
+        int pg = load_uniform(table + __builtin_amdgcn_readfirstlane(j >> a.ps_shift));
+        pg = (unsigned)pg >= (unsigned)pages ? 0 : pg;
+        return ((int64_t)pg << a.ps_shift) + (j & (a.prefix.pm.page_size - 1));
+      };
+      const int64_t p0 = at(jt), p1 = at(ju) - 16;
+      const u32x4 k0 = uniform_buffer_of(Kb + p0 * wk2, kbytes), k1 = uniform_buffer_of(Kb + p1 * wk2, kbytes);
+      const u32x4 c0 = uniform_buffer_of(Cb + p0 * wc2, cbytes), c1 = uniform_buffer_of(Cb + p1 * wc2, cbytes);
+#pragma unroll
+      for (int i = 0; i < KI; ++i) {
+        if (lane < 32) load_to_lds(k0, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
+        else load_to_lds(k1, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
+      }
+#pragma unroll
+      for (int i = 0; i < CI; ++i) {
+        const unsigned to = fill + T::K_BYTES + (wave + T::NW * i) * T::C_PITCH;
+        if constexpr (CI == 1) {
+          if (lane < 32) load_to_lds(c0, cv[i], to);
+          else load_to_lds(c1, cv[i], to);
+        } else load_to_lds(i < CI / 2 ? c0 : c1, cv[i], to);
+      }
+    } else {
+      const u32x4 rk = uniform_buffer_of(Kb + (int64_t)j0 * wk2, kbytes), rc = uniform_buffer_of(Cb + (int64_t)j0 * wc2, cbytes);
+#pragma unroll
+      for (int i = 0; i < KI; ++i) load_to_lds(rk, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
+#pragma unroll
+      for (int i = 0; i < CI; ++i) load_to_lds(rc, cv[i], fill + T::K_BYTES + (wave + T::NW * i) * T::C_PITCH);
+    }
+    --blk_next;
+    fill = fill == lds0 + (T::NSTAGE - 1) * T::STAGE ? lds0 : fill + T::STAGE;
+  };
+  auto wait_meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+  const int ksel = T::k_sel(ln / T::K_INSTR) * (T::K_ROW / 2);
+  const int koff = ln % T::K_INSTR * T::K_PITCH + ln / T::K_INSTR * T::K_ROW + h * 16;
+  const int koff_lo = koff + ksel, koff_hi = koff - ksel;
+  const int coff = T::K_BYTES + ((lane & 15) >> 2) * T::C_PITCH + h * (T::c_row(1) - T::c_row(0)) +
+                   (((lane >> 4) & 1) * 16 + (lane & 3) * 4) * 2 + cg * T::NDLB * 64;
+  auto c_frag = [&](int st, int mm, int dlb) {
+    const char *p = smem + (st + coff) + T::c_row(4 * mm) + dlb * 64;
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p));
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(p + T::c_row(2)));
+    const s16x8 c8 = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, c8);
+  };
+  auto k_frag = [&](int st, int ks) {
+    return *reinterpret_cast<const bf16x8 *>(smem + (st + (ks < T::DH / 32 ? koff_lo : koff_hi)) + ks * 32);
+  };
+  auto scores = [&](int st, f32x16 &s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    bf16x8 kf[T::DH / 16];
+#pragma unroll
+    for (int ks = 0; ks < T::DH / 16; ++ks) kf[ks] = k_frag(st, ks);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < T::DH / 16; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
+  };
+  // register e of a lane: key 8 (e / 4) + 4 h + e % 4 of its block
+  auto key_of = [](int e) { return 8 * (e >> 2) + (e & 3); };
+  // product to score, plus `plus`, in units of log 2; d0 = position less the block's first key less 4 h
+  auto score_of = [&](float s, int e, float d0, float plus) {
+    float base2 = plus;
+    if constexpr (MODS & kBias) base2 = fmaf(-slope2, fabsf(d0 - (float)key_of(e)), plus);
+    if constexpr (MODS & kCap) return fmaf(cap2, tanh_exactly(s * ck), base2);
+    else return fmaf(s, sc2, base2);
+  };
+  auto dist0 = [&](int blk) { return MODS & kBias ? (float)(own - blk * 32 - 4 * h) : 0.f; };
+  // the whole step for the scores of a block: rules, mask, running maximum, weights as the second product wants them
+  auto softmax = [&](const f32x16 &s, int blk, bool masked, bf16x8 (&pn)[2], float &corr) __attribute__((always_inline)) {
+    const float d0 = dist0(blk);
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = score_of(s[e], e, d0, 0.f);
+    if (masked) {
+      const int from = lo - blk * 32 - 4 * h, to = hi - blk * 32 - 4 * h;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = key_of(e) < from || key_of(e) > to ? -INFINITY : v[e];
+    }
+    float bm = fmaxf(v[0], v[1]);
+#pragma unroll
+    for (int e = 2; e < 16; e += 2) bm = fmaxf(fmaxf(v[e], v[e + 1]), bm);
+    const float m_cand = pair_max(bm), m_new = m_cand > m_run + kLazyThreshold ? fmaxf(m_run, m_cand) : m_run;
+    const float ref = m_new > -INFINITY ? m_new : 0.f;
+    corr = __builtin_amdgcn_exp2f(m_run - ref);
+    m_run = m_new;
+    const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+    float ps = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e += 2) {
+      bf16x2 pk;
+      pk[0] = (bf16)__builtin_amdgcn_exp2f(v[e] - ref);
+      pk[1] = (bf16)__builtin_amdgcn_exp2f(v[e + 1] - ref);
+      pn[e >> 3][e & 7] = pk[0]; pn[e >> 3][(e & 7) + 1] = pk[1];
+      ps = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, ps, false);   // the row sum uses the rounded values
+    }
+    l_run = fmaf(l_run, corr, ps);
+  };
+
+  bf16x8 pf[2] = {};
+  float corr = 1.f;
+  issue();
+  issue();
+  {
+    const bf16 *qg = (const bf16 *)a.q + (start + tok) * a.qs + g * T::DH + h * 8;
+#pragma unroll
+    for (int ks = 0; ks < T::DH / 16; ++ks) qf[ks] = *reinterpret_cast<const bf16x8 *>(qg + ks * 16);
+#pragma unroll
+    for (int ks = 0; ks < T::DH / 16; ++ks) asm volatile("" : "+v"(qf[ks]));   // waited for here and not in the loop
+  }
+  issue();
+  wait_meet();
+  auto interior = [&](int t) { const int j = (b1 - 1 - t) * 32; return j >= ilo && j + 31 <= ihi; };
+  auto mine = [&](int t) { return t >= ta && t <= tb; };
+  int cur = (T::NSTAGE - 1) * T::STAGE, nxt = 0;   // of step -1, which has the scores of block 0
+  auto rescale = [&]() {
+    if (__builtin_amdgcn_ballot_w64(corr != 1.f) != 0) {   // rare: the running maximum moved
+      each<T::NDLB>(EACH(i) { acc[i] *= corr; });
+    }
+  };
+  auto rotate = [&]() {
+    wait_meet();
+    cur = nxt;
+    nxt = nxt == (T::NSTAGE - 1) * T::STAGE ? 0 : nxt + T::STAGE;
+  };
+  // Steps whose next block all rows see: p0 <= t < p1 <= nsteps.  Every wave takes nsteps of them in all: they meet at each one's end.
+  const int p0 = max(ta, b1 - 2 - (ihi - 31 < 0 ? -1 : (ihi - 31) >> 5)), p1 = min(tb, b1 - 1 - ((ilo + 31) >> 5));
+  int t = -1;
+  // Steps before and behind them, and those of blocks that the wave skips.
+  auto plain_until = [&](int end) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (; t < end; ++t) {
+      const bool here = mine(t), next = mine(t + 1);
+      if (t > 0) issue();
+      if (here) rescale();
+      f32x16 s;
+      bf16x8 pn[2] = {};
+      if (next) {
+        scores(nxt, s);
+        softmax(s, b1 - 2 - t, !interior(t + 1), pn, corr);
+      }
+      if (here) {
+        each<2 * T::NDLB>(EACH(i) {
+          constexpr int mm = i / T::NDLB, dlb = i % T::NDLB;
+          acc[dlb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c_frag(cur, mm, dlb), pf[mm], acc[dlb], 0, 0, 0);
+        });
+      }
+      pf[0] = pn[0]; pf[1] = pn[1];
+      if (!here || !next) corr = 1.f;   // nothing to rescale yet, or nothing left
+      rotate();
+    }
+  };
+  plain_until(min(p0, nsteps));
+#pragma unroll 1
+  for (; t < p1; ++t) {
+    // The scores of block t + 1, then the second product of block t with the softmax of block t + 1 between its instructions;
+    // fragments are read a few instructions ahead of their use, and the scheduling barriers keep this order.
+    constexpr int KS = T::DH / 16, KS1 = KS / 2;
+    bf16x8 kf[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS1; ++ks) kf[ks] = k_frag(nxt, ks);
+    __builtin_amdgcn_sched_barrier(0);
+    if (t > 0) issue();
+    rescale();
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if (ks == 1) {
+#pragma unroll
+        for (int k2 = KS1; k2 < KS; ++k2) kf[k2] = k_frag(nxt, k2);
+      }
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    constexpr int NS = 2 * T::NDLB, LA = NS < 3 ? NS : 3;
+    auto cread = [&](int i) { return c_frag(cur, i / T::NDLB, i % T::NDLB); };
+    bf16x8 cf[NS + LA], pn[2];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) cf[i] = cread(i);
+    float ps = 0.f;
+    const float negm = -m_run, d0 = dist0(b1 - 2 - t);
+    const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
+    auto soft_pair = [&](int e) {
+      bf16x2 pk;
+      pk[0] = (bf16)__builtin_amdgcn_exp2f(score_of(s[e], e, d0, negm));
+      pk[1] = (bf16)__builtin_amdgcn_exp2f(score_of(s[e + 1], e + 1, d0, negm));
+      pn[e >> 3][e & 7] = pk[0]; pn[e >> 3][(e & 7) + 1] = pk[1];
+      ps = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, ps, false);
+    };
+    each<NS>(EACH(i) {
+      if constexpr (i + LA < NS) cf[i + LA] = cread(i + LA);
+      acc[i % T::NDLB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(cf[i], pf[i / T::NDLB], acc[i % T::NDLB], 0, 0, 0);
+#pragma unroll
+      for (int e = i * 16 / NS; e < (i + 1) * 16 / NS; ++e)
+        if (e % 2 == 0) soft_pair(e);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if (__builtin_amdgcn_ballot_w64(!(ps < kRowSumLimit)) != 0) {   // rare
+      softmax(s, b1 - 2 - t, false, pn, corr);
+    } else {
+      l_run += ps;
+      corr = 1.f;
+    }
+    pf[0] = pn[0]; pf[1] = pn[1];
+    rotate();
+  }
+  plain_until(nsteps);
+  asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");   // no load may land in what follows
+
+  const float l_all = pair_sum(l_run);
+  float z[4] = {};
+  each<T::NDLB>(EACH(i) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z[e % 4] = fmaf(acc[i][e], 0.f, z[e % 4]);
+  });
+  const bool finite = (z[0] + z[1]) + (z[2] + z[3]) == 0.f || !sees || idle;
+  const bool split = CACHE || pieces > 1;
+  const int64_t at = ((int64_t)(slot + piece) * a.cells + cell) * T::BQ;   // row 0 of the piece's sums
+  const int my = qw * 32 + ln;                                            // row of the tile
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(!finite) != 0, 0)) {
+    const int c0 = cg * T::NDLB * 32;
+    constexpr int COLS = (T::NDLB + 1) / 2;   // of 64 lanes; 32 columns: the upper half of the lanes repeats the lower
+#pragma unroll 1
+    for (int i = 0; i < 32; ++i) {
+      const int rr = wr0 + i;
+      if (rr >= R) break;
+      const int tk = __shfl(tok, i), gg = __shfl(g, i), from = max(__shfl(lo, i), b0 * 32), to = min(__shfl(hi, i), min(b1 * 32, keys) - 1);
+      float sum[COLS];
+      const bf16 *cc = ccol + c0 - (T::NDLB == 1 && lane >= 32 ? 32 : 0);
+      const float2 ml = wave_row<MODS>(a, (const bf16 *)a.q + (start + tk) * a.qs + gg * T::DH, T::DH, kcol, cc, __shfl(slope, i), __shfl(own, i), from, to,
+                                       [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, sum);
+      if (T::NDLB == 1 && lane >= 32) continue;
+      if (split) {
+#pragma unroll
+        for (int e = 0; e < COLS; ++e) a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = sum[e];
+        if (lane == 0 && slice == 0 && cg == 0) a.pml[at + qw * 32 + i] = ml;
+      } else {
+        const float inv = __shfl(sees ? 1 : 0, i) ? 1.f / ml.y : 0.f;
+#pragma unroll
+        for (int e = 0; e < COLS; ++e)
+          *reinterpret_cast<bf16 *>(smem + (qw * 32 + i) * T::OUT_PITCH + (c0 + e * 64 + lane) * 2) = (bf16)(inv != 0.f ? sum[e] * inv : 0.f);
+      }
+    }
+  } else if (split) {
+    if (wr0 + ln < R) {
+      float *pa = a.pacc + (at + my) * a.dl + slice * T::DLW + cg * T::NDLB * 32 + 4 * h;
+      each<T::NDLB * 4>(EACH(i) {
+        constexpr int dlb = i / 4, rq = i % 4;
+        *reinterpret_cast<float4 *>(pa + dlb * 32 + rq * 8) = make_float4(acc[dlb][rq * 4], acc[dlb][rq * 4 + 1], acc[dlb][rq * 4 + 2], acc[dlb][rq * 4 + 3]);
+      });
+      if (h == 0 && slice == 0 && cg == 0) a.pml[at + my] = sees ? make_float2(m_run, l_all) : make_float2(-INFINITY, 0.f);
+    }
+  } else {
+    const float inv = 1.0f / l_all;
+    each<T::NDLB * 4>(EACH(i) {
+      constexpr int dlb = i / 4, rq = i % 4;
+      bf16x4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = (bf16)(sees ? acc[dlb][rq * 4 + e] * inv : 0.f);
+      *reinterpret_cast<bf16x4 *>(smem + my * T::OUT_PITCH + (cg * T::NDLB * 32 + dlb * 32 + rq * 8 + 4 * h) * 2) = v;
+    });
+  }
+  if (split) return;
+  __syncthreads();
+  constexpr int CPR = T::DLW / 8, RPP = T::NT / CPR;   // 16-byte chunks of a row, rows per pass
+  const int rr0 = tid / CPR, ch = tid % CPR;
+#pragma unroll 4
+  for (int it = 0; it < T::BQ / RPP; ++it) {
+    const int rr = it * RPP + rr0, full = r0 + rr;
+    if (full < R) {
+      const int tk = full / a.mpc;
+      bf16 *to = (bf16 *)a.L + ((start + tk) * a.nq + cell * a.mpc + (full - tk * a.mpc)) * (int64_t)a.dl + slice * T::DLW + ch * 8;
+      *reinterpret_cast<u32x4 *>(to) = *reinterpret_cast<const u32x4 *>(smem + rr * T::OUT_PITCH + ch * 16);
+    }
+  }
+}
+
+// Rows of a sequence of n tokens, in tiles
+__device__ __forceinline__ int tiles_of(int n, int mpc, int bq) { return n > 0 ? (int)(((int64_t)n * mpc + bq - 1) / bq) : 0; }
+
+struct PlanArgs {
+  const int32_t *cu;
+  int per_seq, batch, mpc, bq, capacity, max_len;
+  const int32_t *first, *last;
+  int per, most;      // workgroups of a tile; pieces to cut the batch into at least (0: none is cut)
+  int32_t *offsets;   // [batch + 1] tiles in front of each sequence
+  Piece *list;        // [capacity]
+  int32_t *count;     // pieces, tiles that are cut
+  Piece *cut;         // [capacity]
+};
+
+// Lists a batch's tiles, most keys first, one workgroup.  What a tile sees is estimated from its first and last token, which is
+// exact for intervals whose ends do not fall; the kernel works out its own.  With `most` the tiles of a batch that would leave CUs
+// idle are cut into pieces of about as many blocks of keys as make that many.
+constexpr int kPlanThreads = 1024, kBins = 256, kLeastBlocks = 4;
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+  __shared__ int bins[kBins], sums[kPlanThreads / 64], total_s, slots_s, cuts_s;
+  __shared__ unsigned long long cost_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
+  if (tid == 0) { cost_s = 0; slots_s = 0; cuts_s = 0; }
+  int before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {   // tiles in front of each sequence
+    const int b = b0 + tid;
+    const int n = b < a.batch ? tiles_of(a.cu ? a.cu[b + 1] - a.cu[b] : a.per_seq, a.mpc, a.bq) : 0;
+    int run = n;
+    for (int i = 1; i < 64; i <<= 1) { const int v = __shfl_up(run, i); run += lane >= i ? v : 0; }
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    int add = before, all = before;
+    for (int w = 0; w < kPlanThreads / 64; ++w) { add += w < wave ? sums[w] : 0; all += sums[w]; }
+    if (b < a.batch) a.offsets[b] = add + run - n;
+    before = all;
+    __syncthreads();
+  }
+  if (tid == 0) a.offsets[a.batch] = before;
+  __threadfence_block();
+  __syncthreads();
+  const int tiles = min(before, a.capacity);
+  auto look = [&](int t, int &b, int &tile) {
+    int lo = 0, hi = a.batch;   // offsets[lo] <= t < offsets[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.offsets[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    tile = t - a.offsets[lo];
+    const int64_t start = a.cu ? a.cu[b] : (int64_t)b * a.per_seq;
+    const int n = a.cu ? a.cu[b + 1] - (int)start : a.per_seq;
+    const int t0 = (int)((int64_t)tile * a.bq / a.mpc), t1 = min((int)(((int64_t)(tile + 1) * a.bq - 1) / a.mpc), n - 1);
+    const int from = a.first ? max(a.first[start + t0], 0) : 0, to = min(a.last ? max(a.last[start + t0], a.last[start + t1]) : t1, n - 1);
+    return to < from ? 0 : (to >> 5) - (from >> 5) + 1;
+  };
+  const int widest = (a.max_len + 31) / 32;
+  auto bin_of = [&](int blocks) { return kBins - 1 - min((int)((int64_t)blocks * (kBins - 1) / max(widest, 1)), kBins - 1); };   // most first
+  int target = INT_MAX;
+  if (a.most) {
+    unsigned long long mine = 0;
+    for (int t = tid; t < tiles; t += kPlanThreads) { int b, tile; mine += look(t, b, tile); }
+    if (mine) atomicAdd(&cost_s, mine);
+    __syncthreads();
+    target = max((int)((cost_s * a.per + a.most - 1) / a.most), kLeastBlocks);
+  }
+  auto pieces_of = [&](int blocks) { return a.most && blocks > target ? (blocks + target - 1) / target : 1; };
+  for (int t = tid; t < tiles; t += kPlanThreads) {
+    int b, tile;
+    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+    atomicAdd(&bins[bin_of(blocks / n)], n);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int run = 0;
+    for (int i = 0; i < kBins; ++i) { const int n = bins[i]; bins[i] = run; run += n; }
+    total_s = run;
+  }
+  __syncthreads();
+  for (int t = tid; t < tiles; t += kPlanThreads) {
+    int b, tile;
+    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+    const int slot = n > 1 ? atomicAdd(&slots_s, n) : 0, at = atomicAdd(&bins[bin_of(blocks / n)], n);
+    for (int i = 0; i < n; ++i)
+      if (at + i < a.capacity) a.list[at + i] = Piece{b, tile, i, n, slot, {}};
+    if (n > 1) {
+      const int c = atomicAdd(&cuts_s, 1);
+      if (c < a.capacity) a.cut[c] = Piece{b, tile, 0, n, slot, {}};
+    }
+  }
+  __syncthreads();
+  if (tid == 0) { a.count[0] = min(total_s, a.capacity); a.count[1] = min(cuts_s, a.capacity); }
+}
+
+// Joins the pieces of one row of a tile: weights 2^(m - max); a wave per (row, cell), four columns a lane and step.
+__global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piece *cut, int bq) {
+  if ((int)blockIdx.x >= a.count[1]) return;
+  const Piece p = cut[blockIdx.x];
+  const int lane = threadIdx.x & 63, cell = blockIdx.z, rr = blockIdx.y * 4 + (threadIdx.x >> 6);
+  const int64_t start = a.cu ? a.cu[p.b] : (int64_t)p.b * a.per_seq;
+  const int R = (a.cu ? a.cu[p.b + 1] - (int)start : a.per_seq) * a.mpc, full = p.tile * bq + rr;
+  if (full >= R) return;
+  auto at = [&](int i) { return ((int64_t)(p.slot + i) * a.cells + cell) * bq + rr; };
+  float mx = -INFINITY;
+  for (int i = 0; i < p.pieces; ++i) mx = fmaxf(mx, a.pml[at(i)].x);
+  const float ref = mx > -INFINITY ? mx : 0.f;
+  const int tk = full / a.mpc;
+  bf16 *to = (bf16 *)a.L + ((start + tk) * a.nq + cell * a.mpc + (full - tk * a.mpc)) * (int64_t)a.dl;
+  float l = 0.f;
+  for (int i = 0; i < p.pieces; ++i) {
+    const float2 ml = a.pml[at(i)];
+    if (ml.y != 0.f) l = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, l);
+  }
+  int lo, hi;
+  seen_by(a.rules, start + tk, tk, R / a.mpc, lo, hi);
+  const float inv = lo <= hi ? 1.f / l : 0.f;
+  for (int col = lane * 4; col < a.dl; col += 256) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < p.pieces; ++i) {
+      const float2 ml = a.pml[at(i)];
+      if (ml.y == 0.f) continue;   // sees none of the piece's keys
+      const float w = __builtin_amdgcn_exp2f(ml.x - ref) * inv;
+      const float4 s = *reinterpret_cast<const float4 *>(a.pacc + at(i) * a.dl + col);
+      v.x = fmaf(w, s.x, v.x); v.y = fmaf(w, s.y, v.y); v.z = fmaf(w, s.z, v.z); v.w = fmaf(w, s.w, v.w);
+    }
+    if (lo <= hi && !(l > 0.f)) v.x = v.y = v.z = v.w = NAN;   // scores of nothing but -infinity, or NaN among them
+    bf16x4 o;
+    o[0] = (bf16)v.x; o[1] = (bf16)v.y; o[2] = (bf16)v.z; o[3] = (bf16)v.w;
+    *reinterpret_cast<bf16x4 *>(to + col) = o;
+  }
+}
+
+template <class T, int MODS, bool CACHE>
+void launch_mods(const RowsArgs &a, unsigned grid, hipStream_t st) {
+  allow_dynamic_lds((const void *)rows_attn_kernel<T, MODS, CACHE>, T::SMEM);
+  rows_attn_kernel<T, MODS, CACHE><<<grid, T::NT, T::SMEM, st>>>(a);
+}
+
+template <class T, bool CACHE>
+void launch_tile(RowsArgs a, hipStream_t st) {
+  const int64_t tiles = a.tiles < 64 ? a.tiles : (a.tiles + 7) / 8 * 8;
+  const unsigned grid = (unsigned)(tiles * a.cells * a.slices);
+  switch ((a.rules.cap > 0.f ? kCap : 0) | (a.rules.slopes ? kBias : 0)) {
+    case 0: launch_mods<T, 0, CACHE>(a, grid, st); break;
+    case kCap: launch_mods<T, kCap, CACHE>(a, grid, st); break;
+    case kBias: launch_mods<T, kBias, CACHE>(a, grid, st); break;
+    default: launch_mods<T, kCap | kBias, CACHE>(a, grid, st);
+  }
+}
+
+// Latent columns of a workgroup of 128 rows
+int wide_tile(const Dims &d) { return d.dh == 128 ? (d.dl % 256 == 0 ? 256 : 128) : (d.dl % 128 == 0 ? 128 : 64); }
+
+template <bool CACHE>
+void launch_rows(const Dims &d, RowsArgs a, int dlw, hipStream_t st) {
+  a.slices = d.dl / dlw;
+  if (d.dh == 64) {
+    if (dlw == 128) launch_tile<Tile<64, 128, 4>, CACHE>(a, st);
+    else launch_tile<Tile<64, 64, 4>, CACHE>(a, st);
+  } else if (dlw == 256) launch_tile<Tile<128, 256, 4>, CACHE>(a, st);
+  else launch_tile<Tile<128, 128, 4>, CACHE>(a, st);
+}
+
+constexpr int kAtOnce = 256;   // pieces of a batch that is cut
+
+struct MaskedWs {
+  int32_t *offsets, *count;
+  Piece *list, *cut;
+  float *pacc; float2 *pml;
+  int64_t capacity, slots;
+  int most;
+  size_t bytes;
+};
+
+MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base) {
+  MaskedWs w{};
+  const int mpc = maps_per_cell(d), bq = 128, cells = d.nq / mpc, per = cells * (d.dl / wide_tile(d));
+  const int64_t tiles = total * mpc / bq + batch;
+  w.most = tiles * per < kAtOnce ? kAtOnce : 0;
+  w.slots = w.most ? tiles + kAtOnce / per + 1 : 0;
+  w.capacity = std::max(tiles, w.slots);
+  size_t off = 0;
+  auto take = [&](size_t n) { void *p = base ? (char *)base + off : nullptr; off += align_up(n); return p; };
+  w.offsets = (int32_t *)take(((size_t)batch + 1) * 4);
+  w.count = (int32_t *)take(8);
+  w.list = (Piece *)take((size_t)w.capacity * sizeof(Piece));
+  w.cut = (Piece *)take(w.most ? (size_t)w.capacity * sizeof(Piece) : 0);
+  w.pml = (float2 *)take((size_t)w.slots * cells * bq * 8);
+  w.pacc = (float *)take((size_t)w.slots * cells * bq * d.dl * 4);
+  w.bytes = off;
+  return w;
+}
+
+}  // namespace
+
+bool rows_bf16_ok(const Dims &d) {
+  return d.dtype == GTA_BF16 && ((d.dh == 128 && d.dl % 128 == 0) || (d.dh == 64 && d.dl % 64 == 0));
+}
+
+// 16-byte chunks, and 32 rows within the 2 GiB that an offset reaches
+bool rows_operands_ok(const void *p, int64_t stride, int esize) {
+  return !((uintptr_t)p & 15u) && stride * esize % 16 == 0 && stride * esize * 32 < ((int64_t)1 << 31);
+}
+
+// Row numbers of 32 bits and the threads of a launch
+bool masked_bf16_fits(const Dims &d, int batch, int64_t total) {
+  const int mpc = maps_per_cell(d);
+  return total * mpc < INT32_MAX - 256 && (total * mpc / 128 + batch + 8 + kAtOnce) * (d.nq / mpc) * (d.dl / wide_tile(d)) < (1 << 24) && d.nq / mpc <= 65535;
+}
+
+size_t masked_bf16_bytes(const Dims &d, int batch, int64_t total) { return masked_bf16_fits(d, batch, total) ? carve_masked(d, batch, total, nullptr).bytes : 0; }
+
+int launch_masked_bf16(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) {
+  const MaskedWs w = carve_masked(d, m.batch, m.total, ws);
+  RowsArgs a{};
+  a.q = m.q; a.k = m.k; a.c = m.c; a.qs = m.q_stride; a.ks = m.k_stride; a.cs = m.c_stride; a.L = m.l_out;
+  a.cu = m.cu; a.per_seq = (int)(m.total / m.batch); a.batch = m.batch;
+  a.nq = d.nq; a.mpc = maps_per_cell(d); a.cells = d.nq / a.mpc; a.kdiv = d.qpk / a.mpc; a.cdiv = d.qpc / a.mpc; a.dl = d.dl;
+  a.rules = m.rules;
+  const int dlw = wide_tile(d), per = a.cells * (d.dl / dlw);
+  a.list = w.list; a.count = w.count; a.tiles = (int)w.capacity; a.pacc = w.pacc; a.pml = w.pml;
+  plan_kernel<<<1, kPlanThreads, 0, st>>>(PlanArgs{m.cu, a.per_seq, m.batch, a.mpc, 128, (int)w.capacity, m.max_len, m.rules.first, m.rules.last,
+                                                  per, w.most, w.offsets, w.list, w.count, w.cut});
+  launch_rows<false>(d, a, dlw, st);
+  if (w.most) join_pieces_kernel<<<dim3((unsigned)(w.slots / 2 + 1), 32, (unsigned)a.cells), 256, 0, st>>>(a, w.cut, 128);
+  return check_launch();
+}
+
+}  // namespace gta

@@ -50,7 +50,7 @@ __device__ __forceinline__ float ruled_score(const Rules &r, float dot, float sl
 // What a token at `own` of `keys` keys sees: lo .. hi, nothing where lo > hi
 __device__ __forceinline__ void seen_by(const Rules &r, int64_t token, int own, int keys, int &lo, int &hi) {
   lo = r.first ? max(r.first[token], 0) : 0;
-  hi = min(r.last ? r.last[token] : own, keys - 1);
+  hi = max(min(r.last ? r.last[token] : own, keys - 1), -1);
 }
 
 constexpr int kRulesMaxHead = 1024, kRulesMaxLatent = 4096;
