@@ -283,7 +283,7 @@ int gta_uses_tuned_kernels(const gta_config *cfg, int mode) {
   if (mode == GTA_MODE_PREFILL_CHUNK) return tuned_prefill_chunk_supported(d, 1) ? 1 : 0;   // up to the cache-size limit
   if (mode == GTA_MODE_MX_DECODE) return !mx_decode_dims_ok(d) ? GTA_ERR_UNSUPPORTED : mx_decode_tuned(d) ? 1 : 0;   // up to the page size
   if (mode == GTA_MODE_PREFILL_MASKED) return !rules_dims_ok(d) ? GTA_ERR_UNSUPPORTED : rows_bf16_ok(d) ? 1 : 0;
-  if (mode == GTA_MODE_PREFIX_DECODE) return rules_dims_ok(d) ? 0 : GTA_ERR_UNSUPPORTED;
+  if (mode == GTA_MODE_PREFIX_DECODE) return !rules_dims_ok(d) ? GTA_ERR_UNSUPPORTED : prefix_tuned(d) ? 1 : 0;   // up to the page sizes
   return GTA_ERR_DTYPE;
 }
 
@@ -310,7 +310,8 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
   if (mode == GTA_MODE_PREFILL_MASKED || mode == GTA_MODE_PREFIX_DECODE) {
     if (!rules_dims_ok(d) || total_tokens < 0) return 0;
     if (mode == GTA_MODE_PREFILL_MASKED) return (rows_bf16_ok(d) ? masked_bf16_bytes(d, batch, total_tokens) : 0) + 256;
-    return 256;
+    if (total_tokens > (1 << 30) || max_len > (1 << 30)) return 0;
+    return prefix_bytes(d, batch, (int)total_tokens, max_len) + 256;
   }
   if (mode == GTA_MODE_DECODE) {
     int splits = choose_splits(d, batch, max_len, num_splits);
@@ -586,6 +587,11 @@ int gta_prefix_decode_attention(const gta_config *cfg, const void *q, const gta_
   if (misaligned(q) || misaligned(l_out) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
   if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
   const PrefixArgs p{q, view_of(prefix, nullptr), view_of(cache, slots), prefix_slot, batch, rules_of(d, rules), l_out};
+  if (prefix_fits(d, batch, prefix->max_seq, cache->max_seq)) {
+    if (workspace_bytes < prefix_bytes(d, batch, prefix->max_seq, cache->max_seq)) return GTA_ERR_WORKSPACE;
+    if (prefix_layout_ok(*prefix, *cache)) return launch_prefix(d, p, workspace, (hipStream_t)hip_stream);
+  }
+  note_generic_path(d, "gta_prefix_decode_attention");
   return launch_prefix_any(d, p, (hipStream_t)hip_stream);
 }
 

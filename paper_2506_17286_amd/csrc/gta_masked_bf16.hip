@@ -730,6 +730,31 @@ bool masked_bf16_fits(const Dims &d, int batch, int64_t total) {
   return total * mpc < INT32_MAX - 256 && (total * mpc / 128 + batch + 8 + kAtOnce) * (d.nq / mpc) * (d.dl / wide_tile(d)) < (1 << 24) && d.nq / mpc <= 65535;
 }
 
+// A batch of few rows takes tiles of 64 or 32, whose waves share the columns.
+int prefix_tile_rows(const Dims &d, int rows) {
+  if (d.dh == 64) return d.dl % 128 == 0 && rows <= 32 ? 32 : 128;
+  return rows <= 32 ? 32 : rows <= 64 && d.dl % 256 == 0 ? 64 : 128;
+}
+static int prefix_columns(const Dims &d, int bq) {   // latent columns of a workgroup
+  if (d.dh == 64 || bq == 128) return wide_tile(d);
+  return d.dl % 512 == 0 ? 512 : d.dl % 256 == 0 ? 256 : 128;
+}
+int prefix_slices(const Dims &d, int bq) { return d.dl / prefix_columns(d, bq); }
+
+void launch_prefix_rows(const Dims &d, const RowsArgs &args, int bq, hipStream_t st) {
+  RowsArgs a = args;
+  const int w = prefix_columns(d, bq);
+  if (bq == 128) { launch_rows<true>(d, a, w, st); return; }
+  a.slices = d.dl / w;
+  if (d.dh == 64) launch_tile<Tile<64, 128, 1>, true>(a, st);
+  else if (bq == 64) {
+    if (w == 512) launch_tile<Tile<128, 512, 2>, true>(a, st);
+    else launch_tile<Tile<128, 256, 2>, true>(a, st);
+  } else if (w == 512) launch_tile<Tile<128, 512, 1>, true>(a, st);
+  else if (w == 256) launch_tile<Tile<128, 256, 1>, true>(a, st);
+  else launch_tile<Tile<128, 128, 1>, true>(a, st);
+}
+
 size_t masked_bf16_bytes(const Dims &d, int batch, int64_t total) { return masked_bf16_fits(d, batch, total) ? carve_masked(d, batch, total, nullptr).bytes : 0; }
 
 int launch_masked_bf16(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) {

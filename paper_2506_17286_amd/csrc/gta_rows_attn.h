@@ -48,4 +48,16 @@ bool masked_bf16_fits(const Dims &d, int batch, int64_t total);
 size_t masked_bf16_bytes(const Dims &d, int batch, int64_t total);
 int launch_masked_bf16(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st);
 
+// The prefix's rows: rows of a tile for `rows` query rows of a cell, workgroups that share its latent columns, launch
+int prefix_tile_rows(const Dims &d, int rows);
+int prefix_slices(const Dims &d, int bq);
+void launch_prefix_rows(const Dims &d, const RowsArgs &a, int bq, hipStream_t st);
+
+// gta_prefix_decode.hip
+bool prefix_tuned(const Dims &d);   // with pages of a power of two of at least 16 rows
+bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq);
+bool prefix_layout_ok(const gta_cache &prefix, const gta_cache &own);
+size_t prefix_bytes(const Dims &d, int batch, int prefix_max, int max_seq);
+int launch_prefix(const Dims &d, const PrefixArgs &x, void *ws, hipStream_t st);
+
 }  // namespace gta
