@@ -11,7 +11,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libgta.so")
 SOURCES = ["gta_api.cpp", "gta_generic.hip", "gta_tuned.hip", "gta_f32.hip", "gta_rows_bf16.hip", "gta_decode_bf16.hip", "gta_gemm_bf16.hip", "gta_prefill_bf16.hip",
            "gta_norm_rope.hip", "gta_mx_cache.hip", "gta_mx_decode.hip",
-           "gta_rope_rows.hip", "gta_rules_any.hip", "gta_masked_bf16.hip", "gta_prefix_decode.hip"]
+           "gta_rope_rows.hip", "gta_rules_any.hip", "gta_masked_plan.hip", "gta_masked_bf16.hip", "gta_masked_f32.hip",
+           "gta_prefix_decode.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-I", os.path.join(ROOT, "include"), "-I", CSRC]

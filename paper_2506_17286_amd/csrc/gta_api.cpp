@@ -282,7 +282,7 @@ int gta_uses_tuned_kernels(const gta_config *cfg, int mode) {
   if (mode == GTA_MODE_DECODE) return tuned_decode_supported(d) ? 1 : 0;
   if (mode == GTA_MODE_PREFILL_CHUNK) return tuned_prefill_chunk_supported(d, 1) ? 1 : 0;   // up to the cache-size limit
   if (mode == GTA_MODE_MX_DECODE) return !mx_decode_dims_ok(d) ? GTA_ERR_UNSUPPORTED : mx_decode_tuned(d) ? 1 : 0;   // up to the page size
-  if (mode == GTA_MODE_PREFILL_MASKED) return !rules_dims_ok(d) ? GTA_ERR_UNSUPPORTED : rows_bf16_ok(d) ? 1 : 0;
+  if (mode == GTA_MODE_PREFILL_MASKED) return !rules_dims_ok(d) ? GTA_ERR_UNSUPPORTED : masked_tuned(d) ? 1 : 0;
   if (mode == GTA_MODE_PREFIX_DECODE) return !rules_dims_ok(d) ? GTA_ERR_UNSUPPORTED : prefix_tuned(d) ? 1 : 0;   // up to the page sizes
   return GTA_ERR_DTYPE;
 }
@@ -309,7 +309,7 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
   }
   if (mode == GTA_MODE_PREFILL_MASKED || mode == GTA_MODE_PREFIX_DECODE) {
     if (!rules_dims_ok(d) || total_tokens < 0) return 0;
-    if (mode == GTA_MODE_PREFILL_MASKED) return (rows_bf16_ok(d) ? masked_bf16_bytes(d, batch, total_tokens) : 0) + 256;
+    if (mode == GTA_MODE_PREFILL_MASKED) return masked_bytes(d, batch, total_tokens) + 256;
     if (total_tokens > (1 << 30) || max_len > (1 << 30)) return 0;
     return prefix_bytes(d, batch, (int)total_tokens, max_len) + 256;
   }
@@ -563,10 +563,11 @@ int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q
   if (total_tokens == 0 || max_seqlen == 0) return GTA_OK;
   if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
   const MaskedArgs m{q, k, c, q_stride, k_stride, c_stride, cu_seqlens, batch, total_tokens, max_seqlen, rules_of(d, rules), l_out};
-  if (rows_bf16_ok(d) && masked_bf16_fits(d, batch, total_tokens)) {
-    if (workspace_bytes < masked_bf16_bytes(d, batch, total_tokens)) return GTA_ERR_WORKSPACE;
-    if (rows_operands_ok(q, q_stride, 2) && rows_operands_ok(k, k_stride, 2) && rows_operands_ok(c, c_stride, 2))
-      return launch_masked_bf16(d, m, workspace, (hipStream_t)hip_stream);
+  if (masked_fits(d, batch, total_tokens)) {
+    if (workspace_bytes < masked_bytes(d, batch, total_tokens)) return GTA_ERR_WORKSPACE;
+    const int es = d.esize();
+    if (rows_operands_ok(q, q_stride, es) && rows_operands_ok(k, k_stride, es) && rows_operands_ok(c, c_stride, es))
+      return launch_masked(d, m, workspace, (hipStream_t)hip_stream);
   }
   note_generic_path(d, "gta_prefill_masked_attention");
   return launch_masked_any(d, m, (hipStream_t)hip_stream);

@@ -1,0 +1,215 @@
+// A batch of packed sequences as a list of tiles of query rows for the kernels of gta_prefill_masked_attention, and the join of tiles
+// whose keys were shared out.
+#include <math.h>
+
+#include "gta_rows_attn.h"
+
+namespace gta {
+namespace {
+
+// Rows of a sequence of n tokens, in tiles
+__device__ __forceinline__ int tiles_of(int n, int mpc, int bq) { return n > 0 ? (int)(((int64_t)n * mpc + bq - 1) / bq) : 0; }
+
+struct PlanArgs {
+  const int32_t *cu;
+  int per_seq, batch, mpc, bq, capacity, max_len;
+  const int32_t *first, *last;
+  int per, most;      // workgroups of a tile; pieces to cut the batch into at least (0: none is cut)
+  int32_t *offsets;   // [batch + 1] tiles in front of each sequence
+  Piece *list;        // [capacity]
+  int32_t *count;     // pieces, tiles that are cut
+  Piece *cut;         // [capacity]
+};
+
+// Lists a batch's tiles, most keys first, one workgroup.  What a tile sees is estimated from its first and last token, which is
+// exact for intervals whose ends do not fall; the kernel works out its own.  With `most` the tiles of a batch that would leave CUs
+// idle are cut into pieces of about as many blocks of keys as make that many.
+constexpr int kPlanThreads = 1024, kBins = 256, kLeastBlocks = 4;
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+  __shared__ int bins[kBins], sums[kPlanThreads / 64], total_s, slots_s, cuts_s;
+  __shared__ unsigned long long cost_s;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
+  if (tid == 0) { cost_s = 0; slots_s = 0; cuts_s = 0; }
+  int before = 0;
+  for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {   // tiles in front of each sequence
+    const int b = b0 + tid;
+    const int n = b < a.batch ? tiles_of(a.cu ? a.cu[b + 1] - a.cu[b] : a.per_seq, a.mpc, a.bq) : 0;
+    int run = n;
+    for (int i = 1; i < 64; i <<= 1) { const int v = __shfl_up(run, i); run += lane >= i ? v : 0; }
+    if (lane == 63) sums[wave] = run;
+    __syncthreads();
+    int add = before, all = before;
+    for (int w = 0; w < kPlanThreads / 64; ++w) { add += w < wave ? sums[w] : 0; all += sums[w]; }
+    if (b < a.batch) a.offsets[b] = add + run - n;
+    before = all;
+    __syncthreads();
+  }
+  if (tid == 0) a.offsets[a.batch] = before;
+  __threadfence_block();
+  __syncthreads();
+  const int tiles = min(before, a.capacity);
+  auto look = [&](int t, int &b, int &tile) {
+    int lo = 0, hi = a.batch;   // offsets[lo] <= t < offsets[hi]
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.offsets[mid] <= t) lo = mid;
+      else hi = mid;
+    }
+    b = lo;
+    tile = t - a.offsets[lo];
+    const int64_t start = a.cu ? a.cu[b] : (int64_t)b * a.per_seq;
+    const int n = a.cu ? a.cu[b + 1] - (int)start : a.per_seq;
+    const int t0 = (int)((int64_t)tile * a.bq / a.mpc), t1 = min((int)(((int64_t)(tile + 1) * a.bq - 1) / a.mpc), n - 1);
+    const int from = a.first ? max(a.first[start + t0], 0) : 0, to = min(a.last ? max(a.last[start + t0], a.last[start + t1]) : t1, n - 1);
+    return to < from ? 0 : (to >> 5) - (from >> 5) + 1;
+  };
+  const int widest = (a.max_len + 31) / 32;
+  auto bin_of = [&](int blocks) { return kBins - 1 - min((int)((int64_t)blocks * (kBins - 1) / max(widest, 1)), kBins - 1); };   // most first
+  int target = INT_MAX;
+  if (a.most) {
+    unsigned long long mine = 0;
+    for (int t = tid; t < tiles; t += kPlanThreads) { int b, tile; mine += look(t, b, tile); }
+    if (mine) atomicAdd(&cost_s, mine);
+    __syncthreads();
+    target = max((int)((cost_s * a.per + a.most - 1) / a.most), kLeastBlocks);
+  }
+  auto pieces_of = [&](int blocks) { return a.most && blocks > target ? (blocks + target - 1) / target : 1; };
+  for (int t = tid; t < tiles; t += kPlanThreads) {
+    int b, tile;
+    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+    atomicAdd(&bins[bin_of(blocks / n)], n);
+  }
+  __syncthreads();
+  if (tid == 0) {
+    int run = 0;
+    for (int i = 0; i < kBins; ++i) { const int n = bins[i]; bins[i] = run; run += n; }
+    total_s = run;
+  }
+  __syncthreads();
+  for (int t = tid; t < tiles; t += kPlanThreads) {
+    int b, tile;
+    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+    const int slot = n > 1 ? atomicAdd(&slots_s, n) : 0, at = atomicAdd(&bins[bin_of(blocks / n)], n);
+    for (int i = 0; i < n; ++i)
+      if (at + i < a.capacity) a.list[at + i] = Piece{b, tile, i, n, slot, {}};
+    if (n > 1) {
+      const int c = atomicAdd(&cuts_s, 1);
+      if (c < a.capacity) a.cut[c] = Piece{b, tile, 0, n, slot, {}};
+    }
+  }
+  __syncthreads();
+  if (tid == 0) { a.count[0] = min(total_s, a.capacity); a.count[1] = min(cuts_s, a.capacity); }
+}
+
+// Joins the pieces of one row of a tile: weights 2^(m - max); a wave per (row, cell), four columns a lane and step.
+template <typename T>
+__global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piece *cut, int bq) {
+  if ((int)blockIdx.x >= a.count[1]) return;
+  const Piece p = cut[blockIdx.x];
+  const int lane = threadIdx.x & 63, cell = blockIdx.z, rr = blockIdx.y * 4 + (threadIdx.x >> 6);
+  const int64_t start = a.cu ? a.cu[p.b] : (int64_t)p.b * a.per_seq;
+  const int R = (a.cu ? a.cu[p.b + 1] - (int)start : a.per_seq) * a.mpc, full = p.tile * bq + rr;
+  if (full >= R) return;
+  auto at = [&](int i) { return ((int64_t)(p.slot + i) * a.cells + cell) * bq + rr; };
+  float mx = -INFINITY;
+  for (int i = 0; i < p.pieces; ++i) mx = fmaxf(mx, a.pml[at(i)].x);
+  const float ref = mx > -INFINITY ? mx : 0.f;
+  const int tk = full / a.mpc;
+  T *to = (T *)a.L + ((start + tk) * a.nq + cell * a.mpc + (full - tk * a.mpc)) * (int64_t)a.dl;
+  float l = 0.f;
+  for (int i = 0; i < p.pieces; ++i) {
+    const float2 ml = a.pml[at(i)];
+    if (ml.y != 0.f) l = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, l);
+  }
+  int lo, hi;
+  seen_by(a.rules, start + tk, tk, R / a.mpc, lo, hi);
+  const float inv = lo <= hi ? 1.f / l : 0.f;
+  for (int col = lane * 4; col < a.dl; col += 256) {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < p.pieces; ++i) {
+      const float2 ml = a.pml[at(i)];
+      if (ml.y == 0.f) continue;   // sees none of the piece's keys
+      const float w = __builtin_amdgcn_exp2f(ml.x - ref) * inv;
+      const float4 s = *reinterpret_cast<const float4 *>(a.pacc + at(i) * a.dl + col);
+      v.x = fmaf(w, s.x, v.x); v.y = fmaf(w, s.y, v.y); v.z = fmaf(w, s.z, v.z); v.w = fmaf(w, s.w, v.w);
+    }
+    if (lo <= hi && !(l > 0.f)) v.x = v.y = v.z = v.w = NAN;   // scores of nothing but -infinity, or NaN among them
+    to[col] = (T)v.x; to[col + 1] = (T)v.y; to[col + 2] = (T)v.z; to[col + 3] = (T)v.w;
+  }
+}
+
+constexpr int kAtOnce = 256;   // pieces of a batch that is cut
+
+int tile_rows(const Dims &d) { return d.dtype == GTA_BF16 ? 128 : 32; }
+int columns(const Dims &d) { return d.dtype == GTA_BF16 ? masked_bf16_columns(d) : rows_f32_columns(d); }
+
+struct MaskedWs {
+  int32_t *offsets, *count;
+  Piece *list, *cut;
+  float *pacc; float2 *pml;
+  int64_t capacity, slots;
+  int most;
+  size_t bytes;
+};
+
+MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base) {
+  MaskedWs w{};
+  const int mpc = maps_per_cell(d), bq = tile_rows(d), cells = d.nq / mpc, per = cells * (d.dl / columns(d));
+  const int64_t tiles = total * mpc / bq + batch;
+  w.most = tiles * per < kAtOnce ? kAtOnce : 0;
+  w.slots = w.most ? tiles + kAtOnce / per + 1 : 0;
+  w.capacity = std::max(tiles, w.slots);
+  size_t off = 0;
+  auto take = [&](size_t n) { void *p = base ? (char *)base + off : nullptr; off += align_up(n); return p; };
+  w.offsets = (int32_t *)take(((size_t)batch + 1) * 4);
+  w.count = (int32_t *)take(8);
+  w.list = (Piece *)take((size_t)w.capacity * sizeof(Piece));
+  w.cut = (Piece *)take(w.most ? (size_t)w.capacity * sizeof(Piece) : 0);
+  w.pml = (float2 *)take((size_t)w.slots * cells * bq * 8);
+  w.pacc = (float *)take((size_t)w.slots * cells * bq * d.dl * 4);
+  w.bytes = off;
+  return w;
+}
+
+}  // namespace
+
+bool masked_tuned(const Dims &d) { return rows_bf16_ok(d) || rows_f32_ok(d); }
+
+// 16-byte chunks, and 32 rows within the 2 GiB that an offset reaches
+bool rows_operands_ok(const void *p, int64_t stride, int esize) {
+  return !((uintptr_t)p & 15u) && stride * esize % 16 == 0 && stride * esize * 32 < ((int64_t)1 << 31);
+}
+
+// Row numbers of 32 bits and the threads of a launch
+bool masked_fits(const Dims &d, int batch, int64_t total) {
+  if (!masked_tuned(d)) return false;
+  const int mpc = maps_per_cell(d);
+  return total * mpc < INT32_MAX - 256 && (total * mpc / tile_rows(d) + batch + 8 + kAtOnce) * (d.nq / mpc) * (d.dl / columns(d)) < (1 << 24);
+}
+
+size_t masked_bytes(const Dims &d, int batch, int64_t total) { return masked_fits(d, batch, total) ? carve_masked(d, batch, total, nullptr).bytes : 0; }
+
+int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) {
+  const MaskedWs w = carve_masked(d, m.batch, m.total, ws);
+  RowsArgs a{};
+  a.q = m.q; a.k = m.k; a.c = m.c; a.qs = m.q_stride; a.ks = m.k_stride; a.cs = m.c_stride; a.L = m.l_out;
+  a.cu = m.cu; a.per_seq = (int)(m.total / m.batch); a.batch = m.batch;
+  a.nq = d.nq; a.mpc = maps_per_cell(d); a.cells = d.nq / a.mpc; a.kdiv = d.qpk / a.mpc; a.cdiv = d.qpc / a.mpc; a.dl = d.dl;
+  a.slices = d.dl / columns(d);
+  a.rules = m.rules;
+  a.list = w.list; a.count = w.count; a.tiles = (int)w.capacity; a.pacc = w.pacc; a.pml = w.pml;
+  const int bq = tile_rows(d);
+  plan_kernel<<<1, kPlanThreads, 0, st>>>(PlanArgs{m.cu, a.per_seq, m.batch, a.mpc, bq, (int)w.capacity, m.max_len, m.rules.first, m.rules.last,
+                                                  a.cells * a.slices, w.most, w.offsets, w.list, w.count, w.cut});
+  if (d.dtype == GTA_BF16) launch_masked_bf16(d, a, st);
+  else launch_rows_f32(d, a, false, st);
+  if (w.most) {
+    const dim3 grid((unsigned)(w.slots / 2 + 1), (unsigned)(bq / 4), (unsigned)a.cells);
+    if (d.dtype == GTA_BF16) join_pieces_kernel<__bf16><<<grid, 256, 0, st>>>(a, w.cut, bq);
+    else join_pieces_kernel<float><<<grid, 256, 0, st>>>(a, w.cut, bq);
+  }
+  return check_launch();
+}
+
+}  // namespace gta

@@ -365,9 +365,9 @@ PrefixPlan prefix_plan(const Dims &d, int batch, int prefix_max) {
   PrefixPlan p{};
   p.mpc = maps_per_cell(d);
   p.cells = d.nq / p.mpc;
-  p.bq = prefix_tile_rows(d, batch * p.mpc);
+  p.bq = d.dtype == GTA_BF16 ? prefix_tile_rows(d, batch * p.mpc) : 32;
   p.tiles = (int)(((int64_t)batch * p.mpc + p.bq - 1) / p.bq);
-  const int64_t per = (int64_t)p.tiles * p.cells * prefix_slices(d, p.bq);
+  const int64_t per = (int64_t)p.tiles * p.cells * (d.dtype == GTA_BF16 ? prefix_slices(d, p.bq) : d.dl / rows_f32_columns(d));
   p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(256 + per - 1) / per, ((int64_t)prefix_max + 255) / 256, 256}));
   return p;
 }
@@ -410,7 +410,7 @@ void launch_stream(const StreamArgs &a, int nf, int groups, int lds, hipStream_t
 // Page sizes of a power of two from 16 rows on
 static bool pages_ok(const gta_cache &c) { return !c.block_table || (c.page_size >= 16 && !(c.page_size & (c.page_size - 1))); }
 
-bool prefix_tuned(const Dims &d) { return rows_bf16_ok(d); }
+bool prefix_tuned(const Dims &d) { return rows_bf16_ok(d) || (rows_f32_ok(d) && d.dh >= 64); }
 bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq) {
   const int mpc = maps_per_cell(d);
   return prefix_tuned(d) && (int64_t)batch * mpc < (1 << 24) && d.nq <= 512 && (int64_t)d.wk_w * d.esize() * 32 < (1 << 30) &&
@@ -434,7 +434,8 @@ int launch_prefix(const Dims &d, const PrefixArgs &x, void *ws, hipStream_t st) 
   r.nq = d.nq; r.mpc = p.mpc; r.cells = p.cells; r.kdiv = d.qpk / p.mpc; r.cdiv = d.qpc / p.mpc; r.dl = d.dl; r.rules = x.rules;
   r.tiles = p.tiles * p.pieces; r.pacc = w.pacc; r.pml = w.pml; r.prefix = x.prefix; r.own = x.own; r.prefix_slot = x.prefix_slot;
   r.pieces = p.pieces; r.ps_shift = shift_of(x.prefix.pm);
-  launch_prefix_rows(d, r, p.bq, st);
+  if (d.dtype == GTA_BF16) launch_prefix_rows(d, r, p.bq, st);
+  else launch_rows_f32(d, r, true, st);
   StreamArgs a{};
   a.q = x.q; a.prefix = x.prefix; a.own = x.own; a.prefix_slot = x.prefix_slot; a.batch = x.batch; a.nq = d.nq; a.qpk = d.qpk; a.qpc = d.qpc;
   a.dh = d.dh; a.dl = d.dl; a.kw = d.wk_w; a.cw = d.wc_w; a.rules = x.rules; a.maps = s.maps; a.blocks = s.blocks; a.heads = s.heads;

@@ -41,12 +41,64 @@ __device__ __forceinline__ void prefix_seen(const RowsArgs &a, int b, int P, int
   hi = min(hi, P - 1);
 }
 
+// Row `tok`'s map g over keys lo .. hi by one wave, a key a lane for the scores, columns lane, lane + 64, .. of `cols` for the sums;
+// rows(j): pool row of key j.  Returns maximum and weight.
+template <typename T, int COLS, class F>
+__device__ float2 wave_row(const RowsArgs &a, const T *q, int dh, const T *k, const T *c, float slope, int own, int lo, int hi, F rows,
+                           float (&acc)[COLS]) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+#pragma unroll 1
+  for (int64_t j0 = lo; j0 <= hi; j0 += 64) {
+    const int cnt = (int)min((int64_t)64, hi - j0 + 1);
+    float sc = -INFINITY;
+    int64_t row = 0;
+    if (lane < cnt) {
+      row = rows((int)j0 + lane);
+      const T *kr = k + row * a.ks;
+      float dot = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < dh; ++i) dot = fmaf((float)kr[i], (float)q[i], dot);
+      sc = ruled_score(a.rules, dot, slope, fabsf((float)(own - ((int)j0 + lane))));
+    }
+    float mx = sc;
+    for (int i = 32; i; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
+    const float mn = fmaxf(m, mx), ref = mn > -INFINITY ? mn : 0.f, corr = __builtin_amdgcn_exp2f(m - ref);
+    const float p = lane < cnt ? __builtin_amdgcn_exp2f(sc - ref) : 0.f;
+    float sum = p;
+    for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
+    m = mn;
+    l = fmaf(l, corr, sum);
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) acc[i] *= corr;
+#pragma unroll 1
+    for (int t = 0; t < cnt; ++t) {
+      const float pt = __shfl(p, t);
+      const int64_t at = ((int64_t)__shfl((int)(row >> 32), t) << 32) | (unsigned)__shfl((int)row, t);
+      const T *cr = c + at * a.cs;
+#pragma unroll
+      for (int i = 0; i < COLS; ++i) acc[i] = fmaf(pt, (float)cr[i * 64 + lane], acc[i]);
+    }
+  }
+  return make_float2(m, l);
+}
+
 // bf16 (gta_masked_bf16.hip)
 bool rows_bf16_ok(const Dims &d);
+int masked_bf16_columns(const Dims &d);   // latent columns of a workgroup of 128 rows
+void launch_masked_bf16(const Dims &d, const RowsArgs &a, hipStream_t st);
+// fp32 (gta_masked_f32.hip): rows of 32 per tile
+bool rows_f32_ok(const Dims &d);
+int rows_f32_columns(const Dims &d);
+void launch_rows_f32(const Dims &d, const RowsArgs &a, bool cache, hipStream_t st);
+// either (gta_masked_plan.hip)
+bool masked_tuned(const Dims &d);
+bool masked_fits(const Dims &d, int batch, int64_t total);
 bool rows_operands_ok(const void *p, int64_t stride, int esize);
-bool masked_bf16_fits(const Dims &d, int batch, int64_t total);
-size_t masked_bf16_bytes(const Dims &d, int batch, int64_t total);
-int launch_masked_bf16(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st);
+size_t masked_bytes(const Dims &d, int batch, int64_t total);
+int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st);
 
 // The prefix's rows: rows of a tile for `rows` query rows of a cell, workgroups that share its latent columns, launch
 int prefix_tile_rows(const Dims &d, int rows);
