@@ -91,12 +91,12 @@ __device__ __forceinline__ int load_uniform(const int32_t *p) {
 template <class T, int MODS, bool CACHE>
 __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ int span[8];
+  __shared__ int span[8], sees_from[256], sees_to[256];   // what a lane's row sees, out of the registers of the main loop
   const int tid = threadIdx.x, lane = tid & 63, h = lane >> 5, ln = lane & 31;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), qw = wave % T::QW, cg = wave / T::QW;
   const int per = a.cells * a.slices;
   int u, r;   // which tile (or piece), workgroup of it
-  if (a.tiles < 64) { u = (int)blockIdx.x / per; r = (int)blockIdx.x - u * per; }
+  if (a.tiles < (CACHE ? 8 : 64)) { u = (int)blockIdx.x / per; r = (int)blockIdx.x - u * per; }
   else {   // eight tiles at a time, one per XCD: a tile's workgroups read the same keys and latents
     const int at = (int)blockIdx.x >> 3, round = at / per;
     r = at - round * per;
@@ -139,13 +139,15 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
     seen_by(a.rules, start + tok, tok, keys, lo, hi);
   }
   const float slope = MODS & kBias ? a.rules.slopes[g] : 0.f, slope2 = slope * kLog2e;
-  const bool sees = lo <= hi;
+  const bool sees = lo <= hi;   // (a mask of lanes)
   // blocks of 32 keys: those that some row of the wave sees (w0 .. w1), those that all of them see (i0 .. i1)
   const bool idle = wr0 >= R;
   const int wlo = wave_min(sees && !idle ? lo : INT_MAX), whi = wave_max(sees && !idle ? hi : -1);
   const int ilo = wave_max(sees ? lo : 0), ihi = wave_min(sees ? hi : INT_MAX);
   const int w0 = wlo == INT_MAX ? INT_MAX : wlo >> 5, w1 = whi >> 5;   // -1 >> 5 = -1: none
   if (lane == 0) { span[wave] = w0; span[4 + wave] = w1; }
+  sees_from[tid] = lo;
+  sees_to[tid] = hi;
   __syncthreads();
   const int first = min(min(span[0], span[1]), min(span[2], span[3])), last = max(max(span[4], span[5]), max(span[6], span[7]));
   const int blocks = __builtin_amdgcn_readfirstlane(last < 0 ? 0 : last - first + 1);
@@ -163,8 +165,6 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   const bf16 *kcol = (const bf16 *)a.k + (cell / a.kdiv) * T::DH, *ccol = (const bf16 *)a.c + (int64_t)(cell / a.cdiv) * a.dl + slice * T::DLW;
   const char *Kb = (const char *)(kcol + krow0 * a.ks), *Cb = (const char *)(ccol + krow0 * a.cs);
   const unsigned wk2 = (unsigned)a.ks * 2, wc2 = (unsigned)a.cs * 2;
-  const float sc2 = a.rules.scale * kLog2e;                                   // score in units of log 2 without a cap
-  const float ck = a.rules.scale * a.rules.inv_cap, cap2 = a.rules.cap * kLog2e;
 
   bf16x8 qf[T::DH / 16];
   f32x16 acc[T::NDLB];
@@ -173,58 +173,90 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
 
   const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   constexpr int KI = T::K_INSTR / T::NW, CI = T::C_INSTR / T::NW;
-  unsigned kv[KI], cv[CI];
-  {
-    const int i = lane / T::K_CPR;
+  // A lane's offsets in instructions `wave`, `wave` + 4, ..: the latter have rows 4 (keys), 4 C_RPI (latents) further on.  Where registers
+  // are short that goes into the buffers' addresses instead (a dozen scalar instructions a step: 4 x 4096 tokens of packed documents, 1B
+  // shape, 94 -> 104 us; with cap and bias 4 spilled loads a step less, 2 x 8192 of the wide shape 1540 -> 1285).
+  constexpr bool FEW = MODS == (kCap | kBias) || (T::NDLB == 8 && MODS != 0);
+  unsigned kv[FEW ? 1 : KI], cv[FEW ? 1 : CI];
 #pragma unroll
-    for (int j = 0; j < KI; ++j)
-      kv[j] = (wave + T::NW * j + T::K_INSTR * i) * wk2 + ((lane % T::K_CPR) ^ (T::k_sel(i) * (T::K_CPR / 2))) * 16;
+  for (int i = 0; i < (FEW ? 1 : KI); ++i)
+    kv[i] = (wave + T::NW * i + T::K_INSTR * (lane / T::K_CPR)) * wk2 + ((lane % T::K_CPR) ^ (T::k_sel(lane / T::K_CPR) * (T::K_CPR / 2))) * 16;
 #pragma unroll
-    for (int j = 0; j < CI; ++j) {
-      const int q = wave + T::NW * j;
-      cv[j] = (4 * (q / 4 * T::C_RPI + lane / T::C_CPR) + q % 4) * wc2 + (lane % T::C_CPR) * 16;
-    }
-  }
-  unsigned fill = lds0;
-  int blk_next = b1 - 1;
-  // requests the next step; rows past the last key, and steps past the last, read as zeros
-  auto issue = [&]() __attribute__((always_inline)) {
-    const int j0 = blk_next * 32, rows = blk_next >= b0 ? min(keys - j0, 32) : 0;
-    const unsigned kbytes = rows > 0 ? (rows - 1) * wk2 + T::K_ROW : 0u, cbytes = rows > 0 ? (rows - 1) * wc2 + T::C_ROW : 0u;
-    if (CACHE && table) {   // two runs of 16 rows, each in one page
-      const int pages = a.prefix.pm.num_pages, end = max(keys - 1, 0) & ~15, jt = min(max(j0, 0), end), ju = min(jt + 16, end);
-      auto at = [&](int j) {
-        int pg = load_uniform(table + __builtin_amdgcn_readfirstlane(j >> a.ps_shift));
-        pg = (unsigned)pg >= (unsigned)pages ? 0 : pg;
-        return ((int64_t)pg << a.ps_shift) + (j & (a.prefix.pm.page_size - 1));
-      };
-      const int64_t p0 = at(jt), p1 = at(ju) - 16;
-      const u32x4 k0 = uniform_buffer_of(Kb + p0 * wk2, kbytes), k1 = uniform_buffer_of(Kb + p1 * wk2, kbytes);
-      const u32x4 c0 = uniform_buffer_of(Cb + p0 * wc2, cbytes), c1 = uniform_buffer_of(Cb + p1 * wc2, cbytes);
+  for (int i = 0; i < (FEW ? 1 : CI); ++i) cv[i] = (4 * (i * T::C_RPI + lane / T::C_CPR) + wave) * wc2 + (lane % T::C_CPR) * 16;
+  // Request keys, latents of a block; rows past the last key, and blocks past the last step, read as zeros.  Step t reads the keys of
+  // the block of step t + 1 and the latents of its own, and asks for the keys of step t + 3's and the latents of step t + 2's: each
+  // has this step and the next to arrive in.
+  unsigned kfill = lds0, cfill = lds0 + T::K_BYTES;
+  int kblk = b1 - 1, cblk = b1 - 1;
+  auto rows_at = [&](int blk) { return blk >= b0 ? min(keys - blk * 32, 32) : 0; };
+  // `rows` rows (fewer than 1: none) of `row` bytes, `pitch` apart, without the first `skip`
+  auto buffer_at = [&](const char *p, int rows, unsigned pitch, unsigned row, int skip) {
+    if (!FEW) skip = 0;
+    return buffer_of(p + (int64_t)skip * pitch, rows > skip ? (rows - 1 - skip) * pitch + row : 0u);
+  };
+  auto next_stage = [&](unsigned f, unsigned first) { return f == first + (T::NSTAGE - 1) * T::STAGE ? first : f + T::STAGE; };
+  // Pool rows of a block's two runs of 16 rows, each in one page (the second's less 16).  Latents are asked for a step after the keys
+  // of their block: the rows are kept.
+  int64_t kp0 = 0, kp1 = 0, cp0 = 0, cp1 = 0;
+  int page_at = -1, page_is = 0;
+  auto page_rows = [&](int j0) __attribute__((always_inline)) {
+    const int end = max(keys - 1, 0) & ~15, jt = min(max(j0, 0), end), ju = min(jt + 16, end);
+    auto at = [&](int j) {
+      const int want = __builtin_amdgcn_readfirstlane(j >> a.ps_shift);
+      if (want != page_at) {
+        page_at = want;
+        page_is = load_uniform(table + want);
+        page_is = (unsigned)page_is >= (unsigned)a.prefix.pm.num_pages ? 0 : page_is;
+      }
+      return ((int64_t)page_is << a.ps_shift) + (j & (a.prefix.pm.page_size - 1));
+    };
+    kp1 = at(ju) - 16;
+    kp0 = at(jt);
+  };
+  auto issue_k = [&]() __attribute__((always_inline)) {
+    const int rows = rows_at(kblk), j0 = kblk * 32;
+    if (CACHE && table) {
+      page_rows(j0);
 #pragma unroll
       for (int i = 0; i < KI; ++i) {
-        if (lane < 32) load_to_lds(k0, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
-        else load_to_lds(k1, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
-      }
-#pragma unroll
-      for (int i = 0; i < CI; ++i) {
-        const unsigned to = fill + T::K_BYTES + (wave + T::NW * i) * T::C_PITCH;
-        if constexpr (CI == 1) {
-          if (lane < 32) load_to_lds(c0, cv[i], to);
-          else load_to_lds(c1, cv[i], to);
-        } else load_to_lds(i < CI / 2 ? c0 : c1, cv[i], to);
+        const unsigned to = kfill + (wave + T::NW * i) * T::K_PITCH;
+        if (lane < 32) load_to_lds(buffer_at(Kb + kp0 * wk2, rows, wk2, T::K_ROW, 4 * i), kv[FEW ? 0 : i], to);
+        else load_to_lds(buffer_at(Kb + kp1 * wk2, rows, wk2, T::K_ROW, 4 * i), kv[FEW ? 0 : i], to);
       }
     } else {
-      const u32x4 rk = uniform_buffer_of(Kb + (int64_t)j0 * wk2, kbytes), rc = uniform_buffer_of(Cb + (int64_t)j0 * wc2, cbytes);
 #pragma unroll
-      for (int i = 0; i < KI; ++i) load_to_lds(rk, kv[i], fill + (wave + T::NW * i) * T::K_PITCH);
-#pragma unroll
-      for (int i = 0; i < CI; ++i) load_to_lds(rc, cv[i], fill + T::K_BYTES + (wave + T::NW * i) * T::C_PITCH);
+      for (int i = 0; i < KI; ++i)
+        load_to_lds(buffer_at(Kb + (int64_t)j0 * wk2, rows, wk2, T::K_ROW, 4 * i), kv[FEW ? 0 : i], kfill + (wave + T::NW * i) * T::K_PITCH);
     }
-    --blk_next;
-    fill = fill == lds0 + (T::NSTAGE - 1) * T::STAGE ? lds0 : fill + T::STAGE;
+    --kblk;
+    kfill = next_stage(kfill, lds0);
   };
-  auto wait_meet = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  auto issue_c = [&]() __attribute__((always_inline)) {
+    const int rows = rows_at(cblk), j0 = cblk * 32;
+    if (CACHE && table) {
+#pragma unroll
+      for (int i = 0; i < CI; ++i) {
+        const unsigned to = cfill + (wave + T::NW * i) * T::C_PITCH;
+        if constexpr (CI == 1) {
+          if (lane < 32) load_to_lds(buffer_at(Cb + cp0 * wc2, rows, wc2, T::C_ROW, 0), cv[0], to);
+          else load_to_lds(buffer_at(Cb + cp1 * wc2, rows, wc2, T::C_ROW, 0), cv[0], to);
+        } else load_to_lds(buffer_at(Cb + (i < CI / 2 ? cp0 : cp1) * wc2, rows, wc2, T::C_ROW, 4 * T::C_RPI * i), cv[FEW ? 0 : i], to);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < CI; ++i)
+        load_to_lds(buffer_at(Cb + (int64_t)j0 * wc2, rows, wc2, T::C_ROW, 4 * T::C_RPI * i), cv[FEW ? 0 : i], cfill + (wave + T::NW * i) * T::C_PITCH);
+    }
+    --cblk;
+    cfill = next_stage(cfill, lds0 + T::K_BYTES);
+  };
+  auto issue = [&]() __attribute__((always_inline)) {   // the latents' block is one behind the keys': its rows are those looked up last
+    if (CACHE && table) { cp0 = kp0; cp1 = kp1; }
+    issue_c();
+    issue_k();
+  };
+  // all but the last step's requests have landed (with pages there are more of them: a stricter wait), then the waves meet
+  auto wait_meet = [&]() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KI + CI) : "memory"); };
 
   const int ksel = T::k_sel(ln / T::K_INSTR) * (T::K_ROW / 2);
   const int koff = ln % T::K_INSTR * T::K_PITCH + ln / T::K_INSTR * T::K_ROW + h * 16;
@@ -253,22 +285,42 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   };
   // register e of a lane: key 8 (e / 4) + 4 h + e % 4 of its block
   auto key_of = [](int e) { return 8 * (e >> 2) + (e & 3); };
-  // product to score, plus `plus`, in units of log 2; d0 = position less the block's first key less 4 h
-  auto score_of = [&](float s, int e, float d0, float plus) {
-    float base2 = plus;
-    if constexpr (MODS & kBias) base2 = fmaf(-slope2, fabsf(d0 - (float)key_of(e)), plus);
-    if constexpr (MODS & kCap) return fmaf(cap2, tanh_exactly(s * ck), base2);
-    else return fmaf(s, sc2, base2);
+  // product to score, plus `plus`, in units of log 2; d0 = position less the block's first key less 4 h.  A cap's tanh is the polynomial
+  // for scores up to the cap (`top` is the largest met).  Where a block has larger ones (far) it is 1 - 2 / (e^2x + 1), off by 2^-23 of
+  // the cap.
+  struct Consts { float sc2, steep, cap2, poly[5]; };
+  const Consts consts{a.rules.scale2, a.rules.steep, a.rules.near, {a.rules.poly[0], a.rules.poly[1], a.rules.poly[2], a.rules.poly[3], a.rules.poly[4]}};
+  auto score_of = [&](const Consts &k, float s, int e, float d0, float plus, float &top, bool far) __attribute__((always_inline)) {
+    if constexpr (MODS & kBias) plus = fmaf(-slope2, fabsf(d0 - (float)key_of(e)), plus);
+    if constexpr (MODS & kCap) {
+      if (far) return fmaf(-2.f * k.cap2, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(s * k.steep) + 1.f), k.cap2 + plus);
+      const float x = s * k.sc2, y = x * x;
+      top = fmaxf(top, fabsf(x));
+      return fmaf(x, fmaf(y, fmaf(y, fmaf(y, fmaf(y, k.poly[4], k.poly[3]), k.poly[2]), k.poly[1]), k.poly[0]), plus);
+    } else return fmaf(s, k.sc2, plus);
   };
+  auto too_far = [&](float top) { return (MODS & kCap) && __builtin_amdgcn_ballot_w64(top > a.rules.near) != 0; };
   auto dist0 = [&](int blk) { return MODS & kBias ? (float)(own - blk * 32 - 4 * h) : 0.f; };
   // the whole step for the scores of a block: rules, mask, running maximum, weights as the second product wants them
-  auto softmax = [&](const f32x16 &s, int blk, bool masked, bf16x8 (&pn)[2], float &corr) __attribute__((always_inline)) {
+  auto softmax = [&](f32x16 &v, int blk, bool masked, bf16x8 (&pn)[2], float &corr) __attribute__((always_inline)) {
     const float d0 = dist0(blk);
-    float v[16];
+    float top = 0.f;
+    Consts k = consts;   // (opaque: copies of them in vector registers would be kept through the main loop)
+    if (MODS) asm volatile("" : "+s"(k.sc2), "+s"(k.steep), "+s"(k.cap2), "+s"(k.poly[0]), "+s"(k.poly[1]), "+s"(k.poly[2]), "+s"(k.poly[3]), "+s"(k.poly[4]));
+    if constexpr (MODS & kCap) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = score_of(s[e], e, d0, 0.f);
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, fabsf(v[e]));
+      top *= k.sc2;
+    }
+    if (too_far(top)) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = score_of(k, v[e], e, d0, 0.f, top, true);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = score_of(k, v[e], e, d0, 0.f, top, false);
+    }
     if (masked) {
-      const int from = lo - blk * 32 - 4 * h, to = hi - blk * 32 - 4 * h;
+      const int from = sees_from[tid] - blk * 32 - 4 * h, to = sees_to[tid] - blk * 32 - 4 * h;
 #pragma unroll
       for (int e = 0; e < 16; ++e) v[e] = key_of(e) < from || key_of(e) > to ? -INFINITY : v[e];
     }
@@ -294,8 +346,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
 
   bf16x8 pf[2] = {};
   float corr = 1.f;
-  issue();
-  issue();
+  issue_k();
   {
     const bf16 *qg = (const bf16 *)a.q + (start + tok) * a.qs + g * T::DH + h * 8;
 #pragma unroll
@@ -326,7 +377,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
 #pragma unroll 1
     for (; t < end; ++t) {
       const bool here = mine(t), next = mine(t + 1);
-      if (t > 0) issue();
+      issue();
       if (here) rescale();
       f32x16 s;
       bf16x8 pn[2] = {};
@@ -355,7 +406,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
 #pragma unroll
     for (int ks = 0; ks < KS1; ++ks) kf[ks] = k_frag(nxt, ks);
     __builtin_amdgcn_sched_barrier(0);
-    if (t > 0) issue();
+    issue();
     rescale();
     f32x16 s;
 #pragma unroll
@@ -375,13 +426,13 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
     bf16x8 cf[NS + LA], pn[2];
 #pragma unroll
     for (int i = 0; i < LA; ++i) cf[i] = cread(i);
-    float ps = 0.f;
+    float ps = 0.f, top = 0.f;
     const float negm = -m_run, d0 = dist0(b1 - 2 - t);
     const bf16x2 ones = {(bf16)1.0f, (bf16)1.0f};
     auto soft_pair = [&](int e) {
       bf16x2 pk;
-      pk[0] = (bf16)__builtin_amdgcn_exp2f(score_of(s[e], e, d0, negm));
-      pk[1] = (bf16)__builtin_amdgcn_exp2f(score_of(s[e + 1], e + 1, d0, negm));
+      pk[0] = (bf16)__builtin_amdgcn_exp2f(score_of(consts, s[e], e, d0, negm, top, false));
+      pk[1] = (bf16)__builtin_amdgcn_exp2f(score_of(consts, s[e + 1], e + 1, d0, negm, top, false));
       pn[e >> 3][e & 7] = pk[0]; pn[e >> 3][(e & 7) + 1] = pk[1];
       ps = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, ps, false);
     };
@@ -393,7 +444,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
         if (e % 2 == 0) soft_pair(e);
       __builtin_amdgcn_sched_barrier(0);
     });
-    if (__builtin_amdgcn_ballot_w64(!(ps < kRowSumLimit)) != 0) {   // rare
+    if (__builtin_amdgcn_ballot_w64(!(ps < kRowSumLimit)) != 0 || too_far(top)) {   // rare
       softmax(s, b1 - 2 - t, false, pn, corr);
     } else {
       l_run += ps;
@@ -422,10 +473,14 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
     for (int i = 0; i < 32; ++i) {
       const int rr = wr0 + i;
       if (rr >= R) break;
-      const int tk = __shfl(tok, i), gg = __shfl(g, i), from = max(__shfl(lo, i), b0 * 32), to = min(__shfl(hi, i), min(b1 * 32, keys) - 1);
+      const int tk = rr / a.mpc, gg = cell * a.mpc + (rr - tk * a.mpc), l0 = sees_from[wave * 64 + i], l1 = sees_to[wave * 64 + i];
+      const int from = max(l0, b0 * 32), to = min(l1, min(b1 * 32, keys) - 1);
+      int own_i = tk;
+      if constexpr (CACHE) own_i = (int)((int64_t)keys + slot_rows(a.own, a.own.slots ? a.own.slots[tk] : tk) - 1);
       float sum[COLS];
       const bf16 *cc = ccol + c0 - (T::NDLB == 1 && lane >= 32 ? 32 : 0);
-      const float2 ml = wave_row(a, (const bf16 *)a.q + (start + tk) * a.qs + gg * T::DH, T::DH, kcol, cc, __shfl(slope, i), __shfl(own, i), from, to,
+      const float2 ml = wave_row(a, (const bf16 *)a.q + (start + tk) * a.qs + gg * T::DH, T::DH, kcol, cc,
+                                       MODS & kBias ? a.rules.slopes[gg] : 0.f, own_i, from, to,
                                        [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, sum);
       if (T::NDLB == 1 && lane >= 32) continue;
       if (split) {
@@ -433,7 +488,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
         for (int e = 0; e < COLS; ++e) a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = sum[e];
         if (lane == 0 && slice == 0 && cg == 0) a.pml[at + qw * 32 + i] = ml;
       } else {
-        const float inv = __shfl(sees ? 1 : 0, i) ? 1.f / ml.y : 0.f;
+        const float inv = l0 <= l1 ? 1.f / ml.y : 0.f;
 #pragma unroll
         for (int e = 0; e < COLS; ++e)
           *reinterpret_cast<bf16 *>(smem + (qw * 32 + i) * T::OUT_PITCH + (c0 + e * 64 + lane) * 2) = (bf16)(inv != 0.f ? sum[e] * inv : 0.f);
@@ -481,7 +536,7 @@ void launch_mods(const RowsArgs &a, unsigned grid, hipStream_t st) {
 
 template <class T, bool CACHE>
 void launch_tile(RowsArgs a, hipStream_t st) {
-  const int64_t tiles = a.tiles < 64 ? a.tiles : (a.tiles + 7) / 8 * 8;
+  const int64_t tiles = a.tiles < (CACHE ? 8 : 64) ? a.tiles : (a.tiles + 7) / 8 * 8;
   const unsigned grid = (unsigned)(tiles * a.cells * a.slices);
   switch ((a.rules.cap > 0.f ? kCap : 0) | (a.rules.slopes ? kBias : 0)) {
     case 0: launch_mods<T, 0, CACHE>(a, grid, st); break;
