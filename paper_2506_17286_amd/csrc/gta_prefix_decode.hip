@@ -24,13 +24,14 @@ typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 struct StreamArgs {
   const void *q;
   CacheView prefix, own;
-  int prefix_slot, batch, nq, qpk, qpc, dh, dl, kw, cw;
+  int prefix_slot, batch, nq, qpk, qpc, dl, kw, cw;
   Rules rules;
   int maps, blocks;            // maps of a workgroup, workgroups of a latent group's maps
   int heads;                   // key heads that a workgroup's maps read at most
-  int pieces, ps_shift;
-  int rows, stages, stage_bytes, k_instr, instr;   // of a tile: rows, load instructions of its keys and in all (1 KiB each)
-  float *pacc; float2 *pml;    // [batch, pieces, n_q, d_l], [batch, pieces, n_q]
+  int wave_lds, ps_shift;      // bytes of a wave
+  int share, each;             // workgroups that a batch's tiles are shared out to; or (> 0) pieces of every sequence
+  int32_t *first;              // [batch + 1] pieces in front of each sequence
+  float *pacc; float2 *pml;    // [pieces, n_q, d_l], [pieces, n_q]
 };
 
 __device__ __forceinline__ int load_uniform(const int32_t *p) {
@@ -55,39 +56,106 @@ __device__ __forceinline__ void wait_loads(int n) {
 }
 
 constexpr float kLazy = 8.0f;        // log2 units by which a score may pass the maximum that weights refer to
-constexpr int kMaxInstr = 16;        // load instructions of a wave and tile
+constexpr int kShared = 64;          // sequences of a batch whose tiles are shared out evenly, a lane each
 
-// A workgroup has up to 16 maps of one latent group of a sequence and NF * 64 of its latent columns.  Tiles of 16 or 32 rows,
-// keys and latents, go from memory straight into LDS, `stages` of them, one barrier a tile; every wave has the scores of all maps
-// (16 columns of a 16 x 16 product, its own head's kept) and sums up a quarter of the columns:
-//   S[row][map] = K q^T: lane (x = l % 16, h = l / 16) ends up with map x, rows 4 h .. 4 h + 3;
-//   L[column][map] += C^T p: which is what the second operand of the other product wants from it.
-// Bound by memory: every row is read once (once per head or slice where a layer's rows are wider than a workgroup's, from L2).
+// Rows lo .. hi of the sequence itself that its new token sees (none: hi < lo); n of them are cached, `own` is the token's position
+__device__ __forceinline__ void own_rows(const StreamArgs &a, int b, int &slot, int &n, int &own, int &lo, int &hi) {
+  slot = a.own.slots ? a.own.slots[b] : b;
+  const int P = slot_rows(a.prefix, a.prefix_slot);
+  n = slot_rows(a.own, slot);
+  own = (int)((int64_t)P + n - 1);
+  seen_by(a.rules, b, own, own + 1, lo, hi);
+  lo = max(lo - P, 0);
+  hi -= P;
+}
+
+// inclusive sums over the lanes of a wave
+__device__ __forceinline__ int wave_scan(int v) {
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    const int up = __shfl_up(v, i);
+    v += (int)(threadIdx.x & 63) >= i ? up : 0;
+  }
+  return v;
+}
+
+// Pieces in front of and of sequence b (lane b) and how many there are, where a batch is shared out: a round is what a workgroup's
+// waves take at a time, and T rounds make a piece, T the least of a growing series with which there are no more pieces than
+// workgroups, all at once on the chip.  Batches of many sequences are cut finer and dealt out as workgroups end.
+template <int NWV>
+__device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &mine) {
+  const int b = threadIdx.x & 63;
+  int rounds = 0;
+  if (b < a.batch) {
+    int slot, n, own, lo, hi;
+    own_rows(a, b, slot, n, own, lo, hi);
+    if (lo <= hi) rounds = min(((hi >> 4) - (lo >> 4) + NWV) / NWV, 1 << 24);   // (64 of them fit 32 bits)
+  }
+  const int total = __shfl(wave_scan(rounds), 63), some = __popcll(__ballot(rounds > 0));
+  int t = max(1, (total + a.share - 1) / a.share);
+  if (2 * some > a.share) t = max(1, (total + 2 * a.share - 1) / (2 * a.share));
+  else
+#pragma unroll 1
+    while (__shfl(wave_scan((rounds + t - 1) / t), 63) > a.share) t += (t + 7) / 8;
+  mine = (rounds + t - 1) / t;
+  const int run = wave_scan(mine);
+  before = run - mine;
+  return __shfl(run, 63);
+}
+
+// A workgroup has a piece of one sequence's rows, up to 16 maps of one latent group and SW = NF * 64 of its latent columns.  A wave takes
+// tiles of 16 rows, keys and latents, by itself: they go from memory straight into LDS of its own, the next tile's keys as this
+// one's have been read, its latents likewise, so that about a tile per wave is on its way at any time, and no barrier is met before the
+// waves' sums are joined.
+//   S[row][map] = K q^T: lane (x = l % 16, h = l / 16) ends up with map x, rows 4 h .. 4 h + 3 (of each key head; its own is kept);
+//   L[column][map] += C^T p: which is what the second operand wants from that lane.
+// Bound by memory: every row is read once (once per block of maps or slice where a layer's rows are wider than 4 KiB, then from L2).
 // bf16 weights are rounded for the second product, as in the kernel of the prefix, and so is their sum.  (Two parts of 16 bits would
 // cost nothing here, but an infinite latent times the second, which may be 0 or less, is no infinity.)
 // Rows in front of the first that is seen are cleared in LDS, rows behind the last read as zeros: what is masked has the weight 0, and
 // that times a latent that is not finite would not be.
-template <typename T, int DH, int NF>
-__global__ __launch_bounds__(256, NF > 8 ? 1 : 2) void stream_kernel(StreamArgs a) {
-  constexpr int ES = sizeof(T), KS = DH * ES / 64, KCH = DH * ES / 16;   // 64-byte steps and chunks of a key head
-  constexpr int SW = NF * 64, CP = SW * ES, CCH = CP / 16;               // latent columns, their bytes and chunks a row
+template <typename T, int DH, int NF, int NWV>
+__global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(StreamArgs a) {
+  constexpr int ES = sizeof(T), KS = DH * ES / 64, KCH = DH * ES / 16;   // 64-byte steps and 16-byte chunks of a key head
+  constexpr int SW = NF * 64, CP = SW * ES, CCH = CP / 16, NFR = NF * 4;  // latent columns, their bytes and chunks a row, blocks of 16
   constexpr int PM = CCH / 2 < 8 ? CCH / 2 - 1 : 7;                      // pairs of chunks that rows are swapped over (bf16)
+  constexpr int KI = KCH / 4, CI = CCH / 4;                              // load instructions (1 KiB) of a head's, of the latents' 16 rows
+  constexpr int KR = 64 / KCH, CR = CCH < 64 ? 64 / CCH : 1;             // rows of an instruction
   extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ float2 stats[NWV][16];
   const int tid = threadIdx.x, lane = tid & 63, x = lane & 15, h = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int b = blockIdx.z, piece = blockIdx.x, slices = a.dl / SW;
-  const int slice = blockIdx.y % slices, rest = blockIdx.y / slices, block = rest % a.blocks, cgrp = rest / a.blocks;
+  const int slices = a.dl / SW, slice = blockIdx.y % slices, rest = blockIdx.y / slices, block = rest % a.blocks, cgrp = rest / a.blocks;
   const int g0 = cgrp * a.qpc + block * a.maps, gn = min(a.maps, a.qpc - block * a.maps);   // maps g0 .. g0 + gn - 1
   const int kh0 = g0 / a.qpk, heads = (g0 + gn - 1) / a.qpk - kh0 + 1;
-  const int slot = a.own.slots ? a.own.slots[b] : b, P = slot_rows(a.prefix, a.prefix_slot), n = slot_rows(a.own, slot);
-  const int own = (int)((int64_t)P + n - 1);
-  int lo, hi;
-  seen_by(a.rules, b, own, own + 1, lo, hi);
-  lo = __builtin_amdgcn_readfirstlane(max(lo - P, 0));      // rows of the sequence itself
-  hi = __builtin_amdgcn_readfirstlane(hi - P);
-  const int64_t at = ((int64_t)b * a.pieces + piece) * a.nq + g0;
-  const int t_lo = lo / a.rows, tiles = hi < lo ? 0 : hi / a.rows - t_lo + 1;
-  const int t0 = t_lo + (int)((int64_t)tiles * piece / a.pieces), t1 = t_lo + (int)((int64_t)tiles * (piece + 1) / a.pieces);
+  int b, piece, pieces;
+  const int id = blockIdx.x;
+  if (a.each) {
+    b = id / a.each; piece = id - b * a.each; pieces = a.each;
+    if (id == 0 && blockIdx.y == 0)
+      for (int i = tid; i <= a.batch; i += NWV * 64) a.first[i] = i * a.each;
+  } else {
+    int before, mine;
+    const int all = share_out<NWV>(a, before, mine);
+    if (id == 0 && blockIdx.y == 0 && tid <= a.batch) a.first[tid] = tid < a.batch ? before : all;   // (a.batch < 64 or this lane has `all`)
+    if (id == 0 && blockIdx.y == 0 && tid == 0) a.first[a.batch] = all;
+    if (id >= all) return;
+    b = 63 - __builtin_clzll(__ballot(lane < a.batch && mine > 0 && before <= id));
+    piece = id - __shfl(before, b);
+    pieces = __shfl(mine, b);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+  piece = __builtin_amdgcn_readfirstlane(piece);
+  pieces = __builtin_amdgcn_readfirstlane(pieces);
+  int slot, n, own, lo, hi;
+  own_rows(a, b, slot, n, own, lo, hi);
+  slot = __builtin_amdgcn_readfirstlane(slot);
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  n = __builtin_amdgcn_readfirstlane(n);
+  const int64_t at = (int64_t)id * a.nq + g0;
+  const int t_lo = lo >> 4, tiles = hi < lo ? 0 : (hi >> 4) - t_lo + 1;
+  const int t0 = t_lo + (int)((int64_t)tiles * piece / pieces), t1 = t_lo + (int)((int64_t)tiles * (piece + 1) / pieces);
   if (t0 >= t1) {
     if (slice == 0 && tid < gn) a.pml[at + tid] = make_float2(-INFINITY, 0.f);
     return;
@@ -95,59 +163,50 @@ __global__ __launch_bounds__(256, NF > 8 ? 1 : 2) void stream_kernel(StreamArgs 
   const int g = min(g0 + x, g0 + gn - 1), head = g / a.qpk - kh0;   // this lane's map (lanes without one repeat the last)
   const float slope = a.rules.slopes ? a.rules.slopes[g] : 0.f;
 
-  const int us = __builtin_amdgcn_readfirstlane(slot);
-  const int32_t *table = a.own.pm.table ? a.own.pm.table + (int64_t)us * a.own.pm.pages_per_slot : nullptr;
-  const int64_t row0 = table ? 0 : (int64_t)us * a.own.max_seq;
+  const int32_t *table = a.own.pm.table ? a.own.pm.table + (int64_t)slot * a.own.pm.pages_per_slot : nullptr;
+  const int64_t row0 = table ? 0 : (int64_t)slot * a.own.max_seq;
   const char *Kb = (const char *)((const T *)a.own.k + row0 * a.kw + (int64_t)kh0 * DH);
   const char *Cb = (const char *)((const T *)a.own.c + row0 * a.cw + (int64_t)cgrp * a.dl + slice * SW);
   const unsigned kws = (unsigned)a.kw * ES, cws = (unsigned)a.cw * ES;
-  const int KP = a.heads * DH * ES, kch = KP / 16;
 
-  // This wave's load instructions of a tile are wave, wave + 4, ..; slot s of a row holds the row's chunk s, swapped with others so
-  // that 16 rows' reads of one chunk fall into different banks.
-  unsigned voff[kMaxInstr];
+  // Slot s of a row in LDS holds its chunk s, swapped with others so that 16 rows' reads of one chunk fall into different banks: keys
+  // s ^ (row % 8), bf16 latents pairs of chunks ^ row, fp32 latents blocks of four chunks ^ row / 4.  A lane's part of that and of the
+  // offset here, an instruction's where it is issued.
+  const unsigned klane = (lane / KCH) * kws, kchunk = lane % KCH ^ (lane / KCH & 7);
+  const int clr = CCH < 64 ? lane / CCH : 0;
+  const unsigned clane = clr * cws, cchunk = (CCH < 64 ? lane % CCH : lane) ^ (ES == 2 ? (clr & PM) * 2 : 0);
+  char *mem = smem + wave * a.wave_lds;
+  const unsigned klds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)mem, clds = klds + a.heads * KI * 1024;
+  const char *kmem = mem, *cmem = mem + a.heads * KI * 1024;
+  int64_t p0 = 0;   // pool row of the tile in work on
+  auto find = [&](int t) {   // its 16 rows lie in one page
+    const int j = min(t * 16, hi & ~15);
+    if (!table) return (int64_t)j;
+    int pg = load_uniform(table + __builtin_amdgcn_readfirstlane(j >> a.ps_shift));
+    pg = (unsigned)pg >= (unsigned)a.own.pm.num_pages ? 0 : pg;
+    return ((int64_t)pg << a.ps_shift) + (j & (a.own.pm.page_size - 1));
+  };
+  auto rows_of = [&](int t) { return t < t1 ? min(hi + 1 - t * 16, 16) : 0; };
+  auto issue_k = [&](int t) __attribute__((always_inline)) {
+    const int rows = rows_of(t);
+    const u32x4 r = uniform_buffer_of(Kb + p0 * kws, rows > 0 ? (rows - 1) * kws + heads * DH * ES : 0u);
+    unsigned to = klds;
+#pragma unroll 1
+    for (int kk = 0; kk < heads; ++kk) {
 #pragma unroll
-  for (int i = 0; i < kMaxInstr; ++i) {
-    const int in = wave + 4 * i;
-    if (in < a.k_instr) {
-      const int s = in * 64 + lane, row = s / kch, c = s % kch ^ (row & 7);
-      voff[i] = c * 16 < heads * DH * ES ? row * kws + c * 16 : ~0u - 15u;   // (fewer heads than others' maps read: nothing)
-    } else {
-      const int s = (in - a.k_instr) * 64 + lane, row = s / CCH;
-      int c = s % CCH;
-      if constexpr (ES == 2) c = ((c >> 1) ^ (row & PM)) * 2 + (c & 1);
-      else c = ((c >> 2) ^ ((row >> 2) & 3)) * 4 + (c & 3);
-      voff[i] = row * cws + c * 16;
-    }
-  }
-  const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
-  const int k_half = a.k_instr * 16 / a.rows, c_half = (a.instr - a.k_instr) * 16 / a.rows;   // instructions of 16 rows
-  auto issue = [&](int t, int st) __attribute__((always_inline)) {
-    const int j0 = t * a.rows, rows = min(hi + 1 - j0, a.rows);
-    const unsigned kbytes = rows > 0 ? (rows - 1) * kws + heads * DH * ES : 0u, cbytes = rows > 0 ? (rows - 1) * cws + CP : 0u;
-    int64_t p0 = j0, p1 = j0;
-    if (table) {   // 16 rows lie in one page
-      auto find = [&](int j) {
-        int pg = load_uniform(table + __builtin_amdgcn_readfirstlane(j >> a.ps_shift));
-        pg = (unsigned)pg >= (unsigned)a.own.pm.num_pages ? 0 : pg;
-        return ((int64_t)pg << a.ps_shift) + (j & (a.own.pm.page_size - 1));
-      };
-      p0 = find(min(j0, hi & ~15));
-      p1 = a.rows > 16 ? find(min(j0 + 16, hi & ~15)) - 16 : p0;
-    }
-    const u32x4 k0 = uniform_buffer_of(Kb + p0 * kws, kbytes), k1 = uniform_buffer_of(Kb + p1 * kws, kbytes);
-    const u32x4 c0 = uniform_buffer_of(Cb + p0 * cws, cbytes), c1 = uniform_buffer_of(Cb + p1 * cws, cbytes);
-    const unsigned to = lds0 + st * a.stage_bytes;
-#pragma unroll
-    for (int i = 0; i < kMaxInstr; ++i) {
-      const int in = wave + 4 * i;
-      if (in < a.instr) {
-        if (in < a.k_instr) load_to_lds(in < k_half ? k0 : k1, voff[i], to + in * 1024);
-        else load_to_lds(in - a.k_instr < c_half ? c0 : c1, voff[i], to + in * 1024);
-      }
+      for (int i = 0; i < KI; ++i, to += 1024) load_to_lds(r, klane + (kchunk ^ (i * KR & 7)) * 16 + (i * KR * kws + kk * DH * ES), to);
     }
   };
-  const int per_tile = (a.instr - wave + 3) / 4;
+  auto issue_c = [&](int t) __attribute__((always_inline)) {
+    const int rows = rows_of(t);
+    const u32x4 r = uniform_buffer_of(Cb + p0 * cws, rows > 0 ? (rows - 1) * cws + CP : 0u);
+#pragma unroll
+    for (int i = 0; i < CI; ++i) {
+      const int row = CCH <= 64 ? i * CR : i / (CCH / 64), sub = CCH <= 64 ? 0 : i % (CCH / 64);
+      const unsigned swap = ES == 2 ? (row & PM) * 2 : (row >> 2 & 3) * 4;
+      load_to_lds(r, clane + (cchunk ^ swap) * 16 + (row * cws + sub * 1024), clds + i * 1024);
+    }
+  };
 
   f32x4 qf[KS];   // 64 bytes' worth of a step, 16 of them per lane
   {
@@ -157,102 +216,120 @@ __global__ __launch_bounds__(256, NF > 8 ? 1 : 2) void stream_kernel(StreamArgs 
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
   }
-  f32x4 acc[NF];
+  f32x4 acc[NFR];
 #pragma unroll
-  for (int f = 0; f < NF; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int f = 0; f < NFR; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
 
-  for (int s = 0; s < a.stages - 1; ++s) issue(t0 + s, s);   // (steps past the last read zeros)
-  int st = 0, fill = a.stages - 1;
+  int t = t0 + wave;
+  p0 = find(t);
+  issue_k(t);
+  issue_c(t);
 #pragma unroll 1
-  for (int t = t0; t < t1; ++t) {
-    wait_loads((a.stages - 2) * per_tile);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    issue(t + a.stages - 1, fill);
-    fill = fill + 1 == a.stages ? 0 : fill + 1;
-    const char *kt = smem + st * a.stage_bytes, *ct = kt + a.k_instr * 1024;
-    st = st + 1 == a.stages ? 0 : st + 1;
-    const int j0 = t * a.rows;
+  for (; t < t1; t += NWV) {
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CI) : "memory");   // the keys are there
+    f32x4 s{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int kk = 0; kk < heads; ++kk) {
+      const char *kr = kmem + kk * KI * 1024 + x * KCH * 16;
+      f32x4 d{0.f, 0.f, 0.f, 0.f}, kf[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const f32x4 *>(kr + ((ks * 4 + h) ^ (x & 7)) * 16);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        if constexpr (ES == 2) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[ks]), __builtin_bit_cast(bf16x8, qf[ks]), d, 0, 0, 0);
+        else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[ks][e], qf[ks][e], d, 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] = head == kk ? d[e] : s[e];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // and have been read
+    p0 = find(t + NWV);
+    issue_k(t + NWV);
+    const int j0 = t * 16;
+    float p[4], mt = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 4 * h + e;
+      const float v = ruled_score(a.rules, s[e], slope, (float)(n - 1 - j));
+      p[e] = j >= lo && j <= hi ? v : -INFINITY;
+      mt = fmaxf(mt, p[e]);
+    }
+    mt = fmaxf(mt, __shfl_xor(mt, 16));
+    mt = fmaxf(mt, __shfl_xor(mt, 32));
+    const float mn = mt > m + kLazy ? mt : m, ref = mn > -INFINITY ? mn : 0.f;
+    const float corr = __builtin_amdgcn_exp2f(m - ref);
+    if (__builtin_amdgcn_ballot_w64(mn != m) != 0) {
+      l *= corr;
+#pragma unroll
+      for (int f = 0; f < NFR; ++f) acc[f] *= corr;
+    }
+    m = mn;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      if constexpr (ES == 2) p[e] = (float)(__bf16)p[e];
+      l += p[e];
+    }
+    wait_loads(heads * KI);                                      // the latents are there
     if (j0 < lo) {   // clear what is in front of the first row
-      for (int i = tid; i < (lo - j0) * CCH; i += 256) *reinterpret_cast<u32x4 *>(smem + (ct - smem) + i * 16) = u32x4{0u, 0u, 0u, 0u};
-      __syncthreads();
+      for (int i = lane; i < (lo - j0) * CCH; i += 64) *reinterpret_cast<u32x4 *>(mem + (cmem - mem) + i * 16) = u32x4{0u, 0u, 0u, 0u};
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
-#pragma unroll 1
-    for (int r0 = 0; r0 < a.rows; r0 += 16) {
-      f32x4 s{0.f, 0.f, 0.f, 0.f};
-      const char *kr = kt + (r0 + x) * KP;
-#pragma unroll 1
-      for (int kk = 0; kk < heads; ++kk) {
-        f32x4 d{0.f, 0.f, 0.f, 0.f};
+    if constexpr (ES == 2) {
+      bf16x4 p1;
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const f32x4 kf = *reinterpret_cast<const f32x4 *>(kr + ((kk * KCH + ks * 4 + h) ^ (x & 7)) * 16);
-          if constexpr (ES == 2) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[ks]), d, 0, 0, 0);
-          else {
+      for (int e = 0; e < 4; ++e) p1[e] = (__bf16)p[e];
+      const int row = 4 * h + (x >> 2);
+      const char *cr = cmem + row * CP + (x & 1) * 8 + (x >> 1 & 1) * 16;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[e], qf[ks][e], d, 0, 0, 0);
-          }
+      for (int f = 0; f < NFR; ++f) {   // 16 columns are a pair of chunks
+        const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cr + (f ^ (row & PM)) * 32));
+        acc[f] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(c, __builtin_bit_cast(s16x4, p1), acc[f], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int f = 0; f < NFR; ++f)     // and a block of 64 bytes
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float c = *reinterpret_cast<const float *>(cmem + (4 * h + e) * CP + (f ^ h) * 64 + x * 4);
+          acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(c, p[e], acc[f], 0, 0, 0);
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[e] = head == kk ? d[e] : s[e];
-      }
-      float p[4];
-      float mt = -INFINITY;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int j = j0 + r0 + 4 * h + e;
-        const float v = ruled_score(a.rules, s[e], slope, (float)(n - 1 - j));
-        p[e] = j >= lo && j <= hi ? v : -INFINITY;
-        mt = fmaxf(mt, p[e]);
-      }
-      mt = fmaxf(mt, __shfl_xor(mt, 16));
-      mt = fmaxf(mt, __shfl_xor(mt, 32));
-      const float mn = mt > m + kLazy ? mt : m, ref = mn > -INFINITY ? mn : 0.f;
-      const float corr = __builtin_amdgcn_exp2f(m - ref);
-      if (__builtin_amdgcn_ballot_w64(mn != m) != 0) {
-        l *= corr;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) acc[f] *= corr;
-      }
-      m = mn;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
-        if constexpr (ES == 2) p[e] = (float)(__bf16)p[e];
-        l += p[e];
-      }
-      if constexpr (ES == 2) {
-        bf16x4 p1;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) p1[e] = (__bf16)p[e];
-        const int row = r0 + 4 * h + (x >> 2);
-        const char *cr = ct + row * CP + (x & 1) * 8;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-          const int pair = (wave * NF + f) ^ (row & PM);   // 16 columns are a pair of chunks
-          const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cr + (pair * 2 + ((x >> 1) & 1)) * 16));
-          acc[f] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(c, __builtin_bit_cast(s16x4, p1), acc[f], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = r0 + 4 * h + e, blk = (wave * NF + f) ^ ((row >> 2) & 3);   // 16 columns are a block of 64 bytes
-            const float c = *reinterpret_cast<const float *>(ct + row * CP + blk * 64 + x * 4);
-            acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(c, p[e], acc[f], 0, 0, 0);
-          }
-      }
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    issue_c(t + NWV);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land behind the workgroup's end
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (x < gn) {
-    float *to = a.pacc + (at + x) * a.dl + slice * SW + wave * NF * 16 + 4 * h;
+  // join the waves' sums: [map][column] in each one's LDS
+  if (h == 0) stats[wave][x] = make_float2(m, l);
 #pragma unroll
-    for (int f = 0; f < NF; ++f) *reinterpret_cast<f32x4 *>(to + f * 16) = acc[f];
-    if (slice == 0 && wave == 0 && h == 0) a.pml[at + x] = make_float2(m, l);
+  for (int f = 0; f < NFR; ++f) *reinterpret_cast<f32x4 *>(mem + x * (SW * 4) + ((f * 16 + 4 * h) ^ (x & 7) * 4) * 4) = acc[f];
+  __syncthreads();
+  for (int i = tid; i < gn * (SW / 4); i += NWV * 64) {
+    const int map = i / (SW / 4), col = i % (SW / 4) * 4;
+    float mx = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) mx = fmaxf(mx, stats[w][map].x);
+    const float ref = mx > -INFINITY ? mx : 0.f;
+    f32x4 v{0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) {
+      const float2 ml = stats[w][map];
+      if (ml.y == 0.f) continue;
+      const float wt = ml.y != ml.y ? ml.y : __builtin_amdgcn_exp2f(ml.x - ref);
+      const f32x4 c = *reinterpret_cast<const f32x4 *>(smem + w * a.wave_lds + map * (SW * 4) + (col ^ (map & 7) * 4) * 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, c[e], v[e]);
+      sum = fmaf(wt, ml.y, sum);
+    }
+    *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v;
+    if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, sum);
   }
 }
 
@@ -263,18 +340,21 @@ struct JoinArgs {
   void *l_out;
 };
 
-// One (sequence, map): the sums of the prefix's and the sequence's own pieces, weighed by 2^(maximum - the largest).
-constexpr int kMaxPieces = 512;
+// One (sequence, map) and 128 of its columns: the sums of the prefix's and the sequence's own pieces, weighed by 2^(maximum - the
+// largest).  Eight groups of 32 lanes take every eighth piece, four columns a lane, so that most of what is read is asked for at once.
+constexpr int kMaxPieces = 1280;   // 256 of the prefix, 4 workgroups per CU
 template <typename T>
 __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
   __shared__ float weight[kMaxPieces];
   __shared__ float red[8];
-  const int b = blockIdx.x, g = blockIdx.y, tid = threadIdx.x, S = j.r.pieces, all = S + j.s.pieces;
+  __shared__ f32x4 part[8][32];
+  const int b = blockIdx.x, g = blockIdx.y, tid = threadIdx.x, S = j.r.pieces;
+  const int first = j.s.first[b], all = min(S + j.s.first[b + 1] - first, kMaxPieces);
   const int cell = g / j.r.mpc, row = b * j.r.mpc + g % j.r.mpc, tile = row / j.bq;
   auto shared_at = [&](int i) { return ((int64_t)(tile * S + i) * j.r.cells + cell) * j.bq + row % j.bq; };
-  auto own_at = [&](int i) { return ((int64_t)b * j.s.pieces + i) * j.s.nq + g; };
-  float2 ml[kMaxPieces / 256];
+  auto own_at = [&](int i) { return (int64_t)(first + i) * j.s.nq + g; };
   float mx = -INFINITY;
+  float2 ml[kMaxPieces / 256];
 #pragma unroll
   for (int v = 0; v < kMaxPieces / 256; ++v) {
     const int i = v * 256 + tid;
@@ -300,37 +380,42 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
   if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
   __syncthreads();
   sum = (red[4] + red[5]) + (red[6] + red[7]);
-  const int slot = j.s.own.slots ? j.s.own.slots[b] : b;
-  const int own = (int)((int64_t)slot_rows(j.s.prefix, j.s.prefix_slot) + slot_rows(j.s.own, slot) - 1);
-  int lo, hi;
-  seen_by(j.s.rules, b, own, own + 1, lo, hi);
-  const bool sees = lo <= hi;
-  for (int col = tid * 4; col < j.s.dl; col += 1024) {
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
+  const int group = tid >> 5, col = blockIdx.z * 128 + (tid & 31) * 4;
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+  if (col < j.s.dl) {
 #pragma unroll 4
-    for (int i = 0; i < all; ++i) {
+    for (int i = group; i < all; i += 8) {
       const float w = weight[i];
-      if (w == 0.f) continue;
       const float *from = i < S ? j.r.pacc + shared_at(i) * j.s.dl : j.s.pacc + own_at(i - S) * j.s.dl;
-      const f32x4 p = *reinterpret_cast<const f32x4 *>(from + col);
+      if (w != 0.f) {
+        const f32x4 p = *reinterpret_cast<const f32x4 *>(from + col);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(w, p[e], v[e]);
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(w, p[e], v[e]);
+      }
     }
-    T *to = (T *)j.l_out + ((int64_t)b * j.s.nq + g) * j.s.dl + col;
-    const float inv = 1.f / sum;   // (sees something: NaN where all scores are -infinity or one is NaN)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) to[e] = (T)(sees ? v[e] * inv : 0.f);
   }
+  part[group][tid & 31] = v;
+  __syncthreads();
+  if (group || col >= j.s.dl) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) v += part[i][tid];
+  int slot, n, own, lo, hi;
+  own_rows(j.s, b, slot, n, own, lo, hi);
+  seen_by(j.s.rules, b, own, own + 1, lo, hi);
+  T *to = (T *)j.l_out + ((int64_t)b * j.s.nq + g) * j.s.dl + col;
+  const float inv = 1.f / sum;   // (sees something: NaN where all scores are -infinity or one is NaN)
+#pragma unroll
+  for (int e = 0; e < 4; ++e) to[e] = (T)(lo <= hi ? v[e] * inv : 0.f);
 }
 
-// How own rows are cut: which maps and columns a workgroup has, rows of a tile, pieces of a sequence.
-struct StreamPlan { int nf, maps, blocks, heads, rows, stages, pieces, lds; };
+// How own rows are cut: which maps and columns a workgroup has, its waves and their LDS, pieces.
+struct StreamPlan { int nf, maps, blocks, heads, waves, wave_lds, share, each, grid; };
 
 StreamPlan stream_plan(const Dims &d, int batch, int max_seq) {
   const int es = d.esize();
   StreamPlan p{};
   p.maps = std::min(d.qpc, 16);
-  p.nf = d.dl % 1024 == 0 ? 16 : d.dl % 512 == 0 ? 8 : d.dl % 256 == 0 ? 4 : d.dl % 128 == 0 ? 2 : 1;
+  p.nf = d.dl % 512 == 0 ? 8 : d.dl % 256 == 0 ? 4 : d.dl % 128 == 0 ? 2 : 1;
   auto heads_of = [&](int maps) {   // key heads that `maps` maps from a multiple of them on lie in at most
     int most = 1;
     for (int c = 0; c < d.nc; ++c)
@@ -348,13 +433,18 @@ StreamPlan stream_plan(const Dims &d, int batch, int max_seq) {
   }
   p.heads = heads_of(p.maps);
   p.blocks = (d.qpc + p.maps - 1) / p.maps;
-  const int row = row_bytes();
-  p.rows = row <= 2048 ? 32 : 16;
-  const int tile = p.rows * row;
-  p.stages = tile <= 16384 ? 3 : std::max(2, std::min(4, 155648 / tile));
-  p.lds = p.stages * tile;
-  const int64_t per = (int64_t)batch * d.nc * p.blocks * (d.dl / (p.nf * 64));
-  p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(512 + per - 1) / per, (max_seq + 127) / 128, 64}));
+  p.wave_lds = std::max(16 * row_bytes(), 16 * p.nf * 64 * 4);   // a tile; the wave's sums in the end
+  p.waves = p.wave_lds > 50 * 1024 ? 2 : p.wave_lds > 38 * 1024 ? 3 : 4;
+  const int per = d.nc * p.blocks * (d.dl / (p.nf * 64)), at_once = std::min(4, 160 * 1024 / (p.waves * p.wave_lds + 1024));
+  if (batch <= kShared) {
+    p.share = std::max(1, 256 * std::max(at_once, 1) / per);
+    p.grid = 2 * batch > p.share ? 2 * p.share + batch : p.share;
+    const int64_t most = (int64_t)batch * ((max_seq + 15) / 16);   // pieces of a tile each
+    p.grid = (int)std::min<int64_t>(p.grid, most);
+  } else {
+    p.each = (int)std::max<int64_t>(1, std::min<int64_t>((512 + (int64_t)batch * per - 1) / ((int64_t)batch * per), (max_seq + 127) / 128));
+    p.grid = batch * p.each;
+  }
   return p;
 }
 
@@ -372,13 +462,14 @@ PrefixPlan prefix_plan(const Dims &d, int batch, int prefix_max) {
   return p;
 }
 
-struct PrefixWs { float *pacc, *oacc; float2 *pml, *oml; size_t bytes; };
+struct PrefixWs { float *pacc, *oacc; float2 *pml, *oml; int32_t *first; size_t bytes; };
 
 PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const StreamPlan &s, void *base) {
   PrefixWs w{};
   size_t off = 0;
   auto take = [&](size_t n) { void *q = base ? (char *)base + off : nullptr; off += align_up(n); return q; };
-  const size_t prows = (size_t)p.tiles * p.pieces * p.cells * p.bq, orows = (size_t)batch * s.pieces * d.nq;
+  const size_t prows = (size_t)p.tiles * p.pieces * p.cells * p.bq, orows = (size_t)s.grid * d.nq;
+  w.first = (int32_t *)take(((size_t)batch + 1) * 4);
   w.pml = (float2 *)take(prows * 8);
   w.oml = (float2 *)take(orows * 8);
   w.pacc = (float *)take(prows * d.dl * 4);
@@ -388,20 +479,24 @@ PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const Strea
 }
 
 template <typename T, int DH, int NF>
-void launch_stream_of(const StreamArgs &a, int slices, int groups, int lds, hipStream_t st) {
-  allow_dynamic_lds((const void *)stream_kernel<T, DH, NF>, lds);
-  stream_kernel<T, DH, NF><<<dim3((unsigned)a.pieces, (unsigned)(slices * a.blocks * groups), (unsigned)a.batch), 256, lds, st>>>(a);
+void launch_stream_of(const StreamArgs &a, const StreamPlan &p, unsigned y, hipStream_t st) {
+  auto run = [&](auto kernel) {
+    allow_dynamic_lds((const void *)kernel, p.waves * p.wave_lds);
+    kernel<<<dim3((unsigned)p.grid, y), p.waves * 64, p.waves * p.wave_lds, st>>>(a);
+  };
+  if (p.waves == 4) run(stream_kernel<T, DH, NF, 4>);
+  else if (p.waves == 3) run(stream_kernel<T, DH, NF, 3>);
+  else run(stream_kernel<T, DH, NF, 2>);
 }
 
 template <typename T, int DH>
-void launch_stream(const StreamArgs &a, int nf, int groups, int lds, hipStream_t st) {
-  const int slices = a.dl / (nf * 64);
-  switch (nf) {
-    case 1: launch_stream_of<T, DH, 1>(a, slices, groups, lds, st); break;
-    case 2: launch_stream_of<T, DH, 2>(a, slices, groups, lds, st); break;
-    case 4: launch_stream_of<T, DH, 4>(a, slices, groups, lds, st); break;
-    case 8: launch_stream_of<T, DH, 8>(a, slices, groups, lds, st); break;
-    default: launch_stream_of<T, DH, 16>(a, slices, groups, lds, st);
+void launch_stream(const StreamArgs &a, const StreamPlan &p, int groups, hipStream_t st) {
+  const unsigned y = (unsigned)(a.dl / (p.nf * 64) * p.blocks * groups);
+  switch (p.nf) {
+    case 1: launch_stream_of<T, DH, 1>(a, p, y, st); break;
+    case 2: launch_stream_of<T, DH, 2>(a, p, y, st); break;
+    case 4: launch_stream_of<T, DH, 4>(a, p, y, st); break;
+    default: launch_stream_of<T, DH, 8>(a, p, y, st);
   }
 }
 
@@ -438,19 +533,17 @@ int launch_prefix(const Dims &d, const PrefixArgs &x, void *ws, hipStream_t st) 
   else launch_rows_f32(d, r, true, st);
   StreamArgs a{};
   a.q = x.q; a.prefix = x.prefix; a.own = x.own; a.prefix_slot = x.prefix_slot; a.batch = x.batch; a.nq = d.nq; a.qpk = d.qpk; a.qpc = d.qpc;
-  a.dh = d.dh; a.dl = d.dl; a.kw = d.wk_w; a.cw = d.wc_w; a.rules = x.rules; a.maps = s.maps; a.blocks = s.blocks; a.heads = s.heads;
-  a.pieces = s.pieces; a.ps_shift = shift_of(x.own.pm); a.rows = s.rows; a.stages = s.stages;
-  a.k_instr = s.rows * s.heads * d.dh * d.esize() / 1024; a.instr = a.k_instr + s.rows * s.nf * 64 * d.esize() / 1024;
-  a.stage_bytes = a.instr * 1024; a.pacc = w.oacc; a.pml = w.oml;
+  a.dl = d.dl; a.kw = d.wk_w; a.cw = d.wc_w; a.rules = x.rules; a.maps = s.maps; a.blocks = s.blocks; a.heads = s.heads;
+  a.wave_lds = s.wave_lds; a.ps_shift = shift_of(x.own.pm); a.share = s.share; a.each = s.each; a.first = w.first; a.pacc = w.oacc; a.pml = w.oml;
   if (d.dtype == GTA_BF16) {
-    if (d.dh == 64) launch_stream<__bf16, 64>(a, s.nf, d.nc, s.lds, st);
-    else launch_stream<__bf16, 128>(a, s.nf, d.nc, s.lds, st);
+    if (d.dh == 64) launch_stream<__bf16, 64>(a, s, d.nc, st);
+    else launch_stream<__bf16, 128>(a, s, d.nc, st);
   } else {
-    if (d.dh == 64) launch_stream<float, 64>(a, s.nf, d.nc, s.lds, st);
-    else launch_stream<float, 128>(a, s.nf, d.nc, s.lds, st);
+    if (d.dh == 64) launch_stream<float, 64>(a, s, d.nc, st);
+    else launch_stream<float, 128>(a, s, d.nc, st);
   }
   const JoinArgs j{a, r, p.bq, x.l_out};
-  const dim3 grid((unsigned)x.batch, (unsigned)d.nq);
+  const dim3 grid((unsigned)x.batch, (unsigned)d.nq, (unsigned)((d.dl + 127) / 128));
   if (d.dtype == GTA_BF16) prefix_join_kernel<__bf16><<<grid, 256, 0, st>>>(j);
   else prefix_join_kernel<float><<<grid, 256, 0, st>>>(j);
   return check_launch();
