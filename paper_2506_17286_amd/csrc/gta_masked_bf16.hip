@@ -75,9 +75,13 @@ __device__ __forceinline__ float pair_sum(float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 __device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int i = 32; i; i >>= 1) v = min(v, __shfl_xor(v, i));
-  return __builtin_amdgcn_readfirstlane(v);
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x111, 0xf, 0xf, false));   // row_shr 1, 2, 4, 8
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x112, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x114, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x118, 0xf, 0xf, false));
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x142, 0xa, 0xf, false));   // row_bcast 15, 31
+  v = min(v, __builtin_amdgcn_update_dpp(INT_MAX, v, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(v, 63);
 }
 __device__ __forceinline__ int wave_max(int v) { return -wave_min(-v); }
 
@@ -133,8 +137,11 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   const int wr0 = r0 + qw * 32, row = min(wr0 + ln, R - 1);  // (rows past the last repeat it and are not stored)
   const int tok = row / a.mpc, g = cell * a.mpc + (row - tok * a.mpc);
   int lo, hi, own;
-  if constexpr (CACHE) prefix_seen(a, tok, keys, lo, hi, own);
-  else {
+  const bool plain = CACHE && !a.rules.first && !a.rules.last;   // every row sees the whole prefix
+  if constexpr (CACHE) {
+    if (plain && !(MODS & kBias)) { lo = 0; hi = keys - 1; own = 0; }   // (no look at the sequences' lengths)
+    else prefix_seen(a, tok, keys, lo, hi, own);
+  } else {
     own = tok;
     seen_by(a.rules, start + tok, tok, keys, lo, hi);
   }
@@ -142,14 +149,24 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   const bool sees = lo <= hi;   // (a mask of lanes)
   // blocks of 32 keys: those that some row of the wave sees (w0 .. w1), those that all of them see (i0 .. i1)
   const bool idle = wr0 >= R;
-  const int wlo = wave_min(sees && !idle ? lo : INT_MAX), whi = wave_max(sees && !idle ? hi : -1);
-  const int ilo = wave_max(sees ? lo : 0), ihi = wave_min(sees ? hi : INT_MAX);
-  const int w0 = wlo == INT_MAX ? INT_MAX : wlo >> 5, w1 = whi >> 5;   // -1 >> 5 = -1: none
-  if (lane == 0) { span[wave] = w0; span[4 + wave] = w1; }
+  int w0, w1, ilo, ihi, first, last;
   sees_from[tid] = lo;
   sees_to[tid] = hi;
-  __syncthreads();
-  const int first = min(min(span[0], span[1]), min(span[2], span[3])), last = max(max(span[4], span[5]), max(span[6], span[7]));
+  if (plain) {
+    first = 0; last = (keys - 1) >> 5;   // -1 >> 5 = -1: none
+    w0 = idle ? INT_MAX : 0; w1 = idle ? -1 : last;
+    ilo = 0; ihi = keys - 1;
+  } else {
+    const int wlo = wave_min(sees && !idle ? lo : INT_MAX), whi = wave_max(sees && !idle ? hi : -1);
+    ilo = wave_max(sees ? lo : 0);
+    ihi = wave_min(sees ? hi : INT_MAX);
+    w0 = wlo == INT_MAX ? INT_MAX : wlo >> 5;
+    w1 = whi >> 5;
+    if (lane == 0) { span[wave] = w0; span[4 + wave] = w1; }
+    __syncthreads();
+    first = min(min(span[0], span[1]), min(span[2], span[3]));
+    last = max(max(span[4], span[5]), max(span[6], span[7]));
+  }
   const int blocks = __builtin_amdgcn_readfirstlane(last < 0 ? 0 : last - first + 1);
   const int base = __builtin_amdgcn_readfirstlane(last < 0 ? 0 : first);
   const int b0 = base + (int)((int64_t)blocks * piece / pieces), b1 = base + (int)((int64_t)blocks * (piece + 1) / pieces);
@@ -570,15 +587,18 @@ int prefix_tile_rows(const Dims &d, int rows) {
   if (d.dh == 64) return d.dl % 128 == 0 && rows <= 32 ? 32 : 128;
   return rows <= 32 ? 32 : rows <= 64 && d.dl % 256 == 0 ? 64 : 128;
 }
-static int prefix_columns(const Dims &d, int bq) {   // latent columns of a workgroup
+// Latent columns of a workgroup: with 256 two of them share a CU, with 512 the scores are worked out half as often.  One call, 256
+// against 512: 64 sequences of the 1B shape behind 1024 rows 24.8 / 29.1 us, 8192 35.5 / 37.9, 32768 47.6 / 49.5; 32 of the wide shape
+// 28.4 / 30.8, 44.4 / 42.8, 102.9 / 86.6.
+static int prefix_columns(const Dims &d, int bq, int prefix_max) {
   if (d.dh == 64 || bq == 128) return wide_tile(d);
-  return d.dl % 512 == 0 ? 512 : d.dl % 256 == 0 ? 256 : 128;
+  return d.dl % 1024 == 0 && prefix_max > 8192 ? 512 : d.dl % 256 == 0 ? 256 : 128;
 }
-int prefix_slices(const Dims &d, int bq) { return d.dl / prefix_columns(d, bq); }
+int prefix_slices(const Dims &d, int bq, int prefix_max) { return d.dl / prefix_columns(d, bq, prefix_max); }
 
 void launch_prefix_rows(const Dims &d, const RowsArgs &args, int bq, hipStream_t st) {
   RowsArgs a = args;
-  const int w = prefix_columns(d, bq);
+  const int w = prefix_columns(d, bq, a.prefix.max_seq);
   if (bq == 128) { launch_rows<true>(d, a, w, st); return; }
   a.slices = d.dl / w;
   if (d.dh == 64) launch_tile<Tile<64, 128, 1>, true>(a, st);

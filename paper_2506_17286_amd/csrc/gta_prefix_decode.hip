@@ -69,13 +69,15 @@ __device__ __forceinline__ void own_rows(const StreamArgs &a, int b, int &slot, 
   hi -= P;
 }
 
+
 // inclusive sums over the lanes of a wave
 __device__ __forceinline__ int wave_scan(int v) {
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const int up = __shfl_up(v, i);
-    v += (int)(threadIdx.x & 63) >= i ? up : 0;
-  }
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);   // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast 15, 31
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
 
@@ -91,16 +93,16 @@ __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &
     own_rows(a, b, slot, n, own, lo, hi);
     if (lo <= hi) rounds = min(((hi >> 4) - (lo >> 4) + NWV) / NWV, 1 << 24);   // (64 of them fit 32 bits)
   }
-  const int total = __shfl(wave_scan(rounds), 63), some = __popcll(__ballot(rounds > 0));
+  const int total = __builtin_amdgcn_readlane(wave_scan(rounds), 63), some = __popcll(__ballot(rounds > 0));
   int t = max(1, (total + a.share - 1) / a.share);
   if (2 * some > a.share) t = max(1, (total + 2 * a.share - 1) / (2 * a.share));
   else
 #pragma unroll 1
-    while (__shfl(wave_scan((rounds + t - 1) / t), 63) > a.share) t += (t + 7) / 8;
+    while (__builtin_amdgcn_readlane(wave_scan((rounds + t - 1) / t), 63) > a.share) t += (t + 7) / 8;
   mine = (rounds + t - 1) / t;
   const int run = wave_scan(mine);
   before = run - mine;
-  return __shfl(run, 63);
+  return __builtin_amdgcn_readlane(run, 63);
 }
 
 // A workgroup has a piece of one sequence's rows, up to 16 maps of one latent group and SW = NF * 64 of its latent columns.  A wave takes
@@ -457,8 +459,8 @@ PrefixPlan prefix_plan(const Dims &d, int batch, int prefix_max) {
   p.cells = d.nq / p.mpc;
   p.bq = d.dtype == GTA_BF16 ? prefix_tile_rows(d, batch * p.mpc) : 32;
   p.tiles = (int)(((int64_t)batch * p.mpc + p.bq - 1) / p.bq);
-  const int64_t per = (int64_t)p.tiles * p.cells * (d.dtype == GTA_BF16 ? prefix_slices(d, p.bq) : d.dl / rows_f32_columns(d));
-  p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(256 + per - 1) / per, ((int64_t)prefix_max + 255) / 256, 256}));
+  const int64_t per = (int64_t)p.tiles * p.cells * (d.dtype == GTA_BF16 ? prefix_slices(d, p.bq, prefix_max) : d.dl / rows_f32_columns(d));
+  p.pieces = (int)std::max<int64_t>(1, std::min<int64_t>({(256 + per - 1) / per, ((int64_t)prefix_max + 127) / 128, 256}));
   return p;
 }
 

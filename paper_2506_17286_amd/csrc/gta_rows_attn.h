@@ -102,7 +102,7 @@ int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st);
 
 // The prefix's rows: rows of a tile for `rows` query rows of a cell, workgroups that share its latent columns, launch
 int prefix_tile_rows(const Dims &d, int rows);
-int prefix_slices(const Dims &d, int bq);
+int prefix_slices(const Dims &d, int bq, int prefix_max);
 void launch_prefix_rows(const Dims &d, const RowsArgs &a, int bq, hipStream_t st);
 
 // gta_prefix_decode.hip
