@@ -45,9 +45,15 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
   if constexpr (CACHE) {
     b = 0; tile = u / a.pieces; piece = u - tile * a.pieces; pieces = a.pieces; slot = tile * a.pieces;
   } else {
-    if (u >= a.count[0]) return;
-    const Piece e = a.list[u];
-    b = e.b; tile = e.tile; piece = e.piece; pieces = e.pieces; slot = e.slot;
+    if (a.list) {
+      if (u >= a.count[0]) return;
+      const Piece e = a.list[u];
+      b = e.b; tile = e.tile; piece = e.piece; pieces = e.pieces; slot = e.slot;
+    } else {   // every tile of every sequence
+      const int lvl = u / a.batch;
+      b = u - lvl * a.batch; tile = a.tiles / a.batch - 1 - lvl;
+      piece = slot = 0; pieces = 1;
+    }
   }
   const int slice = r_ % a.slices, cell = r_ / a.slices;
   int64_t start = 0;
@@ -58,6 +64,7 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
     if (a.cu) Tb = a.cu[b + 1] - (int)start;
     keys = Tb;
   }
+  if (!CACHE && tile * BQ >= Tb * a.mpc) return;
   const int R = Tb * a.mpc, r0 = tile * BQ, row = min(r0 + ln, R - 1);   // (rows past the last repeat it and are not stored)
   const int tok = row / a.mpc, g = cell * a.mpc + (row - tok * a.mpc);
   int lo, hi, own;

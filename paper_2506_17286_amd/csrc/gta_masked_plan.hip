@@ -24,10 +24,12 @@ struct PlanArgs {
 // Lists a batch's tiles, most keys first, one workgroup.  What a tile sees is estimated from its first and last token, which is
 // exact for intervals whose ends do not fall; the kernel works out its own.  With `most` the tiles of a batch that would leave CUs
 // idle are cut into pieces of about as many blocks of keys as make that many.
-constexpr int kPlanThreads = 1024, kBins = 256, kLeastBlocks = 4;
+constexpr int kPlanThreads = 1024, kBins = 256, kLeastBlocks = 4, kPlanBatch = 2047, kPlanKept = 4;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __shared__ int bins[kBins], sums[kPlanThreads / 64], total_s, slots_s, cuts_s;
   __shared__ unsigned long long cost_s;
+  __shared__ int offsets_s[kPlanBatch + 1];
+  int *offsets = a.batch <= kPlanBatch ? offsets_s : a.offsets;   // the search looks at them again and again
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   for (int i = tid; i < kBins; i += kPlanThreads) bins[i] = 0;
   if (tid == 0) { cost_s = 0; slots_s = 0; cuts_s = 0; }
@@ -41,11 +43,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     __syncthreads();
     int add = before, all = before;
     for (int w = 0; w < kPlanThreads / 64; ++w) { add += w < wave ? sums[w] : 0; all += sums[w]; }
-    if (b < a.batch) a.offsets[b] = add + run - n;
+    if (b < a.batch) offsets[b] = add + run - n;
     before = all;
     __syncthreads();
   }
-  if (tid == 0) a.offsets[a.batch] = before;
+  if (tid == 0) offsets[a.batch] = before;
   __threadfence_block();
   __syncthreads();
   const int tiles = min(before, a.capacity);
@@ -53,11 +55,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     int lo = 0, hi = a.batch;   // offsets[lo] <= t < offsets[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.offsets[mid] <= t) lo = mid;
+      if (offsets[mid] <= t) lo = mid;
       else hi = mid;
     }
     b = lo;
-    tile = t - a.offsets[lo];
+    tile = t - offsets[lo];
     const int64_t start = a.cu ? a.cu[b] : (int64_t)b * a.per_seq;
     const int n = a.cu ? a.cu[b + 1] - (int)start : a.per_seq;
     const int t0 = (int)((int64_t)tile * a.bq / a.mpc), t1 = min((int)(((int64_t)(tile + 1) * a.bq - 1) / a.mpc), n - 1);
@@ -66,30 +68,49 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   };
   const int widest = (a.max_len + 31) / 32;
   auto bin_of = [&](int blocks) { return kBins - 1 - min((int)((int64_t)blocks * (kBins - 1) / max(widest, 1)), kBins - 1); };   // most first
+  // f(tile number, sequence, tile, blocks of keys) for this thread's tiles; the first few are looked up once
+  int kept_b[kPlanKept], kept_tile[kPlanKept], kept_blocks[kPlanKept];
+#pragma unroll
+  for (int i = 0; i < kPlanKept; ++i) {
+    const int t = tid + i * kPlanThreads;
+    if (t < tiles) kept_blocks[i] = look(t, kept_b[i], kept_tile[i]);
+  }
+  auto each_tile = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kPlanKept; ++i)
+      if (tid + i * kPlanThreads < tiles) f(kept_b[i], kept_tile[i], kept_blocks[i]);
+    for (int t = tid + kPlanKept * kPlanThreads; t < tiles; t += kPlanThreads) {
+      int b, tile;
+      const int blocks = look(t, b, tile);
+      f(b, tile, blocks);
+    }
+  };
   int target = INT_MAX;
   if (a.most) {
     unsigned long long mine = 0;
-    for (int t = tid; t < tiles; t += kPlanThreads) { int b, tile; mine += look(t, b, tile); }
+    each_tile([&](int, int, int blocks) { mine += blocks; });
     if (mine) atomicAdd(&cost_s, mine);
     __syncthreads();
     target = max((int)((cost_s * a.per + a.most - 1) / a.most), kLeastBlocks);
   }
   auto pieces_of = [&](int blocks) { return a.most && blocks > target ? (blocks + target - 1) / target : 1; };
-  for (int t = tid; t < tiles; t += kPlanThreads) {
-    int b, tile;
-    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+  each_tile([&](int, int, int blocks) {
+    const int n = pieces_of(blocks);
     atomicAdd(&bins[bin_of(blocks / n)], n);
+  });
+  __syncthreads();
+  if (wave == 0) {   // four bins a lane
+    int v[kBins / 64], sum = 0;
+    for (int i = 0; i < kBins / 64; ++i) { v[i] = bins[lane * (kBins / 64) + i]; sum += v[i]; }
+    int run = sum;
+    for (int i = 1; i < 64; i <<= 1) { const int up = __shfl_up(run, i); run += lane >= i ? up : 0; }
+    if (lane == 63) total_s = run;
+    run -= sum;
+    for (int i = 0; i < kBins / 64; ++i) { bins[lane * (kBins / 64) + i] = run; run += v[i]; }
   }
   __syncthreads();
-  if (tid == 0) {
-    int run = 0;
-    for (int i = 0; i < kBins; ++i) { const int n = bins[i]; bins[i] = run; run += n; }
-    total_s = run;
-  }
-  __syncthreads();
-  for (int t = tid; t < tiles; t += kPlanThreads) {
-    int b, tile;
-    const int blocks = look(t, b, tile), n = pieces_of(blocks);
+  each_tile([&](int b, int tile, int blocks) {
+    const int n = pieces_of(blocks);
     const int slot = n > 1 ? atomicAdd(&slots_s, n) : 0, at = atomicAdd(&bins[bin_of(blocks / n)], n);
     for (int i = 0; i < n; ++i)
       if (at + i < a.capacity) a.list[at + i] = Piece{b, tile, i, n, slot, {}};
@@ -97,7 +118,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
       const int c = atomicAdd(&cuts_s, 1);
       if (c < a.capacity) a.cut[c] = Piece{b, tile, 0, n, slot, {}};
     }
-  }
+  });
   __syncthreads();
   if (tid == 0) { a.count[0] = min(total_s, a.capacity); a.count[1] = min(cuts_s, a.capacity); }
 }
@@ -140,6 +161,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
 }
 
 constexpr int kAtOnce = 256;   // pieces of a batch that is cut
+constexpr int kShort = 256;    // keys
 
 int tile_rows(const Dims &d) { return d.dtype == GTA_BF16 ? 128 : 32; }
 int columns(const Dims &d) { return d.dtype == GTA_BF16 ? masked_bf16_columns(d) : rows_f32_columns(d); }
@@ -200,6 +222,16 @@ int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) 
   a.rules = m.rules;
   a.list = w.list; a.count = w.count; a.tiles = (int)w.capacity; a.pacc = w.pacc; a.pml = w.pml;
   const int bq = tile_rows(d);
+  // Where the chip holds every (tile, sequence) up to the longest at once and no chain of keys is long, tiles need no list and no cut
+  // (60 tokens of the paper's layer with a cap 17.6 -> 11 us).
+  const int64_t levels = ((int64_t)std::min<int64_t>(m.max_len, m.total) * a.mpc + bq - 1) / bq;
+  if (m.max_len <= kShort && levels * m.batch * a.cells * a.slices <= kAtOnce) {
+    a.list = nullptr;
+    a.tiles = (int)(levels * m.batch);
+    if (d.dtype == GTA_BF16) launch_masked_bf16(d, a, st);
+    else launch_rows_f32(d, a, false, st);
+    return check_launch();
+  }
   plan_kernel<<<1, kPlanThreads, 0, st>>>(PlanArgs{m.cu, a.per_seq, m.batch, a.mpc, bq, (int)w.capacity, m.max_len, m.rules.first, m.rules.last,
                                                   a.cells * a.slices, w.most, w.offsets, w.list, w.count, w.cut});
   if (d.dtype == GTA_BF16) launch_masked_bf16(d, a, st);

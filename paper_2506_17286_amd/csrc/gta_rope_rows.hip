@@ -68,16 +68,20 @@ __device__ __forceinline__ void store8(float *p, const f32x8 &v) {
 template <int PAIRS> struct Turns { uint64_t at[PAIRS]; };
 
 // Heads and their turning parts in whole units of 16 elements, rows and rows' starts in whole 16 bytes.  A thread has one unit of
-// HEADS heads of a token: eight pairs, whose sines it works out once, or 16 elements to copy; loads and stores are 16 bytes.  Bound
-// by memory where there are many tokens, by the launch where there are few.
+// HEADS heads of a token: eight pairs, whose sines it works out once, or 16 elements to copy; loads and stores are 16 bytes, those of
+// neighbouring threads next to each other (21 600 tokens of neighbours in pairs 22 us with 32 bytes a thread).  Bound by memory where there are many tokens, by the launch where there are few.
 template <typename T, int PAIRS, int HEADS, bool INTER, bool NT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, Turns<PAIRS> turns) {
   const unsigned heads = a.q.heads + a.k.heads, groups = (heads + HEADS - 1) / HEADS, units = a.dh / 16, per = groups * units;
   const unsigned item = blockIdx.x * 256 + threadIdx.x, row = item / per, rest = item - row * per, grp = rest / units, u = rest - grp * units;
   const int64_t t = row;
   if (t >= a.total) return;
-  const bool turns_here = (int)u * 16 < a.r;
-  const int lo = INTER || !turns_here ? u * 16 : u * 8, hi = INTER || !turns_here ? lo + 8 : lo + a.r / 2;
+  // Two chunks of eight elements: the halves of eight pairs (u, u + r/2), or, of neighbours in pairs and of what is copied, the thread's
+  // own in either half of the head or its rest.  Neighbouring threads have neighbouring chunks in both.
+  const unsigned pair_units = a.r / 16, rest_units = units - pair_units;
+  const bool halves = !INTER && u < pair_units;
+  const int lo = INTER || halves ? u * 8 : a.r + (u - pair_units) * 8, hi = INTER ? lo + a.dh / 2 : halves ? lo + a.r / 2 : lo + rest_units * 8;
+  const bool turn_lo = INTER ? lo < a.r : halves, turn_hi = INTER ? hi < a.r : halves;
   const int p = a.positions ? a.positions[t] : (int)t;
   f32x8 x[HEADS], y[HEADS];
 #pragma unroll
@@ -87,11 +91,12 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, Turns<PAIRS> turn
     x[i] = load8(in + lo);
     y[i] = load8(in + hi);
   }
-  f32x8 cs, sn;
-  if (turns_here) {
+  f32x8 cs, sn;   // halves: of the eight pairs; neighbours: of four pairs of either chunk
+  if (turn_lo || turn_hi) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float2 c = cos_sin(T(), p, turns.at[u * 8 + e]);
+      const int pair = !INTER ? lo + e : min(e < 4 ? lo / 2 + e : hi / 2 + e - 4, PAIRS - 1);   // (not used where the chunk is copied)
+      const float2 c = cos_sin(T(), p, turns.at[pair]);
       cs[e] = c.x * a.magnitude;
       sn[e] = (a.back ? -c.y : c.y) * a.magnitude;
     }
@@ -102,17 +107,17 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, Turns<PAIRS> turn
     if (h >= (int)heads) break;
     T *out = hk < 0 ? (T *)a.q.out + t * a.q.out_stride + h * a.dh : (T *)a.k.out + t * a.k.out_stride + hk * a.dh;
     f32x8 v = x[i], w = y[i];
-    if (turns_here) {
-      if constexpr (INTER) {   // v: pairs 0 .. 3, w: 4 .. 7
-        const f32x8 a0 = __builtin_shufflevector(v, w, 0, 2, 4, 6, 8, 10, 12, 14), b0 = __builtin_shufflevector(v, w, 1, 3, 5, 7, 9, 11, 13, 15);
+    if constexpr (INTER) {
+      const f32x8 a0 = __builtin_shufflevector(v, w, 0, 2, 4, 6, 8, 10, 12, 14), b0 = __builtin_shufflevector(v, w, 1, 3, 5, 7, 9, 11, 13, 15);
+      if (turn_lo || turn_hi) {
         const f32x8 a1 = a0 * cs - b0 * sn, b1 = b0 * cs + a0 * sn;
-        v = __builtin_shufflevector(a1, b1, 0, 8, 1, 9, 2, 10, 3, 11);
-        w = __builtin_shufflevector(a1, b1, 4, 12, 5, 13, 6, 14, 7, 15);
-      } else {
-        const f32x8 a0 = v;
-        v = a0 * cs - w * sn;
-        w = w * cs + a0 * sn;
+        if (turn_lo) v = __builtin_shufflevector(a1, b1, 0, 8, 1, 9, 2, 10, 3, 11);
+        if (turn_hi) w = __builtin_shufflevector(a1, b1, 4, 12, 5, 13, 6, 14, 7, 15);
       }
+    } else if (halves) {
+      const f32x8 a0 = v;
+      v = a0 * cs - w * sn;
+      w = w * cs + a0 * sn;
     }
     store8<NT>(out + lo, v);
     store8<NT>(out + hi, w);
