@@ -48,7 +48,9 @@ struct Tile {
   static constexpr int K_BYTES = K_INSTR * K_PITCH, STAGE = K_BYTES + C_INSTR * C_PITCH, NSTAGE = 3;
   static constexpr int OUT_PITCH = DLW * 2 + 16;
   static constexpr int SMEM = NSTAGE * STAGE > BQ * OUT_PITCH ? NSTAGE * STAGE : BQ * OUT_PITCH;
-  static constexpr int BLOCKS = SMEM > 80 * 1024 ? 1 : DH == 64 && SMEM <= 53 * 1024 ? 3 : 2;   // workgroups of a CU
+  // Workgroups of a CU, as the registers are shared out.  (Tiles of 512 columns fill a CU's LDS, but with 512 registers a lane the
+  // accumulators go to the half that takes no arithmetic, and are copied out and back every step.)
+  static constexpr int BLOCKS = DH == 64 && SMEM <= 53 * 1024 ? 3 : 2;
   static_assert(K_INSTR >= NW && C_INSTR >= NW && C_RPI >= 1 && NDLB >= 1 && SMEM <= 160 * 1024, "tile");
   __device__ static constexpr int k_sel(int i) { return K_CPR == 16 ? i & 1 : (i ^ (i >> 1)) & 1; }
   __device__ static constexpr int c_row(int a) { return a / C_RPI * C_GROUP + a % C_RPI * C_ROW; }
