@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
 }
 
 constexpr int kAtOnce = 256;   // pieces of a batch that is cut
-constexpr int kShort = 256;    // keys
+constexpr int kShort = 1536;   // keys
 
 int tile_rows(const Dims &d) { return d.dtype == GTA_BF16 ? 128 : 32; }
 int columns(const Dims &d) { return d.dtype == GTA_BF16 ? masked_bf16_columns(d) : rows_f32_columns(d); }
@@ -222,10 +222,11 @@ int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) 
   a.rules = m.rules;
   a.list = w.list; a.count = w.count; a.tiles = (int)w.capacity; a.pacc = w.pacc; a.pml = w.pml;
   const int bq = tile_rows(d);
-  // Where the chip holds every (tile, sequence) up to the longest at once and no chain of keys is long, tiles need no list and no cut
-  // (60 tokens of the paper's layer with a cap 17.6 -> 11 us).
+  // Where the chip holds every (tile, sequence) up to the longest at once and no chain of keys is long, tiles need no list and no cut.
+  // With and without: one prompt of the paper's layer of 128 tokens 15.8 / 9.2 us, 500 24.6 / 15.5, 1000 35.8 / 24.3, 2000 45.1 / 41.4; of the
+  // 1B shape 19.4 / 12.2, 30.7 / 20.5, 44.2 / 31.6, 51.1 / 53.5; fp32 paper's layer 19.0 / 11.9, 28.7 / 23.4, 46.9 / 38.3, 83.5 / 82.7.
   const int64_t levels = ((int64_t)std::min<int64_t>(m.max_len, m.total) * a.mpc + bq - 1) / bq;
-  if (m.max_len <= kShort && levels * m.batch * a.cells * a.slices <= kAtOnce) {
+  if (m.max_len <= kShort && levels * m.batch * a.cells * a.slices <= 2 * kAtOnce) {
     a.list = nullptr;
     a.tiles = (int)(levels * m.batch);
     if (d.dtype == GTA_BF16) launch_masked_bf16(d, a, st);
