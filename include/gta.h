@@ -190,7 +190,7 @@ typedef struct {
  * is less, last as the last key there is where it is more.  One that sees none gets a row of zeros.  What is not seen is not read
  * into the result, NaN and infinities included. */
 typedef struct {
-  float          cap;     /* 0 = off; finite and not negative */
+  float          cap;     /* 0 = off; 1e-30 .. 1e30 otherwise */
   const float   *slopes;  /* [n_q] fp32, finite, or NULL */
   const int32_t *first;   /* per token, or NULL: 0 */
   const int32_t *last;    /* per token, or NULL: the token's own position */
@@ -408,9 +408,10 @@ GTA_API int gta_prefill_attention(const gta_config *cfg, const void *q, const vo
  *   cu_seqlens, batch, total_tokens, max_seqlen  as for gta_prefill.  Rows of l_out behind the last sequence are left as they are
  *   l_out    device [total_tokens, n_q*d_l], dense, 16-byte aligned; must not overlap the inputs
  *   workspace  mode PREFILL_MASKED
- * Sums and softmax statistics are fp32.  head_dim up to 1024, latent_dim up to 4096 (GTA_ERR_UNSUPPORTED).  Runs on the matrix
- * instructions where gta_uses_tuned_kernels(cfg, GTA_MODE_PREFILL_MASKED) is 1, rows consist of 16-byte aligned chunks and a
- * sequence's key / latent rows stay below 2 GiB, on a general kernel otherwise. */
+ * Sums and softmax statistics are fp32; bf16 weights are rounded before the product with the latents, and so is their sum.  head_dim
+ * up to 1024, latent_dim up to 4096, up to 65535 maps (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where
+ * gta_uses_tuned_kernels(cfg, GTA_MODE_PREFILL_MASKED) is 1, rows consist of 16-byte aligned chunks and lie less than 64 MiB apart, on a
+ * general kernel, 10 to 200 times slower, otherwise.  The first call with a cap, and with slopes, is one of a new shape to stream capture. */
 GTA_API int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                                          const void *c, int64_t c_stride, const int32_t *cu_seqlens, int32_t batch,
                                          int64_t total_tokens, int32_t max_seqlen, const gta_score_rules *rules, void *l_out,
@@ -427,9 +428,10 @@ GTA_API int gta_prefill_masked_attention(const gta_config *cfg, const void *q, i
  *   rules      first, last [batch], over positions 0 .. P+n-1 (first = P: without the prefix)
  *   workspace  mode PREFIX_DECODE
  * A sequence that sees no row gets zeros.  l_out goes on into gta_prefill_decoder.  head_dim up to 1024, latent_dim up to 4096,
- * max_seq of each cache up to 2^30 (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where
- * gta_uses_tuned_kernels(cfg, GTA_MODE_PREFIX_DECODE) is 1 and pages, if any, are of a power of two of at least 16 rows, on a
- * general kernel otherwise. */
+ * up to 65535 maps, max_seq of each cache up to 2^30 (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where
+ * gta_uses_tuned_kernels(cfg, GTA_MODE_PREFIX_DECODE) is 1, there are at most 512 maps and pages, if any, are of a power of two of at
+ * least 16 rows, on a general kernel, which reads the prefix once for every sequence and map, otherwise.  Arithmetic and capture as in
+ * gta_prefill_masked_attention. */
 GTA_API int gta_prefix_decode_attention(const gta_config *cfg, const void *q, const gta_cache *prefix, int32_t prefix_slot,
                                         const gta_cache *cache, const int32_t *slots, int32_t batch, const gta_score_rules *rules,
                                         void *l_out, void *workspace, size_t workspace_bytes, void *hip_stream);
@@ -484,6 +486,8 @@ GTA_API const char *gta_strerror(int code);
  * allows (widths in units of 64, heads of at most 64; attention: heads of 32, 64 or 128, latents in units
  * of 64; decode: one key of 64 and one latent of 128 for at most 16 maps, rope_base at least 1).  With
  * GTA_DEBUG set in the environment a bf16 call that takes the generic kernels says so on stderr.
+ * GTA_MODE_PREFILL_MASKED, GTA_MODE_PREFIX_DECODE: bf16 heads of 128 with latents in units of 128 or of 64 with units of 64; fp32 heads of
+ * 64 or 128 (masked: 32, too) with latents in units of 64.
  * GTA_MODE_MX_DECODE (either dtype): heads of up to 512; GTA_ERR_UNSUPPORTED where the widths are refused.  Rows are
  * read once with at most 16 maps, heads a multiple of 64, and key rows of 64 or 128 elements with latent rows of
  * 128, 256 or 512, of 256 with 256, 512 or 1024, of 512 with 512 or 1024, of 1024 with 1024; others run in blocks

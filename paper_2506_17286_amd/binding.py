@@ -205,17 +205,23 @@ def make_weights(w: Dict[str, "object"]) -> gta_weights:
     return gta_weights(_ptr(w["wq"]), _ptr(w["wk"]), _ptr(w["wc"]), _ptr(w["wg"]), _ptr(w["wp"]), _ptr(w.get("wo")))
 
 
+def _known(cache: gta_cache, k, c) -> gta_cache:
+    """Notes what the arrays are, for the calls that look at it."""
+    cache.device, cache.dtype, cache.widths = k.get_device(), k.dtype, tuple(t.shape[2:].numel() for t in (k, c))
+    return cache
+
+
 def make_cache(k, c, seq_lens, status) -> gta_cache:
     """k [slots, max_seq, n_k*d_h], c [slots, max_seq, n_c*d_l], seq_lens/status int32 [slots] (device)."""
-    return gta_cache(_ptr(k), _ptr(c), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1])
+    return _known(gta_cache(_ptr(k), _ptr(c), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1]), k, c)
 
 
 def make_paged_cache(k_pool, c_pool, seq_lens, status, block_table) -> gta_cache:
     """k_pool [num_pages, page_size, n_k*d_h], c_pool [num_pages, page_size, n_c*d_l], block_table int32
     [slots, pages_per_slot] (device): row p of slot s is row p % page_size of page block_table[s, p // page_size]."""
     slots, pps = block_table.shape
-    return gta_cache(_ptr(k_pool), _ptr(c_pool), _ptr(seq_lens), _ptr(status), slots, pps * k_pool.shape[1],
-                     _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0])
+    return _known(gta_cache(_ptr(k_pool), _ptr(c_pool), _ptr(seq_lens), _ptr(status), slots, pps * k_pool.shape[1],
+                            _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0]), k_pool, c_pool)
 
 
 def _mx_cache(k, c, k_scale, c_scale, seq_lens, status, slots: int, max_seq: int, table=None) -> gta_mx_cache:
@@ -314,6 +320,21 @@ def _rules(device: int, cfg: gta_config, rules: Optional[gta_score_rules], token
             raise ValueError(f"{name} has {t.numel()} entries for {need}")
         _on(device, t)
     return ctypes.byref(rules)
+
+
+def _rows_of(device: int, cfg: gta_config, cache: Optional[gta_cache]):
+    """The cache as the library takes it, if it is on the current device and has the widths and the type of cfg (one whose fields the
+    caller filled in is taken as it is)."""
+    if cache is None:
+        return None
+    if getattr(cache, "device", device) != device:
+        raise ValueError(f"cache on {'cpu' if cache.device < 0 else f'cuda:{cache.device}'}, current device is cuda:{device}")
+    widths = (cfg.n_kgroups * cfg.head_dim, cfg.n_cgroups * cfg.latent_dim)
+    if getattr(cache, "widths", widths) != widths:
+        raise ValueError(f"cache of rows of {cache.widths}, config of {widths}")
+    if hasattr(cache, "dtype") and str(cache.dtype) != ("torch.float32" if cfg.dtype == GTA_F32 else "torch.bfloat16"):
+        raise ValueError(f"cache of {cache.dtype}")
+    return ctypes.byref(cache)
 
 
 def _check(rc: int, where: str) -> None:
@@ -516,8 +537,8 @@ def gta_prefill_masked_attention(cfg: gta_config, q, q_stride: int, k, k_stride:
 def gta_prefix_decode_attention(cfg: gta_config, q, prefix: gta_cache, prefix_slot: int, cache: gta_cache, slots, batch: int,
                                 rules: Optional[gta_score_rules], l_out, workspace, stream=None, check: bool = True) -> int:
     d = _device()
-    rc = load().gta_prefix_decode_attention(ctypes.byref(cfg), _on(d, q), ctypes.byref(prefix) if prefix is not None else None,
-                                            prefix_slot, ctypes.byref(cache) if cache is not None else None, _on(d, slots), batch,
+    rc = load().gta_prefix_decode_attention(ctypes.byref(cfg), _on(d, q), _rows_of(d, cfg, prefix), prefix_slot,
+                                            _rows_of(d, cfg, cache), _on(d, slots), batch,
                                             _rules(d, cfg, rules, batch), _on(d, l_out), _on(d, workspace),
                                             0 if workspace is None else workspace.numel() * workspace.element_size(),
                                             _stream(stream))

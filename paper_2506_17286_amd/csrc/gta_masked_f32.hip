@@ -261,8 +261,10 @@ void launch_of(const RowsArgs &a, bool cache, hipStream_t st) {
   constexpr int LDS = 4 * 32 * (DLW + 4) * 4;
   const unsigned grid = (unsigned)((int64_t)a.tiles * a.cells * a.slices);
   if (cache) {
+    if constexpr (DH >= 64) {   // (what prefix_tuned lets through)
     allow_dynamic_lds((const void *)rows_attn_f32_kernel<DH, DLW, true>, LDS);
     rows_attn_f32_kernel<DH, DLW, true><<<grid, 256, LDS, st>>>(a);
+    }
   } else {
     allow_dynamic_lds((const void *)rows_attn_f32_kernel<DH, DLW, false>, LDS);
     rows_attn_f32_kernel<DH, DLW, false><<<grid, 256, LDS, st>>>(a);

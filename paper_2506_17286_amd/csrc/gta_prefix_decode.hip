@@ -411,6 +411,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
 }
 
 // How own rows are cut: which maps and columns a workgroup has, its waves and their LDS, pieces.
+constexpr int kFour = 38 * 1024, kThree = 50 * 1024;   // LDS of a wave that four, three of a workgroup have room for
 struct StreamPlan { int nf, maps, blocks, heads, waves, wave_lds, share, each, grid; };
 
 StreamPlan stream_plan(const Dims &d, int batch, int max_seq) {
@@ -436,7 +437,7 @@ StreamPlan stream_plan(const Dims &d, int batch, int max_seq) {
   p.heads = heads_of(p.maps);
   p.blocks = (d.qpc + p.maps - 1) / p.maps;
   p.wave_lds = std::max(16 * row_bytes(), 16 * p.nf * 64 * 4);   // a tile; the wave's sums in the end
-  p.waves = p.wave_lds > 50 * 1024 ? 2 : p.wave_lds > 38 * 1024 ? 3 : 4;
+  p.waves = p.wave_lds > kThree ? 2 : p.wave_lds > kFour ? 3 : 4;
   const int per = d.nc * p.blocks * (d.dl / (p.nf * 64)), at_once = std::min(4, 160 * 1024 / (p.waves * p.wave_lds + 1024));
   if (batch <= kShared) {
     p.share = std::max(1, 256 * std::max(at_once, 1) / per);
@@ -486,16 +487,26 @@ void launch_stream_of(const StreamArgs &a, const StreamPlan &p, unsigned y, hipS
     allow_dynamic_lds((const void *)kernel, p.waves * p.wave_lds);
     kernel<<<dim3((unsigned)p.grid, y), p.waves * 64, p.waves * p.wave_lds, st>>>(a);
   };
-  if (p.waves == 4) run(stream_kernel<T, DH, NF, 4>);
-  else if (p.waves == 3) run(stream_kernel<T, DH, NF, 3>);
-  else run(stream_kernel<T, DH, NF, 2>);
+  // what stream_plan comes to: one key head leaves room for four waves but in fp32 rows of 128 + 512, sixteen may take it
+  constexpr int LEAST = 16 * (DH + NF * 64) * (int)sizeof(T), MOST = std::min(16 * (16 * DH + NF * 64) * (int)sizeof(T), 65536);
+  if constexpr (LEAST <= kFour) {
+    if (p.waves == 4) run(stream_kernel<T, DH, NF, 4>);
+  }
+  if constexpr (MOST > kFour) {
+    if (p.waves == 3) run(stream_kernel<T, DH, NF, 3>);
+  }
+  if constexpr (MOST > kThree) {
+    if (p.waves == 2) run(stream_kernel<T, DH, NF, 2>);
+  }
 }
 
 template <typename T, int DH>
 void launch_stream(const StreamArgs &a, const StreamPlan &p, int groups, hipStream_t st) {
   const unsigned y = (unsigned)(a.dl / (p.nf * 64) * p.blocks * groups);
   switch (p.nf) {
-    case 1: launch_stream_of<T, DH, 1>(a, p, y, st); break;
+    case 1:
+      if constexpr (DH == 64 || sizeof(T) == 4) launch_stream_of<T, DH, 1>(a, p, y, st);   // bf16 heads of 128 have latents in units of 128
+      break;
     case 2: launch_stream_of<T, DH, 2>(a, p, y, st); break;
     case 4: launch_stream_of<T, DH, 4>(a, p, y, st); break;
     default: launch_stream_of<T, DH, 8>(a, p, y, st);

@@ -23,12 +23,18 @@ SHAPES = {
     "paper": shape(5, 1, 1, 64, 128), "paper768": shape(3, 1, 1, 64, 128), "1b": shape(4, 4, 1, 128, 512), "wide": shape(8, 8, 1, 128, 1024),
     "c2": shape(6, 1, 2, 64, 128), "q8k4c2": shape(8, 4, 2, 128, 512), "q6k2c3": shape(6, 2, 3, 64, 64), "l256": shape(4, 2, 1, 128, 256),
     "l128": shape(2, 1, 2, 128, 128), "l192": shape(3, 3, 1, 64, 192), "maps20": shape(20, 1, 1, 64, 128), "maps40": shape(40, 4, 1, 64, 128),
-    "h32": shape(4, 2, 1, 32, 64), "odd": shape(6, 3, 2, 20, 44), "h96": shape(2, 1, 1, 96, 160), "mha": shape(4, 4, 4, 64, 64),
+    "h32": shape(4, 2, 1, 32, 64), "h32l128": shape(4, 4, 1, 32, 128), "h128l192": shape(2, 2, 1, 128, 192), "odd": shape(6, 3, 2, 20, 44), "h96": shape(2, 1, 1, 96, 160), "mha": shape(4, 4, 4, 64, 64),
 }
+
+# layers whose own rows take kernels that none of those takes
+ROWS = {f"k{nk}x{dh}l{dl}": shape(nk, nk, 1, dh, dl) for nk, dh, dl in (
+    (16, 64, 256), (12, 64, 512), (12, 128, 128), (9, 128, 128), (11, 128, 256), (8, 128, 256), (9, 128, 512), (6, 128, 512), (12, 64, 64), (9, 64, 64),
+    (11, 64, 128), (8, 64, 128), (9, 64, 256), (6, 64, 256), (1, 64, 256), (5, 64, 512), (2, 64, 512), (1, 64, 512), (6, 128, 128), (4, 128, 128),
+    (1, 128, 128), (5, 128, 256), (3, 128, 256), (1, 128, 256), (3, 128, 512), (1, 128, 512), (5, 128, 192), (6, 128, 192))}
 
 
 def config(name, dtype, **kw):
-    return B.make_config(dtype=dtype, **SHAPES[name], **kw)
+    return B.make_config(dtype=dtype, **SHAPES.get(name, ROWS.get(name)), **kw)
 
 
 # ------------------------------------------------------------------------------------------ rotation

@@ -13,6 +13,8 @@ pytestmark = pytest.mark.gpu
 def intervals(kind, n, rng):
     """First and last key of every token of a sequence of n."""
     lo, hi = [0] * n, list(range(n))
+    if n == 0:
+        return lo, hi
     if kind == "documents":
         at = 0
         while at < n:
@@ -175,6 +177,23 @@ def test_what_is_not_seen_does_not_leak(name, dtype, value):
             c[130, ::2] = value
     for kind in ("causal", "documents", "window", "any", "holes"):
         run(name, dtype, [160, 30], kind, edit=edit, seed=16, what=str(value))
+        # with a bound of more keys tiles are listed and their keys shared out
+        run(name, dtype, [160, 30], kind, edit=edit, seed=16, what=str(value), longest=5000, cap=20.0, bias=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("name", ["paper", "1b", "c2", "q6k2c3", "l192"])
+def test_masks_of_listed_and_cut_tiles(name, kind, dtype):
+    run(name, dtype, LENS, kind, seed=23, longest=2000, bias=True)
+    run(name, dtype, [1, 700, 0, 400], kind, seed=24, longest=3000)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_tiles_than_the_list_keeps(dtype):
+    """More than four tiles a thread of the list's workgroup, and more sequences than its LDS has room for."""
+    rng = random.Random(3)
+    run("paper768", dtype, [rng.choice([0, 1, 2, 3]) for _ in range(4500)], "any", seed=25, longest=2000)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -14,7 +14,7 @@ class Cache:
     """Slots of random rows, contiguous or in shuffled pages; rows behind a slot's length hold `fill`."""
 
     def __init__(self, name, dtype, lens, room, gen, page=0, fill=float("nan"), seed=0, lens_tensor=None):
-        sh = R.SHAPES[name]
+        sh = R.SHAPES.get(name, R.ROWS.get(name))
         self.lens, self.room = lens, room
         self.k, self.c = (torch.full((len(lens), room, w), fill, dtype=R.DT[dtype], device="cuda")
                           for w in (sh["n_kgroups"] * sh["head_dim"], sh["n_cgroups"] * sh["latent_dim"]))
@@ -57,7 +57,7 @@ def reference(cfg, q, prefix, prefix_slot, own, slots, rules):
 
 def run(name, dtype, prefix_len, lens, *, page=0, prefix_page=None, cap=0.0, bias=False, first=None, last=None, slots=None, seed=0,
         prefix_room=None, room=None, prefix_slot=0, edit=None, scale=2.0, batch=None):
-    cfg, sh, dt = R.config(name, dtype), R.SHAPES[name], R.DT[dtype]
+    cfg, sh, dt = R.config(name, dtype), R.SHAPES.get(name, R.ROWS.get(name)), R.DT[dtype]
     gen = R.generator(seed)
     unit = max(page, 64)
     prefix_page = page if prefix_page is None else prefix_page
@@ -87,6 +87,13 @@ def run(name, dtype, prefix_len, lens, *, page=0, prefix_page=None, cap=0.0, bia
 def test_layers(name, dtype):
     run(name, dtype, 150, [1, 70, 0, 33], seed=1)
     run(name, dtype, 333, [5, 200], cap=10.0, bias=True, page=16, seed=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", sorted(R.ROWS))
+def test_layers_of_other_kernels(name, dtype):
+    run(name, dtype, 40, [1, 75, 0, 200], seed=20, cap=8.0)
+    run(name, dtype, 9300, [30, 130] * 10, bias=True, page=16, seed=21, first=[0, 9280] * 10)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -182,6 +189,12 @@ def test_long_contexts(name, dtype):
     run(name, dtype, 9000, [20, 700, 3000], seed=14, cap=30.0)
     run(name, dtype, 3, [5000, 1, 2500, 0], seed=15, page=64)
     run(name, dtype, 5000, [1], seed=16, bias=True)
+
+
+@pytest.mark.parametrize("cap,bias", [(0.0, False), (6.0, False), (0.0, True), (6.0, True)])
+@pytest.mark.parametrize("name,batch", [("wide", 40), ("wide", 3), ("1b", 40), ("1b", 100), ("paper", 40)])
+def test_many_readers_of_a_long_prefix(name, batch, cap, bias):
+    run(name, "bf16", 8500, [(7 * i) % 50 for i in range(batch)], seed=30, cap=cap, bias=bias, page=32)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

@@ -124,7 +124,7 @@ def _prefix(cfg, q=FAKE, prefix=None, slot=0, cache=None, batch=1, rules=None, o
 @pytest.mark.parametrize("call", [_masked, _prefix])
 def test_rules_of_either_attention(call):
     cfg = _cfg()
-    for cap in (-1.0, math.nan, math.inf):
+    for cap in (-1.0, math.nan, math.inf, 1e-31, 1e-40, 2e30):
         assert call(cfg, rules=B.gta_score_rules(cap)) == B.GTA_ERR_SHAPE
     for field in ("slopes", "first", "last"):
         rules = B.gta_score_rules(0.0)
@@ -202,3 +202,28 @@ def test_workspaces(mode):
     assert B.gta_workspace_bytes(cfg, mode, 1, 1, -1) == 0
     assert B.gta_workspace_bytes(_cfg(latent_dim=4100), mode, 1, 1, 1) == 0
     assert B.gta_uses_tuned_kernels(_cfg(latent_dim=4100), mode) == B.GTA_ERR_UNSUPPORTED
+
+
+def test_binding_looks_at_tensors():
+    import torch
+    cfg = _cfg()
+    with pytest.raises(ValueError):
+        B.make_score_rules(slopes=torch.zeros(4, dtype=torch.float64))
+    with pytest.raises(ValueError):
+        B.make_score_rules(first=torch.zeros(4, dtype=torch.int64))
+    with pytest.raises(ValueError):
+        B.make_score_rules(last=torch.zeros(8, dtype=torch.int32)[::2])
+    rules = B.make_score_rules(first=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        B._rules(-1, cfg, rules, 4)                     # fewer than there are tokens
+    with pytest.raises(ValueError):
+        B._rules(0, cfg, rules, 3)                      # on the host
+    k, c = torch.zeros(2, 64, 256, dtype=torch.bfloat16), torch.zeros(2, 64, 128, dtype=torch.bfloat16)
+    n = torch.zeros(2, dtype=torch.int32)
+    cache = B.make_cache(k, c, n, n)
+    assert B._rows_of(-1, cfg, cache) is not None
+    for bad, kw in ((cache, dict(latent_dim=256)), (B.make_cache(k.float(), c.float(), n, n), {}), (B.make_cache(k, c[..., :64], n, n), {})):
+        with pytest.raises(ValueError):
+            B._rows_of(-1, _cfg(**kw), bad)
+    with pytest.raises(ValueError):
+        B._rows_of(0, cfg, cache)                       # on the host
