@@ -179,10 +179,11 @@ def _ptr(t) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
     if stream is None:
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None   # 0.5 us; a Stream object takes 3
+        device = torch.cuda.current_device() if device is None else device
+        return torch._C._cuda_getCurrentRawStream(device) or None   # 0.5 us; a Stream object takes 3
     h = stream if isinstance(stream, int) else stream.cuda_stream
     return h or None
 
@@ -514,7 +515,7 @@ def gta_qk_rope(cfg: gta_config, rotation: gta_rotation, q, q_stride: int, k, k_
                 transposed: bool, q_out, q_out_stride: int, k_out, k_out_stride: int, stream=None, check: bool = True) -> int:
     d = _device()
     rc = load().gta_qk_rope(ctypes.byref(cfg), ctypes.byref(rotation), _on(d, q), q_stride, _on(d, k), k_stride, _on(d, positions),
-                            total_tokens, int(transposed), _on(d, q_out), q_out_stride, _on(d, k_out), k_out_stride, _stream(stream))
+                            total_tokens, int(transposed), _on(d, q_out), q_out_stride, _on(d, k_out), k_out_stride, _stream(stream, d))
     if check:
         _check(rc, "gta_qk_rope")
     return rc
@@ -528,7 +529,7 @@ def gta_prefill_masked_attention(cfg: gta_config, q, q_stride: int, k, k_stride:
                                              _on(d, cu_seqlens), batch, total_tokens, max_seqlen, _rules(d, cfg, rules, total_tokens),
                                              _on(d, l_out), _on(d, workspace),
                                              0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                             _stream(stream))
+                                             _stream(stream, d))
     if check:
         _check(rc, "gta_prefill_masked_attention")
     return rc
@@ -541,7 +542,7 @@ def gta_prefix_decode_attention(cfg: gta_config, q, prefix: gta_cache, prefix_sl
                                             _rows_of(d, cfg, cache), _on(d, slots), batch,
                                             _rules(d, cfg, rules, batch), _on(d, l_out), _on(d, workspace),
                                             0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                            _stream(stream))
+                                            _stream(stream, d))
     if check:
         _check(rc, "gta_prefix_decode_attention")
     return rc

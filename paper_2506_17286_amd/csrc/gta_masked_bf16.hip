@@ -10,6 +10,10 @@
 // out between the matrix instructions, without looking at their maximum: weights refer to the maximum a row has, whatever their size,
 // and a row sum beyond 2^32 sends the wave through the full step.
 // Weights are rounded to bf16 for the second product (their sum is that of the rounded ones); everything else is fp32.
+// Bound by the softmax's vector arithmetic beside the matrix instructions, which then draw the more power the less they wait: 4 x 4096
+// tokens of documents of 100 to 2000, 1B shape, 82 us (540 TFLOP/s of what is seen; whole sequences, causal, 776); 32 ragged prompts of the
+// paper's layer, a cap, 96 us (620); 2 x 8192 of the wide shape, window, cap and bias 1275 us (690; with the scores, which each of four latent
+// tiles works out, 920).  A cap costs 21 to 28 %, a bias 4 to 11.
 //
 // A masked weight is 0, but 0 times a latent that is not finite is NaN: a wave whose sums are not finite in the end goes through
 // its rows once more, one by one, over the keys that each sees (wave_row).
@@ -584,7 +588,9 @@ bool rows_bf16_ok(const Dims &d) {
   return d.dtype == GTA_BF16 && ((d.dh == 128 && d.dl % 128 == 0) || (d.dh == 64 && d.dl % 64 == 0));
 }
 
-// A batch of few rows takes tiles of 64 or 32, whose waves share the columns.
+// A batch of few rows takes tiles of 64 or 32, whose waves share the columns: scratch memory for as many rows, and less to load where
+// a wave would have none.  One call, behind 8192 rows, with and without: 8 sequences of the 1B shape 25.5 / 26.2 us, 32 29.3 / 29.5, 64 35.8 / 35.2,
+// 32 of the wide shape 46.2 / 48.0, 64 53.8 / 53.6, 6 of the paper's layer 20.2 / 20.2.
 int prefix_tile_rows(const Dims &d, int rows) {
   if (d.dh == 64) return d.dl % 128 == 0 && rows <= 32 ? 32 : 128;
   return rows <= 32 ? 32 : rows <= 64 && d.dl % 256 == 0 ? 64 : 128;

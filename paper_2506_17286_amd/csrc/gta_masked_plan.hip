@@ -23,7 +23,8 @@ struct PlanArgs {
 
 // Lists a batch's tiles, most keys first, one workgroup.  What a tile sees is estimated from its first and last token, which is
 // exact for intervals whose ends do not fall; the kernel works out its own.  With `most` the tiles of a batch that would leave CUs
-// idle are cut into pieces of about as many blocks of keys as make that many.
+// idle are cut into pieces of about as many blocks of keys as make that many.  Bound by its chain of loads, scans and LDS atomics: 5.5 us
+// for 4 sequences of 4096 tokens, 9 for 32 ragged ones.
 constexpr int kPlanThreads = 1024, kBins = 256, kLeastBlocks = 4, kPlanBatch = 2047, kPlanKept = 4;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __shared__ int bins[kBins], sums[kPlanThreads / 64], total_s, slots_s, cuts_s;
@@ -160,7 +161,9 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
   }
 }
 
-constexpr int kAtOnce = 256;   // pieces of a batch that is cut
+// Pieces of a batch that is cut.  Not cut / 256 / 512: 2048 tokens of the paper's layer 46 / 43 / 52 us, 4096 80 / 59 / 63; two prompts of 3000 of the
+// 1B shape, which are 384 workgroups, not cut 91, cut for 512 110.
+constexpr int kAtOnce = 256;
 constexpr int kShort = 1536;   // keys
 
 int tile_rows(const Dims &d) { return d.dtype == GTA_BF16 ? 128 : 32; }

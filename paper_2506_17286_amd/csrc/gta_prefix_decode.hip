@@ -56,7 +56,9 @@ __device__ __forceinline__ void wait_loads(int n) {
 }
 
 constexpr float kLazy = 8.0f;        // log2 units by which a score may pass the maximum that weights refer to
-constexpr int kShared = 64;          // sequences of a batch whose tiles are shared out evenly, a lane each
+// Sequences of a batch whose tiles are shared out evenly, a lane each.  Shared out / in as many pieces for every sequence: 64 of 20 to 1500 rows of the
+// 1B shape 36 / 43 us, 20 to 4096 66 / 75, 4096 each 111 / 114, 32 of the wide shape 73 / 95; 64 of the paper's layer 22 / 21.
+constexpr int kShared = 64;
 
 // Rows lo .. hi of the sequence itself that its new token sees (none: hi < lo); n of them are cached, `own` is the token's position
 __device__ __forceinline__ void own_rows(const StreamArgs &a, int b, int &slot, int &n, int &own, int &lo, int &hi) {
@@ -83,7 +85,8 @@ __device__ __forceinline__ int wave_scan(int v) {
 
 // Pieces in front of and of sequence b (lane b) and how many there are, where a batch is shared out: a round is what a workgroup's
 // waves take at a time, and T rounds make a piece, T the least of a growing series with which there are no more pieces than
-// workgroups, all at once on the chip.  Batches of many sequences are cut finer and dealt out as workgroups end.
+// workgroups, all at once on the chip.  (With more than half as many sequences as those, there may be no such T: about twice as many pieces
+// then, dealt out as workgroups end.)
 template <int NWV>
 __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &mine) {
   const int b = threadIdx.x & 63;
@@ -112,6 +115,8 @@ __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &
 //   S[row][map] = K q^T: lane (x = l % 16, h = l / 16) ends up with map x, rows 4 h .. 4 h + 3 (of each key head; its own is kept);
 //   L[column][map] += C^T p: which is what the second operand wants from that lane.
 // Bound by memory: every row is read once (once per block of maps or slice where a layer's rows are wider than 4 KiB, then from L2).
+// 64 sequences of 20 to 1500 rows of 2 KiB 19.6 us, 5 TB/s; 32 of 100 to 4000 rows of 4 KiB in pages of 64 60 us, 4.7 TB/s; a few short ones 5 us,
+// a chain of lengths, page, keys, latents and the waves' join.
 // bf16 weights are rounded for the second product, as in the kernel of the prefix, and so is their sum.  (Two parts of 16 bits would
 // cost nothing here, but an infinite latent times the second, which may be 0 or less, is no infinity.)
 // Rows in front of the first that is seen are cleared in LDS, rows behind the last read as zeros: what is masked has the weight 0, and
@@ -344,6 +349,7 @@ struct JoinArgs {
 
 // One (sequence, map) and 128 of its columns: the sums of the prefix's and the sequence's own pieces, weighed by 2^(maximum - the
 // largest).  Eight groups of 32 lanes take every eighth piece, four columns a lane, so that most of what is read is asked for at once.
+// Bound by latency: 4.8 us for two sequences, 6.7 for 64 of the 1B shape with 32 pieces of the prefix each.
 constexpr int kMaxPieces = 1280;   // 256 of the prefix, 4 workgroups per CU
 template <typename T>
 __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
@@ -451,7 +457,9 @@ StreamPlan stream_plan(const Dims &d, int batch, int max_seq) {
   return p;
 }
 
-// Prefix: rows of a tile, slices, pieces.
+// Prefix: rows of a tile, slices, pieces, 256 in all, of 128 rows at least.  With 512 and with 128 in all: 64 sequences of the 1B shape behind 8192
+// rows 35.6 us (512: 37.3, 128: 36.2), 256 46.7 (52.4, 56.3), 32 of the wide shape behind 32768 80 (85, 120), fp32 64 of the paper's layer behind 2048
+// 24.1 (24.1, 27.1), two in bf16 behind 32768 28.5 (28.3, 25.1).
 struct PrefixPlan { int bq, mpc, cells, tiles, pieces; };
 
 PrefixPlan prefix_plan(const Dims &d, int batch, int prefix_max) {
