@@ -206,6 +206,7 @@ typedef struct {
  *                 with 0, a smaller workspace that holds one split is used with the splits it holds).
  *   mode PREFILL_MASKED: as PREFILL, for gta_prefill_masked_attention.
  *   mode PREFIX_DECODE: for gta_prefix_decode_attention; total_tokens = prefix->max_seq, max_len = cache->max_seq.
+ *                 (PREFILL_MASKED, PREFIX_DECODE: enough for calls of fewer sequences and tokens, too.)
  * Returns 0 if cfg is NULL or invalid. */
 GTA_API size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64_t total_tokens,
                            int32_t max_len, int32_t num_splits);

@@ -309,9 +309,9 @@ size_t gta_workspace_bytes(const gta_config *cfg, int mode, int32_t batch, int64
   }
   if (mode == GTA_MODE_PREFILL_MASKED || mode == GTA_MODE_PREFIX_DECODE) {
     if (!rules_dims_ok(d) || total_tokens < 0) return 0;
-    if (mode == GTA_MODE_PREFILL_MASKED) return masked_bytes(d, batch, total_tokens) + 256;
+    if (mode == GTA_MODE_PREFILL_MASKED) return masked_bytes_up_to(d, batch, total_tokens) + 256;
     if (total_tokens > (1 << 30) || max_len > (1 << 30)) return 0;
-    return prefix_bytes(d, batch, (int)total_tokens, max_len) + 256;
+    return prefix_bytes_up_to(d, batch, (int)total_tokens, max_len) + 256;
   }
   if (mode == GTA_MODE_DECODE) {
     int splits = choose_splits(d, batch, max_len, num_splits);

@@ -178,19 +178,20 @@ struct MaskedWs {
   size_t bytes;
 };
 
-MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base) {
+// least: slots to have room for at least
+MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base, int64_t least = 0) {
   MaskedWs w{};
   const int mpc = maps_per_cell(d), bq = tile_rows(d), cells = d.nq / mpc, per = cells * (d.dl / columns(d));
   const int64_t tiles = total * mpc / bq + batch;
   w.most = tiles * per < kAtOnce ? kAtOnce : 0;
-  w.slots = w.most ? tiles + kAtOnce / per + 1 : 0;
+  w.slots = std::max(w.most ? tiles + kAtOnce / per + 1 : 0, least);
   w.capacity = std::max(tiles, w.slots);
   size_t off = 0;
   auto take = [&](size_t n) { void *p = base ? (char *)base + off : nullptr; off += align_up(n); return p; };
   w.offsets = (int32_t *)take(((size_t)batch + 1) * 4);
   w.count = (int32_t *)take(8);
   w.list = (Piece *)take((size_t)w.capacity * sizeof(Piece));
-  w.cut = (Piece *)take(w.most ? (size_t)w.capacity * sizeof(Piece) : 0);
+  w.cut = (Piece *)take(w.slots ? (size_t)w.capacity * sizeof(Piece) : 0);
   w.pml = (float2 *)take((size_t)w.slots * cells * bq * 8);
   w.pacc = (float *)take((size_t)w.slots * cells * bq * d.dl * 4);
   w.bytes = off;
@@ -214,6 +215,14 @@ bool masked_fits(const Dims &d, int batch, int64_t total) {
 }
 
 size_t masked_bytes(const Dims &d, int batch, int64_t total) { return masked_fits(d, batch, total) ? carve_masked(d, batch, total, nullptr).bytes : 0; }
+
+size_t masked_bytes_up_to(const Dims &d, int batch, int64_t total) {
+  if (!masked_fits(d, batch, total)) return 0;
+  const MaskedWs w = carve_masked(d, batch, total, nullptr);
+  // the largest batch that is cut has fewer than kAtOnce workgroups
+  const int per = d.nq / maps_per_cell(d) * (d.dl / columns(d));
+  return w.most ? w.bytes : carve_masked(d, batch, total, nullptr, (kAtOnce - 1) / per + kAtOnce / per + 1).bytes;
+}
 
 int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) {
   const MaskedWs w = carve_masked(d, m.batch, m.total, ws);

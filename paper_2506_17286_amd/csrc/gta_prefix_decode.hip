@@ -379,10 +379,12 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
 #pragma unroll
   for (int v = 0; v < kMaxPieces / 256; ++v) {
     const int i = v * 256 + tid;
-    // a piece that sees nothing has left no sums; NaN scores have a weight that is NaN and no maximum
-    const float w = ml[v].y != ml[v].y ? ml[v].y : ml[v].y != 0.f ? __builtin_amdgcn_exp2f(ml[v].x - ref) : 0.f;
+    // a piece that sees nothing has left no sums (weight -1); one of weight 0 takes part: its sums may not be finite.  NaN scores have a
+    // weight that is NaN and no maximum
+    const bool none = ml[v].y == 0.f;
+    const float w = ml[v].y != ml[v].y ? ml[v].y : none ? -1.f : __builtin_amdgcn_exp2f(ml[v].x - ref);
     if (i < all) weight[i] = w;
-    if (w != 0.f) sum = fmaf(w, ml[v].y, sum);
+    if (!none) sum = fmaf(w, ml[v].y, sum);
   }
   for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
   if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
     for (int i = group; i < all; i += 8) {
       const float w = weight[i];
       const float *from = i < S ? j.r.pacc + shared_at(i) * j.s.dl : j.s.pacc + own_at(i - S) * j.s.dl;
-      if (w != 0.f) {
+      if (!(w < 0.f)) {
         const f32x4 p = *reinterpret_cast<const f32x4 *>(from + col);
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = fmaf(w, p[e], v[e]);
@@ -475,11 +477,12 @@ PrefixPlan prefix_plan(const Dims &d, int batch, int prefix_max) {
 
 struct PrefixWs { float *pacc, *oacc; float2 *pml, *oml; int32_t *first; size_t bytes; };
 
-PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const StreamPlan &s, void *base) {
+// prows: rows of pieces of the prefix in all cells; opieces: pieces of own rows
+PrefixWs carve_prefix(const Dims &d, int batch, size_t prows, size_t opieces, void *base) {
   PrefixWs w{};
   size_t off = 0;
   auto take = [&](size_t n) { void *q = base ? (char *)base + off : nullptr; off += align_up(n); return q; };
-  const size_t prows = (size_t)p.tiles * p.pieces * p.cells * p.bq, orows = (size_t)s.grid * d.nq;
+  const size_t orows = opieces * d.nq;
   w.first = (int32_t *)take(((size_t)batch + 1) * 4);
   w.pml = (float2 *)take(prows * 8);
   w.oml = (float2 *)take(orows * 8);
@@ -487,6 +490,9 @@ PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const Strea
   w.oacc = (float *)take(orows * d.dl * 4);
   w.bytes = off;
   return w;
+}
+PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const StreamPlan &s, void *base) {
+  return carve_prefix(d, batch, (size_t)p.tiles * p.pieces * p.cells * p.bq, (size_t)s.grid, base);
 }
 
 template <typename T, int DH, int NF>
@@ -536,6 +542,28 @@ bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq) {
 size_t prefix_bytes(const Dims &d, int batch, int prefix_max, int max_seq) {
   if (!prefix_fits(d, batch, prefix_max, max_seq)) return 0;
   return carve_prefix(d, batch, prefix_plan(d, batch, prefix_max), stream_plan(d, batch, max_seq), nullptr).bytes;
+}
+
+// What is enough for any batch of up to `batch` sequences: fewer may be cut into more pieces, or into larger tiles' worth of them.
+size_t prefix_bytes_up_to(const Dims &d, int batch, int prefix_max, int max_seq) {
+  if (!prefix_fits(d, batch, prefix_max, max_seq)) return 0;
+  const int mpc = maps_per_cell(d);
+  size_t prows = 0;
+  for (int rows : {32, 64, INT_MAX}) {   // where prefix_tile_rows changes
+    const int b = std::min(batch, rows / mpc);
+    if (b == 0) continue;
+    const PrefixPlan p = prefix_plan(d, b, prefix_max);
+    const size_t tiles = (size_t)p.tiles * p.cells, slices = d.dtype == GTA_BF16 ? prefix_slices(d, p.bq, prefix_max) : d.dl / rows_f32_columns(d);
+    prows = std::max(prows, std::min(tiles + 256 / slices, tiles * std::max<size_t>(1, ((size_t)prefix_max + 127) / 128)) * p.bq);
+  }
+  const StreamPlan s = stream_plan(d, batch, max_seq);
+  size_t opieces = (size_t)s.grid;
+  if (batch > kShared) {
+    const size_t per = (size_t)d.nc * s.blocks * (d.dl / (s.nf * 64));
+    opieces = std::max<size_t>(opieces, std::min<size_t>(512 / per + batch, (size_t)batch * (((size_t)max_seq + 127) / 128)));
+    opieces = std::max<size_t>(opieces, (size_t)stream_plan(d, kShared, max_seq).grid);
+  }
+  return std::max(carve_prefix(d, batch, prows, opieces, nullptr).bytes, prefix_bytes(d, batch, prefix_max, max_seq));
 }
 
 bool prefix_layout_ok(const gta_cache &prefix, const gta_cache &own) { return pages_ok(prefix) && pages_ok(own); }

@@ -97,7 +97,8 @@ void launch_rows_f32(const Dims &d, const RowsArgs &a, bool cache, hipStream_t s
 bool masked_tuned(const Dims &d);
 bool masked_fits(const Dims &d, int batch, int64_t total);
 bool rows_operands_ok(const void *p, int64_t stride, int esize);
-size_t masked_bytes(const Dims &d, int batch, int64_t total);
+size_t masked_bytes(const Dims &d, int batch, int64_t total);        // of a call
+size_t masked_bytes_up_to(const Dims &d, int batch, int64_t total);  // of any of as many sequences and tokens or fewer
 int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st);
 
 // The prefix's rows: rows of a tile for `rows` query rows of a cell, workgroups that share its latent columns, launch
@@ -110,6 +111,7 @@ bool prefix_tuned(const Dims &d);   // with pages of a power of two of at least 
 bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq);
 bool prefix_layout_ok(const gta_cache &prefix, const gta_cache &own);
 size_t prefix_bytes(const Dims &d, int batch, int prefix_max, int max_seq);
+size_t prefix_bytes_up_to(const Dims &d, int batch, int prefix_max, int max_seq);
 int launch_prefix(const Dims &d, const PrefixArgs &x, void *ws, hipStream_t st);
 
 }  // namespace gta

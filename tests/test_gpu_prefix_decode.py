@@ -174,6 +174,33 @@ def test_what_is_not_seen_does_not_leak(name, dtype, value):
         run(name, dtype, 120, [30, 30, 30, 30, 30, 30], first=first, last=last, edit=edit, seed=12, page=page)
 
 
+@pytest.mark.parametrize("where", ["prefix", "own"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", ["paper", "1b", "wide", "odd"])
+def test_an_infinite_latent_of_next_to_no_weight_shows(name, dtype, where):
+    """One row has all the weight that fp32 can hold next to it; what is seen and not finite must not be lost with the rest."""
+    cfg, sh, gen = R.config(name, dtype), R.SHAPES[name], R.generator(21)
+    prefix, own = Cache(name, dtype, [600], 640, gen), Cache(name, dtype, [300, 40], 320, gen)
+    dh = sh["head_dim"]
+    for t in (prefix, own):   # q . k / sqrt(d_h): 160 nats below
+        t.k.copy_(torch.full_like(t.k, -80.0 / dh ** 0.5))
+    prefix.k[0, 3] = 80.0 / dh ** 0.5
+    rows = prefix.c[0, 3].double().clone()
+    (prefix if where == "prefix" else own).c[0, 200, 5] = float("inf")
+    q = torch.ones(2, sh["n_qgroups"] * dh, dtype=R.DT[dtype], device="cuda")
+    out = torch.zeros(2, sh["n_qgroups"] * sh["latent_dim"], dtype=R.DT[dtype], device="cuda")
+    ws = B.alloc_workspace(B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFIX_DECODE, 2, prefix.room, own.room))
+    B.gta_prefix_decode_attention(cfg, q, prefix.struct, 0, own.struct, None, 2, None, out, ws)
+    qpc = sh["n_qgroups"] // sh["n_cgroups"]
+    for b in range(2):
+        for g in range(sh["n_qgroups"]):
+            row, latent = out[b].view(-1, sh["latent_dim"])[g].double(), rows.view(-1, sh["latent_dim"])[g // qpc]
+            hit = torch.zeros_like(row, dtype=torch.bool)
+            hit[5] = g // qpc == 0 and (where == "prefix" or b == 0)
+            assert not bool(torch.isfinite(row[hit]).any()), (b, g)
+            assert bool((row[~hit] == latent[~hit]).all()), (b, g)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_a_query_that_is_not_finite_reaches_its_own_row_only(dtype):
     def edit(prefix, own, q):

@@ -72,6 +72,31 @@ for name, dt, sh, cfg in cfgs():
             len(names) == 3 and "rows_attn" in names[0] and "stream_kernel" in names[1] and "prefix_join_kernel" in names[2]), names
 
 
+def test_workspaces_of_fuller_batches():
+    """What gta_workspace_bytes says for a batch is enough for every smaller one."""
+    out = S.run(SETUP + """
+for name, dt, sh, cfg in cfgs():
+    q, k, c = widths(sh)
+    for rows, own in ((500, 1 << 12), (40000, 96)):
+        for most in (40, 70, 300):
+            n = B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFIX_DECODE, most, rows, own)
+            caches = [B.gta_cache(FAKE, FAKE, FAKE, FAKE, 400, r, None, 0, 0, 0) for r in (rows, own)]
+            for batch in (1, 2, 6, 7, 8, 12, 13, 16, 32, 33, 64, 65, 128, 129, 300):
+                if batch <= most:
+                    rc = B.load().gta_prefix_decode_attention(R(cfg), FAKE, R(caches[0]), 0, R(caches[1]), None, batch, None, FAKE, FAKE, n, None)
+                    out.append([rc, [name, dt, most, batch]])
+    for most in (3000, 20000):
+        n = B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFILL_MASKED, 20, most, most)
+        for total in (1, 100, 500, 1000, 1700, 2500, 4000, 6000, 8000, 10000, 15000, 20000):
+            for batch in (1, 20):
+                if total <= most:
+                    rc = B.load().gta_prefill_masked_attention(R(cfg), FAKE, q, FAKE, k, FAKE, c, FAKE, batch, total, total, None, FAKE, FAKE, n, None)
+                    out.append([rc, [name, dt, most, total]])
+    events()
+""")
+    assert out and all(rc == 0 for rc, _ in out), [case for rc, case in out if rc]
+
+
 def test_every_width_of_own_rows_has_its_kernel():
     out = S.run("""
 for dh in (64, 128):

@@ -4,6 +4,7 @@ import math
 
 import pytest
 
+import rules_util as U
 from paper_2506_17286_amd import binding as B
 
 FAKE = 4096   # never dereferenced: every call below is refused first
@@ -194,14 +195,29 @@ def test_workspaces(mode):
         call = _masked if mode == B.GTA_MODE_PREFILL_MASKED else _prefix
         kw = dict(batch=batch, total=total, longest=longest, cu=FAKE) if call is _masked else dict(
             batch=batch, prefix=_cache(max_seq=total), cache=_cache(max_seq=longest, max_batch=65535))
-        need = n - 256
-        if need > 0:
-            assert call(cfg, size=max(need - 1, 0), **kw) == B.GTA_ERR_WORKSPACE
+        if n > 256:
+            assert call(cfg, size=0, **kw) == B.GTA_ERR_WORKSPACE
     assert B.gta_workspace_bytes(cfg, mode, 0, 1, 1) == 0
     assert B.gta_workspace_bytes(cfg, mode, 1, -1, 1) == 0
     assert B.gta_workspace_bytes(cfg, mode, 1, 1, -1) == 0
     assert B.gta_workspace_bytes(_cfg(latent_dim=4100), mode, 1, 1, 1) == 0
     assert B.gta_uses_tuned_kernels(_cfg(latent_dim=4100), mode) == B.GTA_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", sorted(U.SHAPES))
+def test_a_workspace_does_for_fewer_sequences_and_tokens(name, dtype):
+    cfg = U.config(name, dtype)
+    for rows, own in ((0, 0), (1, 1), (500, 4096), (8192, 100), (40000, 1 << 20)):
+        sizes = [B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFIX_DECODE, b, rows, own) for b in [*range(1, 300), 400, 511, 512, 1000, 3000, 65535]]
+        assert sizes == sorted(sizes), (rows, own)
+    totals = [1, 2, 31, 100, 1000, *range(1500, 9000, 250), 10000, 20000, 40000, 1 << 20]
+    for batch in (1, 2, 30, 300, 3000):
+        sizes = [B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFILL_MASKED, batch, t, t) for t in totals]
+        assert sizes == sorted(sizes), batch
+    for t in totals:
+        sizes = [B.gta_workspace_bytes(cfg, B.GTA_MODE_PREFILL_MASKED, b, t, t) for b in (1, 2, 7, 30, 64, 100, 200, 300, 3000)]
+        assert sizes == sorted(sizes), t
 
 
 def test_binding_looks_at_tensors():
