@@ -36,6 +36,9 @@ __device__ __forceinline__ int wave_min(int v) {
 template <int DH, int DLW, bool CACHE>
 __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_kernel(RowsArgs a) {
   constexpr int NT = DLW / 32, OP = DLW + 4, BQ = 32;
+  // A score's products are added up 32 at a time: one sum over a head of 128 is off by twice as much (one sequence of 3000 keys, error of its
+  // row 1.3e-6 and 0.7e-6).  (Two sums where registers are short; four spill 31 of them.)
+  constexpr int SUMS = DH == 128 && DLW == 64 ? 2 : DH / 32;
   typedef float cvec __attribute__((ext_vector_type(NT)));
   extern __shared__ __attribute__((aligned(16))) float dyn[];
   float (*lacc)[32][OP] = reinterpret_cast<float (*)[32][OP]>(dyn);   // [4][32][OP]
@@ -139,11 +142,16 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
     const int next = max(blk - 4, b0);   // (behind the last one: loaded, not used)
     f32x16 s;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    for (int i = 0; i < SUMS; ++i) {
+      f32x16 part;
 #pragma unroll
-    for (int c = 0; c < DH / 8; ++c)
+      for (int e = 0; e < 16; ++e) part[e] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][j], qf[c][j], s, 0, 0, 0);
+      for (int c = i * (DH / 8 / SUMS); c < (i + 1) * (DH / 8 / SUMS); ++c)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) part = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][j], qf[c][j], part, 0, 0, 0);
+      s = i ? s + part : part;
+    }
     runs(next, p0, p1);
     kload(next);
     const int from = lo - blk * 32 - 4 * h, to = hi - blk * 32 - 4 * h;

@@ -239,7 +239,8 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
 #pragma unroll 1
     for (int kk = 0; kk < heads; ++kk) {
       const char *kr = kmem + kk * KI * 1024 + x * KCH * 16;
-      f32x4 d{0.f, 0.f, 0.f, 0.f}, kf[KS];
+      f32x4 d{0.f, 0.f, 0.f, 0.f}, kf[KS], part[3];   // fp32: four sums of a quarter of the products each, off by half as much as one
+      if constexpr (ES == 4) part[0] = part[1] = part[2] = d;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const f32x4 *>(kr + ((ks * 4 + h) ^ (x & 7)) * 16);
 #pragma unroll
@@ -247,9 +248,13 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
         if constexpr (ES == 2) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[ks]), __builtin_bit_cast(bf16x8, qf[ks]), d, 0, 0, 0);
         else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) d = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[ks][e], qf[ks][e], d, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) {
+            f32x4 &to = e == 0 ? d : part[e - 1];
+            to = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[ks][e], qf[ks][e], to, 0, 0, 0);
+          }
         }
       }
+      if constexpr (ES == 4) d = (d + part[0]) + (part[1] + part[2]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] = head == kk ? d[e] : s[e];
     }
