@@ -3,7 +3,7 @@
 // that are joined in LDS at the end.  Both products are transposed, S^T = K Q^T and L^T += C^T P^T: weights go from one's
 // accumulators into the other.  Keys and latents come from memory straight into registers, the next block's as this one's come free.
 // Bound by the matrix instructions (64 cycles for 2048 products) and by how evenly tiles fall on the CUs: 4 x 1024 tokens of the paper's
-// layer with a bias 61 us, 66 TFLOP/s of the 153 that a large matrix product reaches; 640 workgroups, two on a CU, and a wave has up
+// layer with a bias 58 us, 69 TFLOP/s of the 153 that a large matrix product reaches; 640 workgroups, two on a CU, and a wave has up
 // to 8 steps between filling its registers and joining its sums.
 //
 // A masked weight is 0, but 0 times a latent that is not finite is NaN: a tile whose sums are not finite in the end is gone through
@@ -34,10 +34,13 @@ __device__ __forceinline__ int wave_min(int v) {
 }
 
 template <int DH, int DLW, bool CACHE>
-__global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_kernel(RowsArgs a) {
+__global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_attn_f32_kernel(RowsArgs a) {
   constexpr int NT = DLW / 32, OP = DLW + 4, BQ = 32;
   // A score's products are added up 32 at a time: one sum over a head of 128 is off by twice as much (one sequence of 3000 keys, error of its
   // row 1.3e-6 and 0.7e-6).  (Two sums where registers are short; four spill 31 of them.)
+  // Queries in LDS, so that two workgroups share a CU's registers: 1B shape, 4 x 1024 tokens 268 -> 231 us, 464 tokens 125 -> 105, 60 tokens 13.9 -> 14.8.
+  // Not on caches, whose addresses take more of them: 16 sequences of the wide shape behind 8000 rows 114 -> 160.
+  constexpr bool QLDS = DH + DLW == 256 && !CACHE;
   constexpr int SUMS = DH == 128 && DLW == 64 ? 2 : DH / 32;
   typedef float cvec __attribute__((ext_vector_type(NT)));
   extern __shared__ __attribute__((aligned(16))) float dyn[];
@@ -105,11 +108,18 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
       p1 = find(j1);
     } else p0 = p1 = krow0;
   };
-  f32x4 qf[DH / 8];
+  f32x4 qf[QLDS ? 1 : DH / 8];
+  f32x4 *ql = reinterpret_cast<f32x4 *>(dyn) + lane;   // [DH / 8][64], until the waves are joined
   {
     const float *qp = (const float *)a.q + (start + tok) * a.qs + g * DH + h * 4;
+    if constexpr (QLDS) {
 #pragma unroll
-    for (int c = 0; c < DH / 8; ++c) qf[c] = *reinterpret_cast<const f32x4 *>(qp + c * 8);
+      for (int c = wave * (DH / 32); c < (wave + 1) * (DH / 32); ++c) ql[c * 64] = *reinterpret_cast<const f32x4 *>(qp + c * 8);
+      __syncthreads();
+    } else {
+#pragma unroll
+      for (int c = 0; c < DH / 8; ++c) qf[c] = *reinterpret_cast<const f32x4 *>(qp + c * 8);
+    }
   }
   f32x16 acc[NT];
 #pragma unroll
@@ -120,13 +130,30 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
   f32x4 kf[DH / 8];
   cvec cf[16];
   int64_t p0 = 0, p1 = 0;
+  // Packed rows: a block's first row is uniform, its rows are within 32 bits of it (heads of 64, 4 x 1024 tokens with a bias 68.4 -> 63.7 us; heads of
+  // 128, where registers are shorter, 231 -> 275)
+  constexpr bool UNIFORM = !CACHE && DH <= 64;
+  const unsigned ks = (unsigned)a.ks, cs = (unsigned)a.cs;
   auto kload = [&](int blk) {
+    if constexpr (UNIFORM) {
+      const char *base = (const char *)(kcol + (start + blk * 32) * a.ks);
+      const unsigned off = ((unsigned)min(ln, keys - 1 - blk * 32) * ks + h * 4) * 4;
+#pragma unroll
+      for (int c = 0; c < DH / 8; ++c) kf[c] = *reinterpret_cast<const f32x4 *>(base + (off + c * 32));
+      return;
+    }
     const int key = min(blk * 32 + ln, keys - 1);
     const float *p = kcol + ((ln < 16 || key < blk * 32 + 16 ? p0 : p1) + key) * a.ks + h * 4;
 #pragma unroll
     for (int c = 0; c < DH / 8; ++c) kf[c] = *reinterpret_cast<const f32x4 *>(p + c * 8);
   };
   auto cload = [&](int blk, int e) {
+    if constexpr (UNIFORM) {
+      const char *base = (const char *)(ccol + (start + blk * 32) * a.cs);
+      const unsigned off = ((unsigned)min(8 * (e >> 2) + 4 * h + (e & 3), keys - 1 - blk * 32) * cs + ln * NT) * 4;
+      cf[e] = *reinterpret_cast<const cvec *>(base + off);
+      return;
+    }
     const int key = min(blk * 32 + 8 * (e >> 2) + 4 * h + (e & 3), keys - 1);
     cf[e] = *reinterpret_cast<const cvec *>(ccol + ((e < 8 || key < blk * 32 + 16 ? p0 : p1) + key) * a.cs + ln * NT);
   };
@@ -141,15 +168,20 @@ __global__ __launch_bounds__(256, DH + DLW < 256 ? 2 : 1) void rows_attn_f32_ker
   for (; blk >= b0; blk -= 4) {
     const int next = max(blk - 4, b0);   // (behind the last one: loaded, not used)
     f32x16 s;
+    if constexpr (QLDS) asm volatile("" ::: "memory");   // the queries are read again in every step
 #pragma unroll
     for (int i = 0; i < SUMS; ++i) {
       f32x16 part;
 #pragma unroll
       for (int e = 0; e < 16; ++e) part[e] = 0.f;
 #pragma unroll
-      for (int c = i * (DH / 8 / SUMS); c < (i + 1) * (DH / 8 / SUMS); ++c)
+      for (int c = i * (DH / 8 / SUMS); c < (i + 1) * (DH / 8 / SUMS); ++c) {
+        f32x4 q;
+        if constexpr (QLDS) q = ql[c * 64];
+        else q = qf[c];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) part = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][j], qf[c][j], part, 0, 0, 0);
+        for (int j = 0; j < 4; ++j) part = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][j], q[j], part, 0, 0, 0);
+      }
       s = i ? s + part : part;
     }
     runs(next, p0, p1);
