@@ -420,6 +420,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
     }
   };
   plain_until(min(p0, nsteps));
+  __builtin_amdgcn_s_waitcnt(0xc07f);   // lgkmcnt(0): a scalar load on its way would make every wait for LDS in the loop one for all of it (87 -> 90 us)
 #pragma unroll 1
   for (; t < p1; ++t) {
     // The scores of block t + 1, then the second product of block t with the softmax of block t + 1 between its instructions;
@@ -508,8 +509,8 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
       if (T::NDLB == 1 && lane >= 32) continue;
       if (split) {
 #pragma unroll
-        for (int e = 0; e < COLS; ++e) a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = sum[e];
-        if (lane == 0 && slice == 0 && cg == 0) a.pml[at + qw * 32 + i] = ml;
+        for (int e = 0; e < COLS; ++e)
+          a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = sum[e] * (ml.y == 0.f ? 0.f : 1.f / ml.y);
       } else {
         const float inv = l0 <= l1 ? 1.f / ml.y : 0.f;
 #pragma unroll
@@ -520,11 +521,12 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   } else if (split) {
     if (wr0 + ln < R) {
       float *pa = a.pacc + (at + my) * a.dl + slice * T::DLW + cg * T::NDLB * 32 + 4 * h;
+      const float inv = l_all == 0.f ? 0.f : 1.f / l_all;   // (a piece may have none of the keys that a row sees)
       each<T::NDLB * 4>(EACH(i) {
         constexpr int dlb = i / 4, rq = i % 4;
-        *reinterpret_cast<float4 *>(pa + dlb * 32 + rq * 8) = make_float4(acc[dlb][rq * 4], acc[dlb][rq * 4 + 1], acc[dlb][rq * 4 + 2], acc[dlb][rq * 4 + 3]);
+        *reinterpret_cast<float4 *>(pa + dlb * 32 + rq * 8) =
+            make_float4(acc[dlb][rq * 4] * inv, acc[dlb][rq * 4 + 1] * inv, acc[dlb][rq * 4 + 2] * inv, acc[dlb][rq * 4 + 3] * inv);
       });
-      if (h == 0 && slice == 0 && cg == 0) a.pml[at + my] = sees ? make_float2(m_run, l_all) : make_float2(-INFINITY, 0.f);
     }
   } else {
     const float inv = 1.0f / l_all;
@@ -536,7 +538,10 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
       *reinterpret_cast<bf16x4 *>(smem + my * T::OUT_PITCH + (cg * T::NDLB * 32 + dlb * 32 + rq * 8 + 4 * h) * 2) = v;
     });
   }
-  if (split) return;
+  if (split) {   // whether the wave went through its rows again or not
+    if (h == 0 && slice == 0 && cg == 0 && wr0 + ln < R) a.pml[at + my] = sees ? make_float2(m_run, l_all) : make_float2(-INFINITY, 0.f);
+    return;
+  }
   __syncthreads();
   constexpr int CPR = T::DLW / 8, RPP = T::NT / CPR;   // 16-byte chunks of a row, rows per pass
   const int rr0 = tid / CPR, ch = tid % CPR;

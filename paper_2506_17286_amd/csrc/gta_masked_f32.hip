@@ -260,7 +260,13 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
     sums[i] = v;
     odd |= (v[0] * 0.f + v[1] * 0.f) + (v[2] * 0.f + v[3] * 0.f) != 0.f;
   }
-  if (__builtin_expect(__syncthreads_or(odd), 0)) {
+  const bool again = __syncthreads_or(odd);
+  if (split && slice == 0 && tid < BQ && r0 + tid < R) {   // (the first wave has the first 32 rows in its lanes)
+    float top;
+    const float sum = weight_of(tid, top);
+    a.pml[at + tid] = sees ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
+  }
+  if (__builtin_expect(again, 0)) {
 #pragma unroll 1
     for (int i = wave * 8; i < wave * 8 + 8 && r0 + i < R; ++i) {
       constexpr int COLS = DLW / 64;
@@ -270,11 +276,10 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
       const float2 ml = wave_row(a, (const float *)a.q + (start + tk) * a.qs + gg * DH, DH, kcol, ccol, __shfl(slope, i), __shfl(own, i), from, to,
                                  [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, sum);
       float *to_row = split ? a.pacc + (at + i) * a.dl : (float *)a.L + ((start + tk) * a.nq + gg) * (int64_t)a.dl;
-      const float inv = split ? 1.f : 1.f / ml.y;
-      const bool any = split || __shfl(sees ? 1 : 0, i);
+      const float inv = split && ml.y == 0.f ? 0.f : 1.f / ml.y;   // (a piece may have none of the keys that a row sees)
+      const bool any = __shfl(sees ? 1 : 0, i);
 #pragma unroll
       for (int e = 0; e < COLS; ++e) to_row[slice * DLW + e * 64 + lane] = any ? sum[e] * inv : 0.f;
-      if (split && lane == 0 && slice == 0) a.pml[at + i] = ml;
     }
     return;
   }
@@ -285,14 +290,12 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
     if (r0 + rr >= R) continue;
     float top;
     const float sum = weight_of(rr, top);
-    if (split) {
-      *reinterpret_cast<f32x4 *>(a.pacc + (at + rr) * a.dl + slice * DLW + col) = sums[i];
-      if (col == 0 && slice == 0) a.pml[at + rr] = any ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
-    } else {
+    const float inv = any && !(split && sum == 0.f) ? 1.f / sum : 0.f;
+    f32x4 v = sums[i] * inv;
+    if (!any) v = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (split) *reinterpret_cast<f32x4 *>(a.pacc + (at + rr) * a.dl + slice * DLW + col) = v;
+    else {
       const int tk = (r0 + rr) / a.mpc;
-      const float inv = any ? 1.f / sum : 0.f;
-      f32x4 v = sums[i] * inv;
-      if (!any) v = f32x4{0.f, 0.f, 0.f, 0.f};
       *reinterpret_cast<f32x4 *>((float *)a.L + ((start + tk) * a.nq + cell * a.mpc + (r0 + rr - tk * a.mpc)) * (int64_t)a.dl + slice * DLW + col) = v;
     }
   }

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   if (tid == 0) { a.count[0] = min(total_s, a.capacity); a.count[1] = min(cuts_s, a.capacity); }
 }
 
-// Joins the pieces of one row of a tile: weights 2^(m - max); a wave per (row, cell), four columns a lane and step.
+// Joins the pieces of one row of a tile: weights l 2^(m - max); a wave per (row, cell), four columns a lane and step.
 template <typename T>
 __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piece *cut, int bq) {
   if ((int)blockIdx.x >= a.count[1]) return;
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
     for (int i = 0; i < p.pieces; ++i) {
       const float2 ml = a.pml[at(i)];
       if (ml.y == 0.f) continue;   // sees none of the piece's keys
-      const float w = __builtin_amdgcn_exp2f(ml.x - ref) * inv;
+      const float w = __builtin_amdgcn_exp2f(ml.x - ref) * ml.y * inv;
       const float4 s = *reinterpret_cast<const float4 *>(a.pacc + at(i) * a.dl + col);
       v.x = fmaf(w, s.x, v.x); v.y = fmaf(w, s.y, v.y); v.z = fmaf(w, s.z, v.z); v.w = fmaf(w, s.w, v.w);
     }

@@ -1,9 +1,9 @@
 // One new token per sequence over a prefix that the batch shares and over the sequence's own cached rows, with rules on the scores
 // (gta_score_rules):
 //   1. the prefix is read once for all: the batch's queries are the rows of rows_attn_kernel (bf16) and rows_attn_f32_kernel, which
-//      leave un-normalised sums of pieces of the prefix;
+//      leave averages over pieces of the prefix;
 //   2. stream_kernel reads every sequence's own rows once for all its maps, in pieces, too;
-//   3. prefix_join_kernel weighs the sums by their maxima.
+//   3. prefix_join_kernel weighs the averages by what their pieces count.
 #include <math.h>
 
 #include <type_traits>
@@ -31,7 +31,7 @@ struct StreamArgs {
   int wave_lds, ps_shift;      // bytes of a wave
   int share, each;             // workgroups that a batch's tiles are shared out to; or (> 0) pieces of every sequence
   int32_t *first;              // [batch + 1] pieces in front of each sequence
-  float *pacc; float2 *pml;    // [pieces, n_q, d_l], [pieces, n_q]
+  float *pacc; float2 *pml;    // averages [pieces, n_q, d_l], maximum and weight [pieces, n_q]
 };
 
 __device__ __forceinline__ int load_uniform(const int32_t *p) {
@@ -340,7 +340,8 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
       for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, c[e], v[e]);
       sum = fmaf(wt, ml.y, sum);
     }
-    *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v;
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v * inv;
     if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, sum);
   }
 }
@@ -352,8 +353,8 @@ struct JoinArgs {
   void *l_out;
 };
 
-// One (sequence, map) and 128 of its columns: the sums of the prefix's and the sequence's own pieces, weighed by 2^(maximum - the
-// largest).  Eight groups of 32 lanes take every eighth piece, four columns a lane, so that most of what is read is asked for at once.
+// One (sequence, map) and 128 of its columns: the averages of the prefix's and the sequence's own pieces, weighed by weight * 2^(maximum -
+// the largest).  Eight groups of 32 lanes take every eighth piece, four columns a lane, so that most of what is read is asked for at once.
 // Bound by latency: 4.8 us for two sequences, 6.7 for 64 of the 1B shape with 32 pieces of the prefix each.
 constexpr int kMaxPieces = 1280;   // 256 of the prefix, 4 workgroups per CU
 template <typename T>
@@ -384,12 +385,12 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
 #pragma unroll
   for (int v = 0; v < kMaxPieces / 256; ++v) {
     const int i = v * 256 + tid;
-    // a piece that sees nothing has left no sums (weight -1); one of weight 0 takes part: its sums may not be finite.  NaN scores have a
-    // weight that is NaN and no maximum
+    // a piece that sees nothing has left no averages (weight -1); one of weight 0 takes part: its averages may not be finite.  NaN scores
+    // have a weight that is NaN and no maximum
     const bool none = ml[v].y == 0.f;
-    const float w = ml[v].y != ml[v].y ? ml[v].y : none ? -1.f : __builtin_amdgcn_exp2f(ml[v].x - ref);
+    const float w = ml[v].y != ml[v].y ? ml[v].y : none ? -1.f : __builtin_amdgcn_exp2f(ml[v].x - ref) * ml[v].y;
     if (i < all) weight[i] = w;
-    if (!none) sum = fmaf(w, ml[v].y, sum);
+    if (!none) sum += w;
   }
   for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
   if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;

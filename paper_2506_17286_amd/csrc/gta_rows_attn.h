@@ -2,7 +2,9 @@
 //
 // Maps that read the same key head and the same latent group form a cell (mpc of them); the rows of a cell are the (token, map)
 // pairs of a sequence, token by token, and a workgroup takes a tile of BQ of them.  A tile's keys can be shared out over several
-// pieces, which leave un-normalised fp32 sums, their maximum (in units of log 2) and their weight in a slot of scratch memory.
+// pieces, which leave fp32 averages over their keys, and per row a maximum m (in units of log 2) and a weight l, in a slot of scratch
+// memory: the piece counts as l 2^m.  Averages do not depend on what their weights referred to, so that whichever workgroup or wave of a row's
+// columns goes through its keys again (wave_row) leaves what the row's one (m, l) fits.
 #pragma once
 #include <algorithm>
 
@@ -24,7 +26,7 @@ struct RowsArgs {
   const Piece *list;                // work, in the order it is started; NULL: every tile of every sequence, whole
   const int32_t *count;
   int tiles;                        // of the launch
-  float *pacc; float2 *pml;         // [slot, cell, BQ, d_l], [slot, cell, BQ]
+  float *pacc; float2 *pml;         // averages [slot, cell, BQ, d_l], (m, l) [slot, cell, BQ]
   // keys from one slot of a cache (prefix): tokens are sequences, which see its rows; `pieces` of every tile
   CacheView prefix, own;
   int prefix_slot, pieces, ps_shift;
