@@ -206,7 +206,7 @@ static bool bad_stride(int64_t stride, int width) { return stride < width || str
 
 static int check_rules(const gta_score_rules *r) {
   if (!r) return GTA_OK;
-  if (!(r->cap == 0.f || (r->cap >= 1e-30f && r->cap <= 1e30f))) return GTA_ERR_SHAPE;   // its inverse and fourth powers are worked with
+  if (!(r->cap == 0.f || (r->cap >= 1e-30f && r->cap <= 1e30f))) return GTA_ERR_SHAPE;   // its inverse is worked with
   return (((uintptr_t)r->slopes | (uintptr_t)r->first | (uintptr_t)r->last) & 3u) ? GTA_ERR_ALIGN : GTA_OK;
 }
 

@@ -3,6 +3,8 @@
 #pragma once
 #include <math.h>
 
+#include <algorithm>
+
 #include "gta_internal.h"
 
 namespace gta {
@@ -17,9 +19,11 @@ constexpr float kLog2e = 1.4426950408889634f;
 // The rules as kernels take them: scores leave them in units of log 2.
 struct Rules {
   float scale, cap, inv_cap;   // softmax scale; cap and its inverse, 0 where there is none
-  // cap * tanh(s / cap) for |s| <= cap, s and result in units of log 2 as `scale2` makes them: s times a polynomial in s^2, off by
-  // at most 6.9e-6 of the result (the best of its degree for tanh(x) / x up to 1).  Below what weights of 16 bits show (2^-9).
-  float scale2, near, steep, poly[5];   // near: the cap in these units; steep * (q . k) = 2 log2(e) (s / cap)
+  // cap * tanh(s / cap) for |s| <= near, s and result in units of log 2 as `scale2` makes them: s times a polynomial in s^2, off by
+  // at most 6.9e-6 of the result (the best of its degree for tanh(x) / x up to 1).  `near` is the cap, or where that is more 256 (times
+  // log2 e), so that the error is below 2^-9, half of what a rounded weight of 16 bits is off by.  Caps below 2^-10, whose coefficients of up
+  // to cap^-8 would leave fp32, have near = -1: no score is.
+  float scale2, cap2, near, steep, poly[5];   // cap2: the cap in these units; steep * (q . k) = s / cap, where near = cap2 times 2 log2(e)
   const float *slopes;
   const int32_t *first, *last;
 };
@@ -31,9 +35,11 @@ inline Rules rules_of(const Dims &d, const gta_score_rules *r) {
   if (r) {
     const double cap2 = (double)r->cap * 1.4426950408889634;
     const double best[5] = {0.999993088553236, -0.33298064162659136, 0.1303680737376961, -0.044817503256505964, 0.009036401546491156};
-    out.near = (float)cap2;
-    out.steep = r->cap > 0.f ? (float)(2.0 * 1.4426950408889634 * d.scale / r->cap) : 0.f;
-    for (int i = 0; i < 5 && r->cap > 0.f; ++i) out.poly[i] = (float)(best[i] * pow(cap2, -2.0 * i));
+    const bool polynomial = r->cap >= 0x1p-10f;
+    out.cap2 = (float)cap2;
+    out.near = polynomial ? std::min(out.cap2, 256.f * kLog2e) : -1.f;
+    out.steep = r->cap > 0.f ? (float)std::min((out.near == out.cap2 ? 2.0 * 1.4426950408889634 : 1.0) * d.scale / r->cap, 3e38) : 0.f;
+    for (int i = 0; i < 5 && polynomial; ++i) out.poly[i] = (float)(best[i] * pow(cap2, -2.0 * i));
     out.cap = r->cap;
     out.inv_cap = r->cap > 0.f ? 1.f / r->cap : 0.f;
     out.slopes = r->slopes; out.first = r->first; out.last = r->last;
