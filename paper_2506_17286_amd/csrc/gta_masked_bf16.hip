@@ -15,8 +15,8 @@
 // paper's layer, a cap, 96 us (620); 2 x 8192 of the wide shape, window, cap and bias 1275 us (690; with the scores, which each of four latent
 // tiles works out, 920).  A cap costs 21 to 28 %, a bias 4 to 11.
 //
-// A masked weight is 0, but 0 times a latent that is not finite is NaN: a wave whose sums are not finite in the end goes through
-// its rows once more, one by one, over the keys that each sees (wave_row).
+// A masked weight is 0, but 0 times a latent that is not finite is NaN, and sums of finite ones may pass the range: a wave whose sums are not
+// finite in the end goes through its rows once more, one by one, over the keys that each sees (wave_row).
 #include <math.h>
 
 #include <type_traits>
@@ -512,21 +512,19 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
       const int from = max(l0, b0 * 32), to = min(l1, min(b1 * 32, keys) - 1);
       int own_i = tk;
       if constexpr (CACHE) own_i = (int)((int64_t)keys + slot_rows(a.own, a.own.slots ? a.own.slots[tk] : tk) - 1);
-      float sum[COLS];
+      float avg[COLS];
       const bf16 *cc = ccol + c0 - (T::NDLB == 1 && lane >= 32 ? 32 : 0);
-      const float2 ml = wave_row(a, (const bf16 *)a.q + (start + tk) * a.qs + gg * T::DH, T::DH, kcol, cc,
-                                       MODS & kBias ? a.rules.slopes[gg] : 0.f, own_i, from, to,
-                                       [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, sum);
+      const float w = wave_row(a.rules, (const bf16 *)a.q + (start + tk) * a.qs + gg * T::DH, T::DH, kcol, a.ks, cc, a.cs,
+                               MODS & kBias ? a.rules.slopes[gg] : 0.f, own_i, from, to,
+                               [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, avg);
       if (T::NDLB == 1 && lane >= 32) continue;
       if (split) {
 #pragma unroll
-        for (int e = 0; e < COLS; ++e)
-          a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = sum[e] * (ml.y == 0.f ? 0.f : 1.f / ml.y);
+        for (int e = 0; e < COLS; ++e) a.pacc[(at + qw * 32 + i) * a.dl + slice * T::DLW + c0 + e * 64 + lane] = avg[e];
       } else {
-        const float inv = l0 <= l1 ? 1.f / ml.y : 0.f;
 #pragma unroll
         for (int e = 0; e < COLS; ++e)
-          *reinterpret_cast<bf16 *>(smem + (qw * 32 + i) * T::OUT_PITCH + (c0 + e * 64 + lane) * 2) = (bf16)(inv != 0.f ? sum[e] * inv : 0.f);
+          *reinterpret_cast<bf16 *>(smem + (qw * 32 + i) * T::OUT_PITCH + (c0 + e * 64 + lane) * 2) = (bf16)(l0 > l1 ? 0.f : w == 0.f ? NAN : avg[e]);
       }
     }
   } else if (split) {

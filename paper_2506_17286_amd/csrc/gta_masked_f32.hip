@@ -6,8 +6,8 @@
 // layer with a bias 58 us, 69 TFLOP/s of the 153 that a large matrix product reaches; 640 workgroups, two on a CU, and a wave has up
 // to 8 steps between filling its registers and joining its sums.
 //
-// A masked weight is 0, but 0 times a latent that is not finite is NaN: a tile whose sums are not finite in the end is gone through
-// once more, row by row, over the keys that each row sees (wave_row).
+// A masked weight is 0, but 0 times a latent that is not finite is NaN, and sums of finite ones may pass the range: a tile whose sums are not
+// finite in the end is gone through once more, row by row, over the keys that each row sees (wave_row).
 #include <math.h>
 
 #include "gta_rows_attn.h"
@@ -272,14 +272,13 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
       constexpr int COLS = DLW / 64;
       const int tk = (r0 + i) / a.mpc, gg = cell * a.mpc + (r0 + i - tk * a.mpc);
       const int from = max(__shfl(lo, i), b0 * 32), to = min(__shfl(hi, i), min(b1 * 32, keys) - 1);
-      float sum[COLS];
-      const float2 ml = wave_row(a, (const float *)a.q + (start + tk) * a.qs + gg * DH, DH, kcol, ccol, __shfl(slope, i), __shfl(own, i), from, to,
-                                 [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, sum);
+      float avg[COLS];
+      const float w = wave_row(a.rules, (const float *)a.q + (start + tk) * a.qs + gg * DH, DH, kcol, a.ks, ccol, a.cs, __shfl(slope, i), __shfl(own, i),
+                               from, to, [&](int j) { return CACHE ? cache_row_clamped(a.prefix.pm, a.prefix.max_seq, a.prefix_slot, j) : start + j; }, avg);
       float *to_row = split ? a.pacc + (at + i) * a.dl : (float *)a.L + ((start + tk) * a.nq + gg) * (int64_t)a.dl;
-      const float inv = split && ml.y == 0.f ? 0.f : 1.f / ml.y;   // (a piece may have none of the keys that a row sees)
-      const bool any = __shfl(sees ? 1 : 0, i);
+      const bool any = __shfl(sees ? 1 : 0, i), none = w == 0.f && !split;   // (a piece may have none of the keys that a row sees)
 #pragma unroll
-      for (int e = 0; e < COLS; ++e) to_row[slice * DLW + e * 64 + lane] = any ? sum[e] * inv : 0.f;
+      for (int e = 0; e < COLS; ++e) to_row[slice * DLW + e * 64 + lane] = !any ? 0.f : none ? NAN : avg[e];
     }
     return;
   }

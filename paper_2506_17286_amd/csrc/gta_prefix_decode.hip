@@ -119,6 +119,8 @@ __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &
 // a chain of lengths, page, keys, latents and the waves' join.
 // bf16 weights are rounded for the second product, as in the kernel of the prefix, and so is their sum.  (Two parts of 16 bits would
 // cost nothing here, but an infinite latent times the second, which may be 0 or less, is no infinity.)
+// Weights are lowered by a power of two, so that a piece's are at most 1 in all and sums of finite latents stay in their range; what is lost
+// is weights of less than 2^(lift - 126), lift 14 for one tile and 25 for 32768 rows.
 // Rows in front of the first that is seen are cleared in LDS, rows behind the last read as zeros: what is masked has the weight 0, and
 // that times a latent that is not finite would not be.
 template <typename T, int DH, int NF, int NWV>
@@ -227,6 +229,8 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
 #pragma unroll
   for (int f = 0; f < NFR; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
   float m = -INFINITY, l = 0.f;
+  const int lift = (int)kLazy + 1 + 4 + (32 - __builtin_clz(t1 - t0));   // 2^(lift - kLazy) > rows of the piece
+  const float lowered = ldexpf(1.f, -lift);
 
   int t = t0 + wave;
   p0 = find(t);
@@ -282,7 +286,7 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
     m = mn;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - ref);
+      p[e] = __builtin_amdgcn_exp2f(p[e] - ref) * lowered;
       if constexpr (ES == 2) p[e] = (float)(__bf16)p[e];
       l += p[e];
     }
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
     *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v * inv;
-    if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, sum);
+    if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, ldexpf(sum, lift));
   }
 }
 
@@ -396,6 +400,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
   if ((tid & 63) == 0) red[4 + (tid >> 6)] = sum;
   __syncthreads();
   sum = (red[4] + red[5]) + (red[6] + red[7]);
+  const float inv = __builtin_amdgcn_rcpf(sum);   // (something is seen: NaN in the end where all scores are -infinity or one is NaN)
   const int group = tid >> 5, col = blockIdx.z * 128 + (tid & 31) * 4;
   f32x4 v{0.f, 0.f, 0.f, 0.f};
   if (col < j.s.dl) {
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
       if (!(w < 0.f)) {
         const f32x4 p = *reinterpret_cast<const f32x4 *>(from + col);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = fmaf(w, p[e], v[e]);
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(w * inv, p[e], v[e]);   // (averages: a sum of them may pass the range)
       }
     }
   }
@@ -419,9 +424,8 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
   own_rows(j.s, b, slot, n, own, lo, hi);
   seen_by(j.s.rules, b, own, own + 1, lo, hi);
   T *to = (T *)j.l_out + ((int64_t)b * j.s.nq + g) * j.s.dl + col;
-  const float inv = 1.f / sum;   // (sees something: NaN where all scores are -infinity or one is NaN)
 #pragma unroll
-  for (int e = 0; e < 4; ++e) to[e] = (T)(lo <= hi ? v[e] * inv : 0.f);
+  for (int e = 0; e < 4; ++e) to[e] = (T)(lo <= hi ? v[e] : 0.f);
 }
 
 // How own rows are cut: which maps and columns a workgroup has, its waves and their LDS, pieces.

@@ -43,15 +43,17 @@ __device__ __forceinline__ void prefix_seen(const RowsArgs &a, int b, int P, int
   hi = min(hi, P - 1);
 }
 
-// Row `tok`'s map g over keys lo .. hi by one wave, a key a lane for the scores, columns lane, lane + 64, .. of `cols` for the sums;
-// rows(j): pool row of key j.  Returns maximum and weight.
+// One row of queries over keys lo .. hi by one wave, a key a lane for the scores, columns lane, lane + 64, .. for the averages; rows(j): pool
+// row of key j, k and c: the row's key head and columns, rows ks and cs apart.  Returns the row's weight (0: sees none, or scores of
+// -infinity only).  For waves whose sums are not finite: what is not seen is not read, and averages over the keys so far stay in the range
+// of the latents where sums of thousands of large ones do not.
 template <typename T, int COLS, class F>
-__device__ float2 wave_row(const RowsArgs &a, const T *q, int dh, const T *k, const T *c, float slope, int own, int lo, int hi, F rows,
-                           float (&acc)[COLS]) {
+__device__ float wave_row(const Rules &rules, const T *q, int dh, const T *k, int64_t ks, const T *c, int64_t cs, float slope, int own, int lo,
+                           int hi, F rows, float (&avg)[COLS]) {
   const int lane = threadIdx.x & 63;
   float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
+  for (int i = 0; i < COLS; ++i) avg[i] = 0.f;
 #pragma unroll 1
   for (int64_t j0 = lo; j0 <= hi; j0 += 64) {
     const int cnt = (int)min((int64_t)64, hi - j0 + 1);
@@ -59,32 +61,37 @@ __device__ float2 wave_row(const RowsArgs &a, const T *q, int dh, const T *k, co
     int64_t row = 0;
     if (lane < cnt) {
       row = rows((int)j0 + lane);
-      const T *kr = k + row * a.ks;
+      const T *kr = k + row * ks;
       float dot = 0.f;
 #pragma unroll 1
       for (int i = 0; i < dh; ++i) dot = fmaf((float)kr[i], (float)q[i], dot);
-      sc = ruled_score(a.rules, dot, slope, fabsf((float)(own - ((int)j0 + lane))));
+      sc = ruled_score(rules, dot, slope, fabsf((float)(own - ((int)j0 + lane))));
     }
     float mx = sc;
     for (int i = 32; i; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
-    const float mn = fmaxf(m, mx), ref = mn > -INFINITY ? mn : 0.f, corr = __builtin_amdgcn_exp2f(m - ref);
+    const float mn = fmaxf(m, mx), ref = mn > -INFINITY ? mn : 0.f, before = l * __builtin_amdgcn_exp2f(m - ref);
     const float p = lane < cnt ? __builtin_amdgcn_exp2f(sc - ref) : 0.f;
     float sum = p;
     for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
     m = mn;
-    l = fmaf(l, corr, sum);
+    l = before + sum;
+    const float per = l > 0.f ? 1.f / l : 0.f, kept = before * per;
 #pragma unroll
-    for (int i = 0; i < COLS; ++i) acc[i] *= corr;
+    for (int i = 0; i < COLS; ++i) avg[i] *= kept;
 #pragma unroll 1
     for (int t = 0; t < cnt; ++t) {
-      const float pt = __shfl(p, t);
+      const float pt = __shfl(p, t) * per;
       const int64_t at = ((int64_t)__shfl((int)(row >> 32), t) << 32) | (unsigned)__shfl((int)row, t);
-      const T *cr = c + at * a.cs;
+      const T *cr = c + at * cs;
 #pragma unroll
-      for (int i = 0; i < COLS; ++i) acc[i] = fmaf(pt, (float)cr[i * 64 + lane], acc[i]);
+      for (int i = 0; i < COLS; ++i) avg[i] = fmaf(pt, (float)cr[i * 64 + lane], avg[i]);
     }
   }
-  return make_float2(m, l);
+  if (l != l) {   // a score that is NaN
+#pragma unroll
+    for (int i = 0; i < COLS; ++i) avg[i] = l;
+  }
+  return l;
 }
 
 // bf16 (gta_masked_bf16.hip)

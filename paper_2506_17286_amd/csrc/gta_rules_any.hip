@@ -1,5 +1,5 @@
 // Attention with rules on its scores for any shape, stride and alignment: a workgroup per (token, map) walks the keys that the
-// token sees, 256 at a time, a key a thread for the scores and a latent (or several) a thread for the sums.  Every row is read
+// token sees, 256 at a time, a key a thread for the scores and a latent (or several) a thread for the averages.  Every row is read
 // once for every map: the measure of the other kernels, not a fast one.  Bound by the latency of its scalar products: 4 x 4096 tokens of
 // packed documents, 1B shape, 17 ms where the matrix instructions take 87 us.
 #include <algorithm>
@@ -58,20 +58,21 @@ __device__ void attend_row(const Dims &d, const Rules &rules, const T *q, int g,
     for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
     if ((tid & 63) == 0) red2[tid >> 6] = sum;
     __syncthreads();
-    l = l * corr + ((red2[0] + red2[1]) + (red2[2] + red2[3]));
+    const float before = l * corr;
+    l = before + ((red2[0] + red2[1]) + (red2[2] + red2[3]));
     m = mn;
+    const float per = l > 0.f ? 1.f / l : 0.f, kept = before * per;   // averages: sums of large latents would pass the range
     for (int v = 0, col = tid; col < d.dl; ++v, col += 256) {
-      float s = acc[v] * corr;
+      float s = acc[v] * kept;
       for (int r = 0; r < cnt; ++r) {
         const T *cr = j0 + r < cut ? a.c + at[r] * a.cs : b.c + at[r] * b.cs;
-        s = fmaf(ps[r], to_f(cr[ccol + col]), s);
+        s = fmaf(ps[r] * per, to_f(cr[ccol + col]), s);
       }
       acc[v] = s;
     }
     __syncthreads();
   }
-  const float inv = lo <= hi ? 1.f / l : 0.f;
-  for (int v = 0, col = tid; col < d.dl; ++v, col += 256) out[col] = (T)(acc[v] * inv);
+  for (int v = 0, col = tid; col < d.dl; ++v, col += 256) out[col] = (T)(lo > hi ? 0.f : l > 0.f ? acc[v] : NAN);
 }
 
 // The sequence of a packed token: the last b with cu[b] <= t.
