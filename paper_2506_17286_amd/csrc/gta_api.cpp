@@ -561,7 +561,7 @@ int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q
   const uintptr_t el = (uintptr_t)d.esize() - 1;
   if ((((uintptr_t)q | (uintptr_t)k | (uintptr_t)c) & el) || misaligned(l_out) || ((uintptr_t)cu_seqlens & 3u)) return GTA_ERR_ALIGN;
   if (total_tokens == 0 || max_seqlen == 0) return GTA_OK;
-  if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
+  if (!workspace || !workspace_bytes || misaligned(workspace)) return GTA_ERR_WORKSPACE;
   const MaskedArgs m{q, k, c, q_stride, k_stride, c_stride, cu_seqlens, batch, total_tokens, max_seqlen, rules_of(d, rules), l_out};
   if (masked_fits(d, batch, total_tokens)) {
     if (workspace_bytes < masked_bytes(d, batch, total_tokens)) return GTA_ERR_WORKSPACE;
@@ -588,7 +588,7 @@ int gta_prefix_decode_attention(const gta_config *cfg, const void *q, const gta_
   if (misaligned(q) || misaligned(l_out) || ((uintptr_t)slots & 3u)) return GTA_ERR_ALIGN;
   if (!workspace || misaligned(workspace)) return GTA_ERR_WORKSPACE;
   const PrefixArgs p{q, view_of(prefix, nullptr), view_of(cache, slots), prefix_slot, batch, rules_of(d, rules), l_out};
-  if (prefix_fits(d, batch, prefix->max_seq, cache->max_seq)) {
+  if (prefix_fits(d, batch)) {
     if (workspace_bytes < prefix_bytes(d, batch, prefix->max_seq, cache->max_seq)) return GTA_ERR_WORKSPACE;
     if (prefix_layout_ok(*prefix, *cache)) return launch_prefix(d, p, workspace, (hipStream_t)hip_stream);
   }

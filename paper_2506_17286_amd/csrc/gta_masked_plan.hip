@@ -178,11 +178,18 @@ struct MaskedWs {
   size_t bytes;
 };
 
-// least: slots to have room for at least
-MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base, int64_t least = 0) {
+// workgroups of a tile
+int per_tile(const Dims &d) { return d.nq / maps_per_cell(d) * (d.dl / columns(d)); }
+int64_t tiles_at_most(const Dims &d, int batch, int64_t total) { return total * maps_per_cell(d) / tile_rows(d) + batch; }
+
+// What a launch has room for: row numbers of 32 bits, and 2^32 threads (with a last round of eight tiles, and those that are cut)
+constexpr int64_t kMostRows = (int64_t)INT32_MAX - 256;
+int64_t most_tiles(const Dims &d) { return ((1 << 24) - 1) / per_tile(d) - 8 - kAtOnce; }
+
+// tiles: of the batch at most; least: slots to have room for at least
+MaskedWs carve_masked(const Dims &d, int batch, int64_t tiles, void *base, int64_t least = 0) {
   MaskedWs w{};
-  const int mpc = maps_per_cell(d), bq = tile_rows(d), cells = d.nq / mpc, per = cells * (d.dl / columns(d));
-  const int64_t tiles = total * mpc / bq + batch;
+  const int bq = tile_rows(d), cells = d.nq / maps_per_cell(d), per = per_tile(d);
   w.most = tiles * per < kAtOnce ? kAtOnce : 0;
   w.slots = std::max(w.most ? tiles + kAtOnce / per + 1 : 0, least);
   w.capacity = std::max(tiles, w.slots);
@@ -191,7 +198,7 @@ MaskedWs carve_masked(const Dims &d, int batch, int64_t total, void *base, int64
   w.offsets = (int32_t *)take(((size_t)batch + 1) * 4);
   w.count = (int32_t *)take(8);
   w.list = (Piece *)take((size_t)w.capacity * sizeof(Piece));
-  w.cut = (Piece *)take(w.slots ? (size_t)w.capacity * sizeof(Piece) : 0);
+  w.cut = (Piece *)take((size_t)w.slots * sizeof(Piece));   // (a batch that is cut has as many slots as its list has entries)
   w.pml = (float2 *)take((size_t)w.slots * cells * bq * 8);
   w.pacc = (float *)take((size_t)w.slots * cells * bq * d.dl * 4);
   w.bytes = off;
@@ -207,25 +214,27 @@ bool rows_operands_ok(const void *p, int64_t stride, int esize) {
   return !((uintptr_t)p & 15u) && stride * esize % 16 == 0 && stride * esize * 32 < ((int64_t)1 << 31);
 }
 
-// Row numbers of 32 bits and the threads of a launch
 bool masked_fits(const Dims &d, int batch, int64_t total) {
-  if (!masked_tuned(d)) return false;
-  const int mpc = maps_per_cell(d);
-  return total * mpc < INT32_MAX - 256 && (total * mpc / tile_rows(d) + batch + 8 + kAtOnce) * (d.nq / mpc) * (d.dl / columns(d)) < (1 << 24);
+  return masked_tuned(d) && total * maps_per_cell(d) < kMostRows && tiles_at_most(d, batch, total) <= most_tiles(d);
 }
 
-size_t masked_bytes(const Dims &d, int batch, int64_t total) { return masked_fits(d, batch, total) ? carve_masked(d, batch, total, nullptr).bytes : 0; }
+size_t masked_bytes(const Dims &d, int batch, int64_t total) {
+  return masked_fits(d, batch, total) ? carve_masked(d, batch, tiles_at_most(d, batch, total), nullptr).bytes : 0;
+}
 
+// More sequences or tokens than a launch takes: as for the most that it takes.
 size_t masked_bytes_up_to(const Dims &d, int batch, int64_t total) {
-  if (!masked_fits(d, batch, total)) return 0;
-  const MaskedWs w = carve_masked(d, batch, total, nullptr);
+  if (!masked_tuned(d) || most_tiles(d) < 1) return 0;
+  const int64_t tokens = std::min(total, kMostRows / maps_per_cell(d));
+  const int64_t tiles = std::min(tiles_at_most(d, batch, tokens), most_tiles(d));
+  const MaskedWs w = carve_masked(d, batch, tiles, nullptr);
   // the largest batch that is cut has fewer than kAtOnce workgroups
-  const int per = d.nq / maps_per_cell(d) * (d.dl / columns(d));
-  return w.most ? w.bytes : carve_masked(d, batch, total, nullptr, (kAtOnce - 1) / per + kAtOnce / per + 1).bytes;
+  const int per = per_tile(d);
+  return w.most ? w.bytes : carve_masked(d, batch, tiles, nullptr, (kAtOnce - 1) / per + kAtOnce / per + 1).bytes;
 }
 
 int launch_masked(const Dims &d, const MaskedArgs &m, void *ws, hipStream_t st) {
-  const MaskedWs w = carve_masked(d, m.batch, m.total, ws);
+  const MaskedWs w = carve_masked(d, m.batch, tiles_at_most(d, m.batch, m.total), ws);
   RowsArgs a{};
   a.q = m.q; a.k = m.k; a.c = m.c; a.qs = m.q_stride; a.ks = m.k_stride; a.cs = m.c_stride; a.L = m.l_out;
   a.cu = m.cu; a.per_seq = (int)(m.total / m.batch); a.batch = m.batch;

@@ -543,20 +543,22 @@ void launch_stream(const StreamArgs &a, const StreamPlan &p, int groups, hipStre
 static bool pages_ok(const gta_cache &c) { return !c.block_table || (c.page_size >= 16 && !(c.page_size & (c.page_size - 1))); }
 
 bool prefix_tuned(const Dims &d) { return rows_bf16_ok(d) || (rows_f32_ok(d) && d.dh >= 64); }
-bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq) {
-  const int mpc = maps_per_cell(d);
-  return prefix_tuned(d) && (int64_t)batch * mpc < (1 << 24) && d.nq <= 512 && (int64_t)d.wk_w * d.esize() * 32 < (1 << 30) &&
-         (int64_t)d.wc_w * d.esize() * 32 < (1 << 30);
+// sequences that a launch takes
+static int most_sequences(const Dims &d) {
+  const bool any = prefix_tuned(d) && d.nq <= 512 && (int64_t)d.wk_w * d.esize() * 32 < (1 << 30) && (int64_t)d.wc_w * d.esize() * 32 < (1 << 30);
+  return any ? ((1 << 24) - 1) / maps_per_cell(d) : 0;
 }
+bool prefix_fits(const Dims &d, int batch) { return batch <= most_sequences(d); }
 
 size_t prefix_bytes(const Dims &d, int batch, int prefix_max, int max_seq) {
-  if (!prefix_fits(d, batch, prefix_max, max_seq)) return 0;
+  if (!prefix_fits(d, batch)) return 0;
   return carve_prefix(d, batch, prefix_plan(d, batch, prefix_max), stream_plan(d, batch, max_seq), nullptr).bytes;
 }
 
-// What is enough for any batch of up to `batch` sequences: fewer may be cut into more pieces, or into larger tiles' worth of them.
+// What is enough for any batch of up to `batch` sequences (as many of them as a launch takes): fewer may be cut into more pieces, or into larger tiles' worth of them.
 size_t prefix_bytes_up_to(const Dims &d, int batch, int prefix_max, int max_seq) {
-  if (!prefix_fits(d, batch, prefix_max, max_seq)) return 0;
+  batch = std::min(batch, most_sequences(d));
+  if (!batch) return 0;
   const int mpc = maps_per_cell(d);
   size_t prows = 0;
   for (int rows : {32, 64, INT_MAX}) {   // where prefix_tile_rows changes

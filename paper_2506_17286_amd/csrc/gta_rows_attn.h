@@ -117,7 +117,7 @@ void launch_prefix_rows(const Dims &d, const RowsArgs &a, int bq, hipStream_t st
 
 // gta_prefix_decode.hip
 bool prefix_tuned(const Dims &d);   // with pages of a power of two of at least 16 rows
-bool prefix_fits(const Dims &d, int batch, int prefix_max, int max_seq);
+bool prefix_fits(const Dims &d, int batch);
 bool prefix_layout_ok(const gta_cache &prefix, const gta_cache &own);
 size_t prefix_bytes(const Dims &d, int batch, int prefix_max, int max_seq);
 size_t prefix_bytes_up_to(const Dims &d, int batch, int prefix_max, int max_seq);
