@@ -301,18 +301,20 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
 }
 
 template <int DH, int DLW>
-void launch_of(const RowsArgs &a, bool cache, hipStream_t st) {
+bool launch_of(const RowsArgs &a, bool cache, hipStream_t st) {
   constexpr int LDS = 4 * 32 * (DLW + 4) * 4;
   const unsigned grid = (unsigned)((int64_t)a.tiles * a.cells * a.slices);
-  if (cache) {
-    if constexpr (DH >= 64) {   // (what prefix_tuned lets through)
-    allow_dynamic_lds((const void *)rows_attn_f32_kernel<DH, DLW, true>, LDS);
-    rows_attn_f32_kernel<DH, DLW, true><<<grid, 256, LDS, st>>>(a);
-    }
-  } else {
+  if (!cache) {
     allow_dynamic_lds((const void *)rows_attn_f32_kernel<DH, DLW, false>, LDS);
     rows_attn_f32_kernel<DH, DLW, false><<<grid, 256, LDS, st>>>(a);
+    return true;
   }
+  if constexpr (DH >= 64) {   // (what prefix_tuned lets through)
+    allow_dynamic_lds((const void *)rows_attn_f32_kernel<DH, DLW, true>, LDS);
+    rows_attn_f32_kernel<DH, DLW, true><<<grid, 256, LDS, st>>>(a);
+    return true;
+  }
+  return false;
 }
 
 }  // namespace
@@ -320,13 +322,13 @@ void launch_of(const RowsArgs &a, bool cache, hipStream_t st) {
 bool rows_f32_ok(const Dims &d) { return d.dtype == GTA_F32 && (d.dh == 32 || d.dh == 64 || d.dh == 128) && d.dl % 64 == 0; }
 int rows_f32_columns(const Dims &d) { return d.dl % 128 == 0 ? 128 : 64; }
 
-void launch_rows_f32(const Dims &d, const RowsArgs &args, bool cache, hipStream_t st) {
+bool launch_rows_f32(const Dims &d, const RowsArgs &args, bool cache, hipStream_t st) {
   RowsArgs a = args;
   const bool wide = rows_f32_columns(d) == 128;
   a.slices = d.dl / rows_f32_columns(d);
-  if (d.dh == 32) { if (wide) launch_of<32, 128>(a, cache, st); else launch_of<32, 64>(a, cache, st); }
-  else if (d.dh == 64) { if (wide) launch_of<64, 128>(a, cache, st); else launch_of<64, 64>(a, cache, st); }
-  else { if (wide) launch_of<128, 128>(a, cache, st); else launch_of<128, 64>(a, cache, st); }
+  if (d.dh == 32) return wide ? launch_of<32, 128>(a, cache, st) : launch_of<32, 64>(a, cache, st);
+  if (d.dh == 64) return wide ? launch_of<64, 128>(a, cache, st) : launch_of<64, 64>(a, cache, st);
+  return wide ? launch_of<128, 128>(a, cache, st) : launch_of<128, 64>(a, cache, st);
 }
 
 }  // namespace gta

@@ -505,35 +505,38 @@ PrefixWs carve_prefix(const Dims &d, int batch, const PrefixPlan &p, const Strea
   return carve_prefix(d, batch, (size_t)p.tiles * p.pieces * p.cells * p.bq, (size_t)s.grid, base);
 }
 
+// (false: nothing was launched)
 template <typename T, int DH, int NF>
-void launch_stream_of(const StreamArgs &a, const StreamPlan &p, unsigned y, hipStream_t st) {
+bool launch_stream_of(const StreamArgs &a, const StreamPlan &p, unsigned y, hipStream_t st) {
   auto run = [&](auto kernel) {
     allow_dynamic_lds((const void *)kernel, p.waves * p.wave_lds);
     kernel<<<dim3((unsigned)p.grid, y), p.waves * 64, p.waves * p.wave_lds, st>>>(a);
+    return true;
   };
   // what stream_plan comes to: one key head leaves room for four waves but in fp32 rows of 128 + 512, sixteen may take it
   constexpr int LEAST = 16 * (DH + NF * 64) * (int)sizeof(T), MOST = std::min(16 * (16 * DH + NF * 64) * (int)sizeof(T), 65536);
   if constexpr (LEAST <= kFour) {
-    if (p.waves == 4) run(stream_kernel<T, DH, NF, 4>);
+    if (p.waves == 4) return run(stream_kernel<T, DH, NF, 4>);
   }
   if constexpr (MOST > kFour) {
-    if (p.waves == 3) run(stream_kernel<T, DH, NF, 3>);
+    if (p.waves == 3) return run(stream_kernel<T, DH, NF, 3>);
   }
   if constexpr (MOST > kThree) {
-    if (p.waves == 2) run(stream_kernel<T, DH, NF, 2>);
+    if (p.waves == 2) return run(stream_kernel<T, DH, NF, 2>);
   }
+  return false;
 }
 
 template <typename T, int DH>
-void launch_stream(const StreamArgs &a, const StreamPlan &p, int groups, hipStream_t st) {
+bool launch_stream(const StreamArgs &a, const StreamPlan &p, int groups, hipStream_t st) {
   const unsigned y = (unsigned)(a.dl / (p.nf * 64) * p.blocks * groups);
   switch (p.nf) {
     case 1:
-      if constexpr (DH == 64 || sizeof(T) == 4) launch_stream_of<T, DH, 1>(a, p, y, st);   // bf16 heads of 128 have latents in units of 128
-      break;
-    case 2: launch_stream_of<T, DH, 2>(a, p, y, st); break;
-    case 4: launch_stream_of<T, DH, 4>(a, p, y, st); break;
-    default: launch_stream_of<T, DH, 8>(a, p, y, st);
+      if constexpr (DH == 64 || sizeof(T) == 4) return launch_stream_of<T, DH, 1>(a, p, y, st);   // bf16 heads of 128 have latents in units of 128
+      return false;
+    case 2: return launch_stream_of<T, DH, 2>(a, p, y, st);
+    case 4: return launch_stream_of<T, DH, 4>(a, p, y, st);
+    default: return launch_stream_of<T, DH, 8>(a, p, y, st);
   }
 }
 
@@ -591,18 +594,15 @@ int launch_prefix(const Dims &d, const PrefixArgs &x, void *ws, hipStream_t st) 
   r.tiles = p.tiles * p.pieces; r.pacc = w.pacc; r.pml = w.pml; r.prefix = x.prefix; r.own = x.own; r.prefix_slot = x.prefix_slot;
   r.pieces = p.pieces; r.ps_shift = shift_of(x.prefix.pm);
   if (d.dtype == GTA_BF16) launch_prefix_rows(d, r, p.bq, st);
-  else launch_rows_f32(d, r, true, st);
+  else if (!launch_rows_f32(d, r, true, st)) return GTA_ERR_UNSUPPORTED;
   StreamArgs a{};
   a.q = x.q; a.prefix = x.prefix; a.own = x.own; a.prefix_slot = x.prefix_slot; a.batch = x.batch; a.nq = d.nq; a.qpk = d.qpk; a.qpc = d.qpc;
   a.dl = d.dl; a.kw = d.wk_w; a.cw = d.wc_w; a.rules = x.rules; a.maps = s.maps; a.blocks = s.blocks; a.heads = s.heads;
   a.wave_lds = s.wave_lds; a.ps_shift = shift_of(x.own.pm); a.share = s.share; a.each = s.each; a.first = w.first; a.pacc = w.oacc; a.pml = w.oml;
-  if (d.dtype == GTA_BF16) {
-    if (d.dh == 64) launch_stream<__bf16, 64>(a, s, d.nc, st);
-    else launch_stream<__bf16, 128>(a, s, d.nc, st);
-  } else {
-    if (d.dh == 64) launch_stream<float, 64>(a, s, d.nc, st);
-    else launch_stream<float, 128>(a, s, d.nc, st);
-  }
+  bool streamed;
+  if (d.dtype == GTA_BF16) streamed = d.dh == 64 ? launch_stream<__bf16, 64>(a, s, d.nc, st) : launch_stream<__bf16, 128>(a, s, d.nc, st);
+  else streamed = d.dh == 64 ? launch_stream<float, 64>(a, s, d.nc, st) : launch_stream<float, 128>(a, s, d.nc, st);
+  if (!streamed) return GTA_ERR_UNSUPPORTED;   // the join would read piece counts that nobody has written
   const JoinArgs j{a, r, p.bq, x.l_out};
   const dim3 grid((unsigned)x.batch, (unsigned)d.nq, (unsigned)((d.dl + 127) / 128));
   if (d.dtype == GTA_BF16) prefix_join_kernel<__bf16><<<grid, 256, 0, st>>>(j);

@@ -101,7 +101,7 @@ void launch_masked_bf16(const Dims &d, const RowsArgs &a, hipStream_t st);
 // fp32 (gta_masked_f32.hip): rows of 32 per tile
 bool rows_f32_ok(const Dims &d);
 int rows_f32_columns(const Dims &d);
-void launch_rows_f32(const Dims &d, const RowsArgs &a, bool cache, hipStream_t st);
+bool launch_rows_f32(const Dims &d, const RowsArgs &a, bool cache, hipStream_t st);   // false: nothing was launched
 // either (gta_masked_plan.hip)
 bool masked_tuned(const Dims &d);
 bool masked_fits(const Dims &d, int batch, int64_t total);
