@@ -548,7 +548,7 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
     });
   }
   if (split) {   // whether the wave went through its rows again or not
-    if (h == 0 && slice == 0 && cg == 0 && wr0 + ln < R) a.pml[at + my] = sees ? make_float2(m_run, l_all) : make_float2(-INFINITY, 0.f);
+    if (h == 0 && slice == 0 && cg == 0 && wr0 + ln < R) a.pml[at + my] = sees ? make_float2(m_run, l_all) : make_float2(-INFINITY, -1.f);
     return;
   }
   __syncthreads();

@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256, DH + DLW < 256 || !CACHE ? 2 : 1) void rows_at
   if (split && slice == 0 && tid < BQ && r0 + tid < R) {   // (the first wave has the first 32 rows in its lanes)
     float top;
     const float sum = weight_of(tid, top);
-    a.pml[at + tid] = sees ? make_float2(top, sum) : make_float2(-INFINITY, 0.f);
+    a.pml[at + tid] = sees ? make_float2(top, sum) : make_float2(-INFINITY, -1.f);
   }
   if (__builtin_expect(again, 0)) {
 #pragma unroll 1

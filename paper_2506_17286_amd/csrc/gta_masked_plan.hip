@@ -142,7 +142,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
   float l = 0.f;
   for (int i = 0; i < p.pieces; ++i) {
     const float2 ml = a.pml[at(i)];
-    if (ml.y != 0.f) l = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, l);
+    if (!(ml.y < 0.f)) l = fmaf(__builtin_amdgcn_exp2f(ml.x - ref), ml.y, l);
   }
   int lo, hi;
   seen_by(a.rules, start + tk, tk, R / a.mpc, lo, hi);
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(256) void join_pieces_kernel(RowsArgs a, const Piec
     float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int i = 0; i < p.pieces; ++i) {
       const float2 ml = a.pml[at(i)];
-      if (ml.y == 0.f) continue;   // sees none of the piece's keys
+      if (ml.y < 0.f) continue;
       const float w = __builtin_amdgcn_exp2f(ml.x - ref) * ml.y * inv;
       const float4 s = *reinterpret_cast<const float4 *>(a.pacc + at(i) * a.dl + col);
       v.x = fmaf(w, s.x, v.x); v.y = fmaf(w, s.y, v.y); v.z = fmaf(w, s.z, v.z); v.w = fmaf(w, s.w, v.w);

@@ -166,7 +166,7 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
   const int t_lo = lo >> 4, tiles = hi < lo ? 0 : (hi >> 4) - t_lo + 1;
   const int t0 = t_lo + (int)((int64_t)tiles * piece / pieces), t1 = t_lo + (int)((int64_t)tiles * (piece + 1) / pieces);
   if (t0 >= t1) {
-    if (slice == 0 && tid < gn) a.pml[at + tid] = make_float2(-INFINITY, 0.f);
+    if (slice == 0 && tid < gn) a.pml[at + tid] = make_float2(-INFINITY, -1.f);
     return;
   }
   const int g = min(g0 + x, g0 + gn - 1), head = g / a.qpk - kh0;   // this lane's map (lanes without one repeat the last)
@@ -337,7 +337,6 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
 #pragma unroll
     for (int w = 0; w < NWV; ++w) {
       const float2 ml = stats[w][map];
-      if (ml.y == 0.f) continue;
       const float wt = ml.y != ml.y ? ml.y : __builtin_amdgcn_exp2f(ml.x - ref);
       const f32x4 c = *reinterpret_cast<const f32x4 *>(smem + w * a.wave_lds + map * (SW * 4) + (col ^ (map & 7) * 4) * 4);
 #pragma unroll
@@ -376,7 +375,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
 #pragma unroll
   for (int v = 0; v < kMaxPieces / 256; ++v) {
     const int i = v * 256 + tid;
-    ml[v] = make_float2(-INFINITY, 0.f);
+    ml[v] = make_float2(-INFINITY, -1.f);
     if (i < all) ml[v] = i < S ? j.r.pml[shared_at(i)] : j.s.pml[own_at(i - S)];
     mx = fmaxf(mx, ml[v].x);
   }
@@ -391,7 +390,7 @@ __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
     const int i = v * 256 + tid;
     // a piece that sees nothing has left no averages (weight -1); one of weight 0 takes part: its averages may not be finite.  NaN scores
     // have a weight that is NaN and no maximum
-    const bool none = ml[v].y == 0.f;
+    const bool none = ml[v].y < 0.f;
     const float w = ml[v].y != ml[v].y ? ml[v].y : none ? -1.f : __builtin_amdgcn_exp2f(ml[v].x - ref) * ml[v].y;
     if (i < all) weight[i] = w;
     if (!none) sum += w;

@@ -5,6 +5,8 @@
 // pieces, which leave fp32 averages over their keys, and per row a maximum m (in units of log 2) and a weight l, in a slot of scratch
 // memory: the piece counts as l 2^m.  Averages do not depend on what their weights referred to, so that whichever workgroup or wave of a row's
 // columns goes through its keys again (wave_row) leaves what the row's one (m, l) fits.
+// Keys whose scores are -infinity have the weight 0 and take part with it, as what they hold may not be finite; l = -1 marks a row without
+// averages.
 #pragma once
 #include <algorithm>
 
