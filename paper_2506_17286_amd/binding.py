@@ -208,7 +208,8 @@ def make_weights(w: Dict[str, "object"]) -> gta_weights:
 
 def _known(cache: gta_cache, k, c) -> gta_cache:
     """Notes what the arrays are, for the calls that look at it."""
-    cache.device, cache.dtype, cache.widths = k.get_device(), k.dtype, tuple(t.shape[2:].numel() for t in (k, c))
+    if c is not None:
+        cache.device, cache.dtype, cache.widths = k.get_device(), k.dtype, tuple(t.shape[2:].numel() for t in (k, c))
     return cache
 
 
