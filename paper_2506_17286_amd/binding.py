@@ -206,16 +206,27 @@ def make_weights(w: Dict[str, "object"]) -> gta_weights:
     return gta_weights(_ptr(w["wq"]), _ptr(w["wk"]), _ptr(w["wc"]), _ptr(w["wg"]), _ptr(w["wp"]), _ptr(w.get("wo")))
 
 
-def _known(cache: gta_cache, k, c) -> gta_cache:
-    """Notes what the arrays are, for the calls that look at it."""
-    if c is not None:
-        cache.device, cache.dtype, cache.widths = k.get_device(), k.dtype, tuple(t.shape[2:].numel() for t in (k, c))
+def _known(cache: gta_cache, k, c, seq_lens, table=None) -> gta_cache:
+    """Notes what the arrays are, and what about them the kernels would read past the end of or as something else, for the calls that
+    look at it."""
+    import torch
+    if c is None or seq_lens is None:
+        return cache
+    cache.device, cache.dtype, cache.widths = k.get_device(), k.dtype, tuple(t.shape[2:].numel() for t in (k, c))
+    cache.unfit = None
+    for name, t, kind in (("k", k, k.dtype), ("c", c, k.dtype), ("seq_lens", seq_lens, torch.int32), ("block_table", table, torch.int32)):
+        if t is not None and (t.dtype != kind or not t.is_contiguous() or t.device != k.device):
+            cache.unfit = f"{name} is {t.dtype}, {'' if t.is_contiguous() else 'not '}contiguous, on {t.device}; k is {k.dtype} on {k.device}"
+    if c.shape[:2] != k.shape[:2]:
+        cache.unfit = f"c {tuple(c.shape)} next to k {tuple(k.shape)}"
+    if seq_lens.numel() < cache.max_batch:
+        cache.unfit = f"seq_lens has {seq_lens.numel()} entries for {cache.max_batch} slots"
     return cache
 
 
 def make_cache(k, c, seq_lens, status) -> gta_cache:
     """k [slots, max_seq, n_k*d_h], c [slots, max_seq, n_c*d_l], seq_lens/status int32 [slots] (device)."""
-    return _known(gta_cache(_ptr(k), _ptr(c), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1]), k, c)
+    return _known(gta_cache(_ptr(k), _ptr(c), _ptr(seq_lens), _ptr(status), k.shape[0], k.shape[1]), k, c, seq_lens)
 
 
 def make_paged_cache(k_pool, c_pool, seq_lens, status, block_table) -> gta_cache:
@@ -223,7 +234,7 @@ def make_paged_cache(k_pool, c_pool, seq_lens, status, block_table) -> gta_cache
     [slots, pages_per_slot] (device): row p of slot s is row p % page_size of page block_table[s, p // page_size]."""
     slots, pps = block_table.shape
     return _known(gta_cache(_ptr(k_pool), _ptr(c_pool), _ptr(seq_lens), _ptr(status), slots, pps * k_pool.shape[1],
-                            _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0]), k_pool, c_pool)
+                            _ptr(block_table), k_pool.shape[1], pps, k_pool.shape[0]), k_pool, c_pool, seq_lens, block_table)
 
 
 def _mx_cache(k, c, k_scale, c_scale, seq_lens, status, slots: int, max_seq: int, table=None) -> gta_mx_cache:
@@ -325,10 +336,12 @@ def _rules(device: int, cfg: gta_config, rules: Optional[gta_score_rules], token
 
 
 def _rows_of(device: int, cfg: gta_config, cache: Optional[gta_cache]):
-    """The cache as the library takes it, if it is on the current device and has the widths and the type of cfg (one whose fields the
-    caller filled in is taken as it is)."""
+    """The cache as the library takes it, if it is on the current device, has the widths and the type of cfg and arrays that belong
+    together (one whose fields the caller filled in is taken as it is)."""
     if cache is None:
         return None
+    if getattr(cache, "unfit", None):
+        raise ValueError(f"cache: {cache.unfit}")
     if getattr(cache, "device", device) != device:
         raise ValueError(f"cache on {'cpu' if cache.device < 0 else f'cuda:{cache.device}'}, current device is cuda:{device}")
     widths = (cfg.n_kgroups * cfg.head_dim, cfg.n_cgroups * cfg.latent_dim)
