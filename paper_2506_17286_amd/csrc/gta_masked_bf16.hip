@@ -124,7 +124,6 @@ __global__ __launch_bounds__(256, T::BLOCKS) void rows_attn_kernel(RowsArgs a) {
   } else {
     const int per_level = a.batch, lvl = u / per_level;
     b = u - lvl * per_level; tile = a.tiles / a.batch - 1 - lvl;
-    if (tile < 0) return;
   }
   const int slice = r % a.slices, cell = r / a.slices;
   int64_t start = 0;

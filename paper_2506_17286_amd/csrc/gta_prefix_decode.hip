@@ -186,7 +186,8 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
   const unsigned clane = clr * cws, cchunk = (CCH < 64 ? lane % CCH : lane) ^ (ES == 2 ? (clr & PM) * 2 : 0);
   char *mem = smem + wave * a.wave_lds;
   const unsigned klds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)mem, clds = klds + a.heads * KI * 1024;
-  const char *kmem = mem, *cmem = mem + a.heads * KI * 1024;
+  const char *kmem = mem;
+  char *cmem = mem + a.heads * KI * 1024;
   int64_t p0 = 0;   // pool row of the tile in work on
   auto find = [&](int t) {   // its 16 rows lie in one page
     const int j = min(t * 16, hi & ~15);
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
     }
     wait_loads(heads * KI);                                      // the latents are there
     if (j0 < lo) {   // clear what is in front of the first row
-      for (int i = lane; i < (lo - j0) * CCH; i += 64) *reinterpret_cast<u32x4 *>(mem + (cmem - mem) + i * 16) = u32x4{0u, 0u, 0u, 0u};
+      for (int i = lane; i < (lo - j0) * CCH; i += 64) *reinterpret_cast<u32x4 *>(cmem + i * 16) = u32x4{0u, 0u, 0u, 0u};
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     }
     if constexpr (ES == 2) {
