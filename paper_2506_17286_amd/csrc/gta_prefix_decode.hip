@@ -119,8 +119,9 @@ __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &
 // a chain of lengths, page, keys, latents and the waves' join.
 // bf16 weights are rounded for the second product, as in the kernel of the prefix, and so is their sum.  (Two parts of 16 bits would
 // cost nothing here, but an infinite latent times the second, which may be 0 or less, is no infinity.)
-// Weights are lowered by a power of two, so that a piece's are at most 1 in all and sums of finite latents stay in their range; what is lost
-// is weights of less than 2^(lift - 126), lift 14 for one tile and 25 for 32768 rows.
+// Sums of finite latents may pass the range: a workgroup whose averages are not finite in the end goes through its tiles once more, with
+// weights that are lowered by a power of two so that they are at most 1 in all.  (Lowered from the start, they lose what large latents of
+// little weight count: those below 2^(lift - 126), lift 25 for 32768 rows.)
 // Rows in front of the first that is seen are cleared in LDS, rows behind the last read as zeros: what is masked has the weight 0, and
 // that times a latent that is not finite would not be.
 template <typename T, int DH, int NF, int NWV>
@@ -229,124 +230,134 @@ __global__ __launch_bounds__(NWV * 64, NF >= 8 ? 1 : 2) void stream_kernel(Strea
   f32x4 acc[NFR];
 #pragma unroll
   for (int f = 0; f < NFR; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
-  const int lift = (int)kLazy + 1 + 4 + (32 - __builtin_clz(t1 - t0));   // 2^(lift - kLazy) > rows of the piece
-  const float lowered = ldexpf(1.f, -lift);
-
-  int t = t0 + wave;
-  p0 = find(t);
-  issue_k(t);
-  issue_c(t);
+  float m = -INFINITY, l = 0.f, lift = 0.f;   // lift: by how many powers of two weights are lowered
+  while (true) {
+    int t = t0 + wave;
+    p0 = find(t);
+    issue_k(t);
+    issue_c(t);
 #pragma unroll 1
-  for (; t < t1; t += NWV) {
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CI) : "memory");   // the keys are there
-    f32x4 s{0.f, 0.f, 0.f, 0.f};
+    for (; t < t1; t += NWV) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(CI) : "memory");   // the keys are there
+      f32x4 s{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
-    for (int kk = 0; kk < heads; ++kk) {
-      const char *kr = kmem + kk * KI * 1024 + x * KCH * 16;
-      f32x4 d{0.f, 0.f, 0.f, 0.f}, kf[KS], part[3];   // fp32: four sums of a quarter of the products each, off by half as much as one
-      if constexpr (ES == 4) part[0] = part[1] = part[2] = d;
+      for (int kk = 0; kk < heads; ++kk) {
+        const char *kr = kmem + kk * KI * 1024 + x * KCH * 16;
+        f32x4 d{0.f, 0.f, 0.f, 0.f}, kf[KS], part[3];   // fp32: four sums of a quarter of the products each, off by half as much as one
+        if constexpr (ES == 4) part[0] = part[1] = part[2] = d;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const f32x4 *>(kr + ((ks * 4 + h) ^ (x & 7)) * 16);
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = *reinterpret_cast<const f32x4 *>(kr + ((ks * 4 + h) ^ (x & 7)) * 16);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if constexpr (ES == 2) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[ks]), __builtin_bit_cast(bf16x8, qf[ks]), d, 0, 0, 0);
-        else {
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (ES == 2) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[ks]), __builtin_bit_cast(bf16x8, qf[ks]), d, 0, 0, 0);
+          else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f32x4 &to = e == 0 ? d : part[e - 1];
-            to = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[ks][e], qf[ks][e], to, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) {
+              f32x4 &to = e == 0 ? d : part[e - 1];
+              to = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[ks][e], qf[ks][e], to, 0, 0, 0);
+            }
           }
         }
+        if constexpr (ES == 4) d = (d + part[0]) + (part[1] + part[2]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] = head == kk ? d[e] : s[e];
       }
-      if constexpr (ES == 4) d = (d + part[0]) + (part[1] + part[2]);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // and have been read
+      p0 = find(t + NWV);
+      issue_k(t + NWV);
+      const int j0 = t * 16;
+      float p[4], mt = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[e] = head == kk ? d[e] : s[e];
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");          // and have been read
-    p0 = find(t + NWV);
-    issue_k(t + NWV);
-    const int j0 = t * 16;
-    float p[4], mt = -INFINITY;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = j0 + 4 * h + e;
-      const float v = ruled_score(a.rules, s[e], slope, (float)(n - 1 - j));
-      p[e] = j >= lo && j <= hi ? v : -INFINITY;
-      mt = fmaxf(mt, p[e]);
-    }
-    mt = fmaxf(mt, __shfl_xor(mt, 16));
-    mt = fmaxf(mt, __shfl_xor(mt, 32));
-    const float mn = mt > m + kLazy ? mt : m, ref = mn > -INFINITY ? mn : 0.f;
-    const float corr = __builtin_amdgcn_exp2f(m - ref);
-    if (__builtin_amdgcn_ballot_w64(mn != m) != 0) {
-      l *= corr;
-#pragma unroll
-      for (int f = 0; f < NFR; ++f) acc[f] *= corr;
-    }
-    m = mn;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = __builtin_amdgcn_exp2f(p[e] - ref) * lowered;
-      if constexpr (ES == 2) p[e] = (float)(__bf16)p[e];
-      l += p[e];
-    }
-    wait_loads(heads * KI);                                      // the latents are there
-    if (j0 < lo) {   // clear what is in front of the first row
-      for (int i = lane; i < (lo - j0) * CCH; i += 64) *reinterpret_cast<u32x4 *>(cmem + i * 16) = u32x4{0u, 0u, 0u, 0u};
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    if constexpr (ES == 2) {
-      bf16x4 p1;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p1[e] = (__bf16)p[e];
-      const int row = 4 * h + (x >> 2);
-      const char *cr = cmem + row * CP + (x & 1) * 8 + (x >> 1 & 1) * 16;
-#pragma unroll
-      for (int f = 0; f < NFR; ++f) {   // 16 columns are a pair of chunks
-        const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cr + (f ^ (row & PM)) * 32));
-        acc[f] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(c, __builtin_bit_cast(s16x4, p1), acc[f], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        const int j = j0 + 4 * h + e;
+        const float v = ruled_score(a.rules, s[e], slope, (float)(n - 1 - j));
+        p[e] = j >= lo && j <= hi ? v : -INFINITY;
+        mt = fmaxf(mt, p[e]);
       }
-    } else {
+      mt = fmaxf(mt, __shfl_xor(mt, 16));
+      mt = fmaxf(mt, __shfl_xor(mt, 32));
+      const float mn = mt > m + kLazy ? mt : m, ref = mn > -INFINITY ? mn : 0.f;
+      const float corr = __builtin_amdgcn_exp2f(m - ref);
+      if (__builtin_amdgcn_ballot_w64(mn != m) != 0) {
+        l *= corr;
 #pragma unroll
-      for (int f = 0; f < NFR; ++f)     // and a block of 64 bytes
+        for (int f = 0; f < NFR; ++f) acc[f] *= corr;
+      }
+      m = mn;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float c = *reinterpret_cast<const float *>(cmem + (4 * h + e) * CP + (f ^ h) * 64 + x * 4);
-          acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(c, p[e], acc[f], 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        p[e] = __builtin_amdgcn_exp2f(p[e] - (ref + lift));
+        if constexpr (ES == 2) p[e] = (float)(__bf16)p[e];
+        l += p[e];
+      }
+      wait_loads(heads * KI);                                      // the latents are there
+      if (j0 < lo) {   // clear what is in front of the first row
+        for (int i = lane; i < (lo - j0) * CCH; i += 64) *reinterpret_cast<u32x4 *>(cmem + i * 16) = u32x4{0u, 0u, 0u, 0u};
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
+      if constexpr (ES == 2) {
+        bf16x4 p1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p1[e] = (__bf16)p[e];
+        const int row = 4 * h + (x >> 2);
+        const char *cr = cmem + row * CP + (x & 1) * 8 + (x >> 1 & 1) * 16;
+#pragma unroll
+        for (int f = 0; f < NFR; ++f) {   // 16 columns are a pair of chunks
+          const s16x4 c = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(cr + (f ^ (row & PM)) * 32));
+          acc[f] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(c, __builtin_bit_cast(s16x4, p1), acc[f], 0, 0, 0);
         }
+      } else {
+#pragma unroll
+        for (int f = 0; f < NFR; ++f)     // and a block of 64 bytes
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float c = *reinterpret_cast<const float *>(cmem + (4 * h + e) * CP + (f ^ h) * 64 + x * 4);
+            acc[f] = __builtin_amdgcn_mfma_f32_16x16x4f32(c, p[e], acc[f], 0, 0, 0);
+          }
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      issue_c(t + NWV);
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    issue_c(t + NWV);
-  }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
-  // join the waves' sums: [map][column] in each one's LDS
-  if (h == 0) stats[wave][x] = make_float2(m, l);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no load may land in what follows
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    int id0 = tid;
+    asm volatile("" : "+v"(id0));   // (addresses of what follows are worked out here and not kept through the tiles)
+    // join the waves' sums: [map][column] in each one's LDS
+    const int xo = id0 & 15, ho = id0 >> 4 & 3;
+    if (ho == 0) stats[wave][xo] = make_float2(m + lift, l);
 #pragma unroll
-  for (int f = 0; f < NFR; ++f) *reinterpret_cast<f32x4 *>(mem + x * (SW * 4) + ((f * 16 + 4 * h) ^ (x & 7) * 4) * 4) = acc[f];
-  __syncthreads();
-  for (int i = tid; i < gn * (SW / 4); i += NWV * 64) {
-    const int map = i / (SW / 4), col = i % (SW / 4) * 4;
-    float mx = -INFINITY;
+    for (int f = 0; f < NFR; ++f) *reinterpret_cast<f32x4 *>(mem + xo * (SW * 4) + ((f * 16 + 4 * ho) ^ (xo & 7) * 4) * 4) = acc[f];
+    __syncthreads();
+    bool odd = false;   // an average is not finite
+    for (int i = id0; i < gn * (SW / 4); i += NWV * 64) {
+      const int map = i / (SW / 4), col = i % (SW / 4) * 4;
+      float mx = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < NWV; ++w) mx = fmaxf(mx, stats[w][map].x);
-    const float ref = mx > -INFINITY ? mx : 0.f;
-    f32x4 v{0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
+      for (int w = 0; w < NWV; ++w) mx = fmaxf(mx, stats[w][map].x);
+      const float ref = mx > -INFINITY ? mx : 0.f;
+      f32x4 v{0.f, 0.f, 0.f, 0.f};
+      float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < NWV; ++w) {
-      const float2 ml = stats[w][map];
-      const float wt = ml.y != ml.y ? ml.y : __builtin_amdgcn_exp2f(ml.x - ref);
-      const f32x4 c = *reinterpret_cast<const f32x4 *>(smem + w * a.wave_lds + map * (SW * 4) + (col ^ (map & 7) * 4) * 4);
+      for (int w = 0; w < NWV; ++w) {
+        const float2 ml = stats[w][map];
+        const float wt = ml.y != ml.y ? ml.y : __builtin_amdgcn_exp2f(ml.x - ref);
+        const f32x4 c = *reinterpret_cast<const f32x4 *>(smem + w * a.wave_lds + map * (SW * 4) + (col ^ (map & 7) * 4) * 4);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, c[e], v[e]);
-      sum = fmaf(wt, ml.y, sum);
+        for (int e = 0; e < 4; ++e) v[e] = fmaf(wt, c[e], v[e]);
+        sum = fmaf(wt, ml.y, sum);
+      }
+      const float inv = sum == 0.f ? 0.f : ES == 4 ? 1.f / sum : __builtin_amdgcn_rcpf(sum);
+      *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v * inv;
+      if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, sum);
+      odd |= (v[0] * 0.f + v[1] * 0.f) + (v[2] * 0.f + v[3] * 0.f) != 0.f;
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    *reinterpret_cast<f32x4 *>(a.pacc + (at + map) * a.dl + slice * SW + col) = v * inv;
-    if (slice == 0 && col == 0) a.pml[at + map] = make_float2(mx, ldexpf(sum, lift));
+    if (__builtin_expect(!__syncthreads_or(odd) || lift > 0.f, 1)) return;
+    lift = kLazy + 5.f + (float)(32 - __builtin_clz(t1 - t0));   // 2^(lift - kLazy) > 16 (t1 - t0): the waves' sums together are below the largest latent
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int f = 0; f < NFR; ++f) acc[f] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 }
 

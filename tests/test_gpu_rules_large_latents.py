@@ -65,3 +65,38 @@ def test_prefixes(name, page, dtype, signs):
         P.run(name, dtype, 1500, [1, 600, 0, 17], edit=edit, seed=74, page=page, room=1280 if page == 5 else None, prefix_room=1600 if page == 5 else None)
         P.run(name, dtype, 9, [1300, 2], edit=edit, seed=75, page=page, room=1600 if page == 5 else None, prefix_room=unit, cap=30.0)
         P.run(name, dtype, 700, [20 + i for i in range(70)], edit=edit, seed=76, room=320 if page == 5 else None, prefix_room=960 if page == 5 else None, page=page)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", ["paper", "1b", "wide", "l192", "odd"])
+@pytest.mark.parametrize("where", ["prompt", "prefix", "own"])
+def test_large_latents_of_small_weights(name, dtype, where):
+    """A latent of 1e38 with a weight of e^-78 = 2^-112.5 (and its neighbour of 1e37) counts for thousands of others."""
+    dh = R.SHAPES[name]["head_dim"]
+
+    def keys(k, c, row):
+        k[:, :] = 0.0
+        k[row, ::dh] = -78.0 * dh ** 0.5      # times a query of 1, over the root of the head: -78
+        c[row] = 1e38
+        c[row, 1::2] = -1e37
+
+    def queries(q):
+        q[:, :] = 0.0
+        q[:, ::dh] = 1.0
+    if where == "prompt":
+        def edit(q, k, c, lo, hi):
+            queries(q)
+            keys(k, c, 500)
+        for longest in (None, 5000):
+            M.run(name, dtype, [1200], "whole", edit=edit, seed=77, longest=longest)
+    else:
+        def edit(prefix, own, q):
+            queries(q)
+            for t in (prefix, own):
+                for i, n in enumerate(t.lens):
+                    t.k[i, :n] = 0.0
+            t = prefix if where == "prefix" else own
+            for i, n in enumerate(t.lens):
+                if n > 60:
+                    keys(t.k[i, :n], t.c[i, :n], 50)
+        P.run(name, dtype, 1000, [3000, 70, 5], edit=edit, seed=78)
