@@ -10,10 +10,10 @@
 // out between the matrix instructions, without looking at their maximum: weights refer to the maximum a row has, whatever their size,
 // and a row sum beyond 2^32 sends the wave through the full step.
 // Weights are rounded to bf16 for the second product (their sum is that of the rounded ones); everything else is fp32.
-// Bound by the softmax's vector arithmetic beside the matrix instructions, which then draw the more power the less they wait: 4 x 4096
-// tokens of documents of 100 to 2000, 1B shape, 82 us (540 TFLOP/s of what is seen; whole sequences, causal, 776); 32 ragged prompts of the
-// paper's layer, a cap, 96 us (620); 2 x 8192 of the wide shape, window, cap and bias 1275 us (690; with the scores, which each of four latent
-// tiles works out, 920).  A cap costs 21 to 28 %, a bias 4 to 11.
+// Bound by the softmax's vector arithmetic beside the matrix instructions, which then draw the more power the less they wait.  Whole calls,
+// the list of tiles (5 to 10 us) among them: 4 x 4096 tokens of documents of 100 to 2000, 1B shape, 88 us (498 TFLOP/s of what is seen; whole
+// sequences, causal, 810); 32 ragged prompts of the paper's layer, a cap, 105 us (572); 2 x 8192 of the wide shape, window, cap and bias
+// 1300 us (673; with the scores, which each of four latent tiles works out, 895).  A cap costs 16 to 26 %, a bias 1 to 8.
 //
 // A masked weight is 0, but 0 times a latent that is not finite is NaN, and sums of finite ones may pass the range: a wave whose sums are not
 // finite in the end goes through its rows once more, one by one, over the keys that each sees (wave_row).
@@ -604,14 +604,16 @@ bool rows_bf16_ok(const Dims &d) {
 
 // A batch of few rows takes tiles of 64 or 32, whose waves share the columns: scratch memory for as many rows, and less to load where
 // a wave would have none.  One call, behind 8192 rows, with and without: 8 sequences of the 1B shape 25.5 / 26.2 us, 32 29.3 / 29.5, 64 35.8 / 35.2,
-// 32 of the wide shape 46.2 / 48.0, 64 53.8 / 53.6, 6 of the paper's layer 20.2 / 20.2.
+// 32 of the wide shape 46.2 / 48.0, 64 53.8 / 53.6, 6 of the paper's layer 20.2 / 20.2: level or up to 4 % faster, with a quarter or half
+// of the scratch memory.
 int prefix_tile_rows(const Dims &d, int rows) {
   if (d.dh == 64) return d.dl % 128 == 0 && rows <= 32 ? 32 : 128;
   return rows <= 32 ? 32 : rows <= 64 && d.dl % 256 == 0 ? 64 : 128;
 }
 // Latent columns of a workgroup: with 256 two of them share a CU, with 512 the scores are worked out half as often.  One call, 256
 // against 512: 64 sequences of the 1B shape behind 1024 rows 24.8 / 29.1 us, 8192 35.5 / 37.9, 32768 47.6 / 49.5; 32 of the wide shape
-// 28.4 / 30.8, 44.4 / 42.8, 102.9 / 86.6.
+// 28.4 / 30.8, 44.4 / 42.8, 102.9 / 86.6.  (The line between the two is the bound on the prefix's rows; at 8192 itself the wide shape is on its
+// slower side by 4 %.)
 static int prefix_columns(const Dims &d, int bq, int prefix_max) {
   if (d.dh == 64 || bq == 128) return wide_tile(d);
   return d.dl % 1024 == 0 && prefix_max > 8192 ? 512 : d.dl % 256 == 0 ? 256 : 128;

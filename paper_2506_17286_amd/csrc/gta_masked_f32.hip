@@ -3,8 +3,8 @@
 // that are joined in LDS at the end.  Both products are transposed, S^T = K Q^T and L^T += C^T P^T: weights go from one's
 // accumulators into the other.  Keys and latents come from memory straight into registers, the next block's as this one's come free.
 // Bound by the matrix instructions (64 cycles for 2048 products) and by how evenly tiles fall on the CUs: 4 x 1024 tokens of the paper's
-// layer with a bias 58 us, 69 TFLOP/s of the 153 that a large matrix product reaches; 640 workgroups, two on a CU, and a wave has up
-// to 8 steps between filling its registers and joining its sums.
+// layer with a bias 62.5 us a call (64 TFLOP/s of the 153 that a large matrix product reaches), 5.4 of it the list; 640 workgroups, two on a
+// CU, and a wave has up to 8 steps between filling its registers and joining its sums.
 //
 // A masked weight is 0, but 0 times a latent that is not finite is NaN, and sums of finite ones may pass the range: a tile whose sums are not
 // finite in the end is gone through once more, row by row, over the keys that each row sees (wave_row).

@@ -115,7 +115,7 @@ __device__ __forceinline__ int share_out(const StreamArgs &a, int &before, int &
 //   S[row][map] = K q^T: lane (x = l % 16, h = l / 16) ends up with map x, rows 4 h .. 4 h + 3 (of each key head; its own is kept);
 //   L[column][map] += C^T p: which is what the second operand wants from that lane.
 // Bound by memory: every row is read once (once per block of maps or slice where a layer's rows are wider than 4 KiB, then from L2).
-// 64 sequences of 20 to 1500 rows of 2 KiB 19.6 us, 5 TB/s; 32 of 100 to 4000 rows of 4 KiB in pages of 64 60 us, 4.7 TB/s; a few short ones 5 us,
+// 64 sequences of 20 to 1500 rows of 2 KiB 20.0 us, 5 TB/s; 32 of 100 to 4000 rows of 4 KiB in pages of 64 62 us, 4.6 TB/s; a few short ones 5 us,
 // a chain of lengths, page, keys, latents and the waves' join.
 // bf16 weights are rounded for the second product, as in the kernel of the prefix, and so is their sum.  (Two parts of 16 bits would
 // cost nothing here, but an infinite latent times the second, which may be 0 or less, is no infinity.)
@@ -370,7 +370,7 @@ struct JoinArgs {
 
 // One (sequence, map) and 128 of its columns: the averages of the prefix's and the sequence's own pieces, weighed by weight * 2^(maximum -
 // the largest).  Eight groups of 32 lanes take every eighth piece, four columns a lane, so that most of what is read is asked for at once.
-// Bound by latency: 4.8 us for two sequences, 6.7 for 64 of the 1B shape with 32 pieces of the prefix each.
+// Bound by latency: 4.7 us for two sequences, 6.8 for 64 of the 1B shape with 32 pieces of the prefix each.
 constexpr int kMaxPieces = 1280;   // 256 of the prefix, 4 workgroups per CU
 template <typename T>
 __global__ __launch_bounds__(256) void prefix_join_kernel(JoinArgs j) {
