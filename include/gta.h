@@ -409,10 +409,12 @@ GTA_API int gta_prefill_attention(const gta_config *cfg, const void *q, const vo
  *   cu_seqlens, batch, total_tokens, max_seqlen  as for gta_prefill.  Rows of l_out behind the last sequence are left as they are
  *   l_out    device [total_tokens, n_q*d_l], dense, 16-byte aligned; must not overlap the inputs
  *   workspace  mode PREFILL_MASKED
- * Sums and softmax statistics are fp32; bf16 weights are rounded before the product with the latents, and so is their sum.  The
- * average of finite latents is finite, up to 3.4e38 (rows whose sums are not are gone through twice).  head_dim up to 1024, latent_dim up to 4096, up to 65535 maps (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where
- * gta_uses_tuned_kernels(cfg, GTA_MODE_PREFILL_MASKED) is 1, rows consist of 16-byte aligned chunks and lie less than 64 MiB apart, on a
- * general kernel, 10 to 200 times slower, otherwise.  The first call with a cap, and with slopes, is one of a new shape to stream capture. */
+ * Sums and softmax statistics are fp32, and weights below 2^-126 are 0; bf16 weights are rounded before the product with the
+ * latents, and so is their sum, and capped scores of up to 256 are off by up to 6.9e-6 of themselves in bf16.  The average of finite
+ * latents is finite, up to 3.4e38 (rows whose sums are not are gone through twice).  head_dim up to 1024, latent_dim up to 4096, up to 65535
+ * maps (GTA_ERR_UNSUPPORTED).  Runs on the matrix instructions where gta_uses_tuned_kernels(cfg, GTA_MODE_PREFILL_MASKED) is 1, rows
+ * consist of 16-byte aligned chunks and lie less than 64 MiB apart, on a general kernel, 10 to 200 times slower, otherwise.  The first call
+ * with a cap, and with slopes, is one of a new shape to stream capture. */
 GTA_API int gta_prefill_masked_attention(const gta_config *cfg, const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                                          const void *c, int64_t c_stride, const int32_t *cu_seqlens, int32_t batch,
                                          int64_t total_tokens, int32_t max_seqlen, const gta_score_rules *rules, void *l_out,
